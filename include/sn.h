@@ -30,8 +30,9 @@
  *   - An id outside [0, vocab) (or a position outside [0, seq_len)) is never
  *     clamped: that token's output row is written as zeros and the basis'
  *     device error word records SN_ERR_BAD_ID, reported by sn_check_errors.
- *   - Only sn_basis_create allocates (and sn_basis_destroy frees); no other
- *     call allocates memory or falls back to the CPU.  A basis holds two
+ *   - Only sn_basis_create and sn_grads_create allocate (and their _destroy
+ *     calls free); no other call allocates memory or falls back to the CPU.
+ *     A basis holds two
  *     scratch areas of (SM count) x 128 x (k rounded up to 16) floats that the
  *     bf16 contractions use for the partial sums of their last-round row
  *     tiles: one for the forward calls (sn_compress_fwd,
@@ -287,6 +288,137 @@ sn_status sn_quant_compress(const void *X, int64_t T, int32_t d, int32_t format,
  * once to bf16. */
 sn_status sn_quant_restore(const uint8_t *codes, const float *scale, int64_t T, int32_t d,
                            int32_t format, void *X_out, sn_stream_t stream);
+
+/* ---- Embedding lookup and its gradient ------------------------------------------
+ * The first stage's residual stream, and the gradient of its table (the paper
+ * trains T_S; here any table [vocab, d] is looked up and trained).  Tables and
+ * outputs are contiguous; 1 <= d <= 2^20, vocab < 2^31, T < 2^31 - 512.  An id
+ * outside [0, vocab) gives a row of zeros and no gradient and, when `errors` is
+ * a basis (it may be NULL, and gives nothing but its error word), records
+ * SN_ERR_BAD_ID there. */
+
+/* X[t, :] = scale * table[ids[t], :], the product in fp32 rounded once.  table:
+ * [vocab, d] in table_dtype; ids: int32 [T]; X: [T, d] in out_dtype. */
+sn_status sn_embed_fwd(sn_basis_t errors, sn_dtype table_dtype, const void *table, int64_t vocab,
+                       int32_t d, const int32_t *ids, int64_t T, float scale, sn_dtype out_dtype,
+                       void *X, sn_stream_t stream);
+
+/* Bytes of device workspace that sn_embed_bwd needs. */
+sn_status sn_embed_bwd_workspace(int64_t T, int64_t vocab, int32_t d, size_t *bytes);
+
+/* dtable[v, :] = scale * sum over the t with ids[t] = v of G[t, :]; ids without
+ * tokens get zeros.  With accumulate != 0 the sums are added to dtable, whose
+ * other rows are neither read nor written.  G: [T, d] in dtype with row stride
+ * ldg (elements); dtable: [vocab, d] in grad_dtype.  Tokens are sorted by id and
+ * each row summed in fp32 in a fixed order (no atomics: the same inputs give
+ * the same bits) and rounded once.  workspace: 256-byte aligned, at least
+ * sn_embed_bwd_workspace bytes, used only during the call. */
+sn_status sn_embed_bwd(sn_basis_t errors, sn_dtype dtype, const void *G, int64_t ldg, int64_t T,
+                       int32_t d, const int32_t *ids, float scale, sn_dtype grad_dtype,
+                       void *dtable, int64_t vocab, int32_t accumulate, void *workspace,
+                       size_t workspace_bytes, sn_stream_t stream);
+
+/* ---- RMS norm of the residual stream ----------------------------------------------
+ *   h = x + r,   y = h / sqrt(mean(h^2) + eps) * w          (row by row)
+ * X, R, H, Y and the gradients share `dtype`; w: [d] in w_dtype.  X: [T, d] with
+ * row stride ldx (elements); the others contiguous.  R may be NULL (h = x); H
+ * may be NULL (h is not stored).  h is summed in fp32 and rounded once when it is
+ * stored; y comes from the unrounded h and is rounded once.  H may be R, and where
+ * ldx = d also X; Y may be X or R (where ldx = d).  Other overlaps are
+ * SN_ERR_INVALID_ARG.  eps >= 0 and finite; 1 <= d <= 2^20.  A row with an
+ * infinity or a NaN gives NaN. */
+sn_status sn_rmsnorm_fwd(sn_dtype dtype, const void *X, int64_t ldx, const void *R, void *H,
+                         sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps, void *Y,
+                         sn_stream_t stream);
+
+/* The same with y in 8 bits (formats of sn_quant_compress): for a row, or with
+ * group = 32, 64 or 128 for every `group` columns of it (the last may be fewer),
+ *   a = max |y|,  scale = a / qmax,  code = Q(y * (qmax / a)),   from y in fp32.
+ * codes: uint8 [T, d]; scale: fp32 [T] (group = 0) or [T, ceil(d / group)].  A
+ * group of zeros has scale 0; below 2^-100, a counts as 2^-100; a NaN or an
+ * infinity in a group makes its scale one. */
+sn_status sn_rmsnorm_fwd_quant(sn_dtype dtype, const void *X, int64_t ldx, const void *R, void *H,
+                               sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps,
+                               int32_t format, int32_t group, uint8_t *codes, float *scale,
+                               sn_stream_t stream);
+
+/* Bytes of device workspace that sn_rmsnorm_bwd needs. */
+sn_status sn_rmsnorm_bwd_workspace(int64_t T, int32_t d, size_t *bytes);
+
+/* The gradient, from the h that the forward stored (X itself without a residual):
+ *   g = dy * w,  n = h / sqrt(mean(h^2) + eps),
+ *   dx = (g - n mean(g n)) / sqrt(mean(h^2) + eps) + dH,   dw = sum_t dy n
+ * dX is the gradient of x and of r alike.  dY: [T, d] with row stride ldy; dH:
+ * the gradient that reaches h along the residual stream, or NULL; dw: fp32 [d],
+ * added to with accumulate != 0.  dX may be dH, H, or (where ldy = d) dY.
+ * workspace: 16-byte aligned, at least sn_rmsnorm_bwd_workspace bytes. */
+sn_status sn_rmsnorm_bwd(sn_dtype dtype, const void *dY, int64_t ldy, const void *H, const void *dH,
+                         sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps, void *dX,
+                         float *dw, int32_t accumulate, void *workspace, size_t workspace_bytes,
+                         sn_stream_t stream);
+
+/* ---- Log probabilities of given tokens ----------------------------------------------
+ * The last stage's loss and a server's scores.  logits: [T, vocab] in dtype with
+ * row stride ld (elements); z = scale * logits, scale > 0 (the inverse temperature).
+ *   logp[t] = ln p[t, target[t]],   p = exp(z) / sum_v exp(z),
+ *   entropy[t] = -sum_v p ln p
+ * lse: fp32 [T, 2], ln sum_v exp(z) in two parts: the largest logit m, and
+ * ln sum_v exp(scale * (logits - m)); the sum is scale * m plus the second
+ * and the `top` largest logits of a row in order (the lower token first among
+ * equals): top_ids int32 [T, top], top_logp fp32 [T, top].  0 <= top <= 32 and
+ * top <= vocab; logp, entropy (fp32 [T]) and lse (8-byte aligned) may each be NULL,
+ * target and logp only together.  A negative target is none: logp 0.  A target >= vocab counts as
+ * none and records SN_ERR_BAD_ID where `errors` is a basis (it may be NULL).
+ * -infinity masks a token out; a row of nothing else has both parts of lse and
+ * every log probability -infinity and entropy 0.  A row with a NaN or +infinity gives NaN
+ * (its alternatives are the NaNs first). */
+sn_status sn_logprob_fwd(sn_basis_t errors, sn_dtype dtype, const void *logits, int64_t T,
+                         int64_t vocab, int64_t ld, const int32_t *target, float scale, float *logp,
+                         float *lse, float *entropy, int32_t top, int32_t *top_ids, float *top_logp,
+                         sn_stream_t stream);
+
+/* The gradient of logp and entropy with respect to the logits, from sn_logprob_fwd's
+ * lse (and entropy):
+ *   dlogits[t, v] = scale * (dlogp[t] ([v = target[t]] - p) - dentropy[t] p (ln p + entropy[t]))
+ * Tokens without a target have no first term; a row without a token gets zeros.  dlogp with target, dentropy with entropy: either pair may be NULL.  dlogits:
+ * [T, vocab] in dtype with row stride ldd; it may be logits (with ldd = ld). */
+sn_status sn_logprob_bwd(sn_dtype dtype, const void *logits, int64_t T, int64_t vocab, int64_t ld,
+                         const int32_t *target, const float *lse, const float *dlogp,
+                         const float *entropy, const float *dentropy, float scale, void *dlogits,
+                         int64_t ldd, sn_stream_t stream);
+
+/* ---- Global gradient norm and clipping ------------------------------------------------
+ * A list of gradient tensors is described once (the handle keeps a table of them in
+ * device memory), then summed and scaled in one launch each:
+ *   sumsq = sum over all tensors of g^2 (fp64),   norm = sqrt(sumsq),
+ *   dst = src * c,   c = max_norm / max(norm, max_norm)
+ * Where stages or ranks hold parts of a model, their sums are added between the two
+ * calls. */
+typedef struct sn_grads *sn_grads_t;
+
+/* src[i]: count[i] >= 0 contiguous elements in src_dtype[i] (SN_BF16 or SN_F32), dst[i]
+ * as many in dst_dtype[i]; each aligned to its element (16 bytes run faster).  dst[i]
+ * may be src[i] with the same type (in place); any other overlap of a destination
+ * with a source or another destination is SN_ERR_INVALID_ARG, so a tensor is listed
+ * once.  The five arrays are host memory and only read here; the tensors stay the
+ * caller's and must outlive the handle.  Allocates, and synchronises `stream`. */
+sn_status sn_grads_create(int32_t n, const void *const *src, const sn_dtype *src_dtype,
+                          const int64_t *count, void *const *dst, const sn_dtype *dst_dtype,
+                          sn_grads_t *out, sn_stream_t stream);
+
+/* Free a handle (synchronises the device).  NULL is a no-op. */
+sn_status sn_grads_destroy(sn_grads_t grads);
+
+/* *sumsq = (or with accumulate != 0, +=) the sum of the squares of all sources; device
+ * fp64.  Right for every finite gradient (no overflow, no underflow); the same inputs
+ * give the same bits.  Calls on one handle may not overlap each other in time. */
+sn_status sn_grads_sumsq(sn_grads_t grads, double *sumsq, int32_t accumulate, sn_stream_t stream);
+
+/* *norm = sqrt(*sumsq) (fp32, device memory; with one rounding), and every destination
+ * written.  In place with norm <= max_norm nothing is touched.  max_norm > 0 and finite.
+ * An infinite norm scales by 0, a NaN by NaN. */
+sn_status sn_grads_clip(sn_grads_t grads, const double *sumsq, float max_norm, float *norm,
+                        sn_stream_t stream);
 
 /* Bytes on the wire for T tokens: T * k * element size (Sec. 4.3: k/d of X). */
 sn_status sn_wire_bytes(sn_basis_t basis, sn_dtype dtype, int64_t T, size_t *bytes);

@@ -1,10 +1,13 @@
 // sn_api.cu — the C ABI (include/sn.h): argument validation, basis handles,
 // the launch of each call's kernels (bf16: tcgen05 tensor-core kernels; fp32:
 // CUDA-core kernels), the wire copies and the asynchronous error word.
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 #include <initializer_list>
 #include <new>
+#include <vector>
 
 #include "sn_internal.cuh"
 
@@ -624,6 +627,346 @@ sn_status sn_quant_restore(const uint8_t *codes, const float *scale, int64_t T, 
         return SN_ERR_INVALID_ARG;
     return cuda_status(sn::lossy_quant_restore(codes, scale, T, d, format, X_out,
                                                (cudaStream_t)stream));
+}
+
+namespace {
+
+bool is_dtype(sn_dtype dt) { return dt == SN_BF16 || dt == SN_F32; }
+
+// A buffer of a call: `rows` rows of `width` elements of `es` bytes, `ld` elements apart
+struct Buf {
+    const void *p;
+    size_t bytes;
+    Buf(const void *p, int64_t rows, int64_t width, int64_t ld, size_t es)
+        : p(p), bytes(p && rows > 0 ? ((size_t)(rows - 1) * ld + width) * es : 0) {}
+};
+
+bool clash(const Buf &a, const Buf &b) { return a.bytes && b.bytes && overlap(a.p, a.bytes, b.p, b.bytes); }
+
+// Whether `out` overlaps one of `others`
+bool clashes(const Buf &out, std::initializer_list<Buf> others)
+{
+    for (const Buf &b : others)
+        if (clash(out, b))
+            return true;
+    return false;
+}
+
+// Whether `out` overlaps `in` other than by being it, row by row
+bool clashes_unless_same(const Buf &out, const Buf &in, bool same_rows)
+{
+    return clash(out, in) && !(out.p == in.p && same_rows);
+}
+
+constexpr int32_t kMaxWidth = 1 << 20;
+constexpr int64_t kMaxTokens = kMaxRows - 512;   // places of a list of tokens are 32-bit
+
+// The error word that out-of-range ids are recorded in: none without a basis
+sn_status error_word(sn_basis_t b, unsigned int **err)
+{
+    *err = nullptr;
+    if (!b)
+        return SN_OK;
+    const sn_status st = check_basis(b, SN_F32);
+    if (st == SN_OK)
+        *err = b->err;
+    return st;
+}
+
+sn_status check_norm(sn_dtype dt, sn_dtype wdt, int64_t T, int32_t d, int64_t ld, float eps)
+{
+    if (!is_dtype(dt) || !is_dtype(wdt) || T < 0 || T >= kMaxRows || d < 1 || d > kMaxWidth || ld < d ||
+        ld >= kMaxRows || !(eps >= 0.f) || !std::isfinite(eps))
+        return SN_ERR_INVALID_ARG;
+    return SN_OK;
+}
+
+// Both forwards: format < 0 writes Y
+sn_status norm_fwd(sn_dtype dt, const void *X, int64_t ldx, const void *R, void *H, sn_dtype wdt, const void *w,
+                   int64_t T, int32_t d, float eps, void *Y, int32_t format, int32_t group, uint8_t *codes,
+                   float *scale, cudaStream_t s)
+{
+    sn_status st = check_norm(dt, wdt, T, d, ldx, eps);
+    if (st != SN_OK || T == 0)
+        return st;
+    const bool quant = format >= 0;
+    if (!X || !w || (quant ? !codes || !scale : !Y))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(X, 16) || !aligned(R, 16) || !aligned(H, 16) || !aligned(w, 16) || !aligned(Y, 16) ||
+        !aligned(codes, 16) || !aligned(scale, 4))
+        return SN_ERR_ALIGNMENT;
+    const size_t es = esize(dt);
+    const int64_t groups = group ? (d + group - 1) / group : 1;
+    const Buf x(X, T, d, ldx, es), r(R, T, d, d, es), h(H, T, d, d, es), y(Y, T, d, d, es), c(codes, T, d, d, 1),
+        q(scale, T, groups, groups, 4), wb(w, 1, d, d, esize(wdt));
+    if (clashes_unless_same(h, x, ldx == d) || clashes_unless_same(h, r, true) ||
+        clashes_unless_same(y, x, ldx == d) || clashes_unless_same(y, r, true) || clashes(h, {y, c, q, wb}) ||
+        clashes(wb, {y, c, q}) || clashes(c, {x, r, q}) || clashes(q, {x, r}) ||
+        !on_device({X, R, H, w, Y, codes, scale}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::rmsnorm_fwd(dt, X, ldx, R, H, wdt, w, T, d, eps, Y, format, group, codes, scale, s));
+}
+
+}  // namespace
+
+sn_status sn_embed_fwd(sn_basis_t errors, sn_dtype tdt, const void *table, int64_t vocab, int32_t d,
+                       const int32_t *ids, int64_t T, float scale, sn_dtype xdt, void *X, sn_stream_t stream)
+{
+    unsigned int *err;
+    const sn_status st = error_word(errors, &err);
+    if (st != SN_OK)
+        return st;
+    if (!is_dtype(tdt) || !is_dtype(xdt) || vocab < 1 || vocab >= kMaxRows || d < 1 || d > kMaxWidth || T < 0 ||
+        T >= kMaxTokens)
+        return SN_ERR_INVALID_ARG;
+    if (T == 0)
+        return SN_OK;
+    if (!table || !ids || !X)
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(table, 16) || !aligned(ids, 4) || !aligned(X, 16))
+        return SN_ERR_ALIGNMENT;
+    if (clashes(Buf(X, T, d, d, esize(xdt)), {Buf(table, vocab, d, d, esize(tdt)), Buf(ids, 1, T, T, 4)}) ||
+        !on_device({table, ids, X}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::embed_fwd(tdt, table, vocab, d, ids, T, scale, xdt, X, err, (cudaStream_t)stream));
+}
+
+sn_status sn_embed_bwd_workspace(int64_t T, int64_t vocab, int32_t d, size_t *bytes)
+{
+    if (!bytes || T < 0 || T >= kMaxTokens || vocab < 1 || vocab >= kMaxRows || d < 1 || d > kMaxWidth)
+        return SN_ERR_INVALID_ARG;
+    *bytes = sn::embed_bwd_workspace(T, vocab, d);
+    return SN_OK;
+}
+
+sn_status sn_embed_bwd(sn_basis_t errors, sn_dtype dt, const void *G, int64_t ldg, int64_t T, int32_t d,
+                       const int32_t *ids, float scale, sn_dtype edt, void *dE, int64_t vocab, int32_t accumulate,
+                       void *ws, size_t ws_bytes, sn_stream_t stream)
+{
+    unsigned int *err;
+    const sn_status st = error_word(errors, &err);
+    if (st != SN_OK)
+        return st;
+    size_t need = 0;
+    if (!is_dtype(dt) || !is_dtype(edt) || sn_embed_bwd_workspace(T, vocab, d, &need) != SN_OK || ldg < d ||
+        ldg >= kMaxRows)
+        return SN_ERR_INVALID_ARG;
+    if (T == 0 && accumulate)
+        return SN_OK;
+    if ((T > 0 && (!G || !ids)) || !dE || !ws || ws_bytes < need)
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(G, 16) || !aligned(ids, 4) || !aligned(dE, 16) || !aligned(ws, 256))
+        return SN_ERR_ALIGNMENT;
+    const Buf g(G, T, d, ldg, esize(dt)), i(ids, 1, T, T, 4), e(dE, vocab, d, d, esize(edt)), w(ws, 1, need, need, 1);
+    if (clashes(e, {g, i, w}) || clashes(w, {g, i}) || !on_device({G, ids, dE, ws}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::embed_bwd(dt, G, ldg, T, d, ids, scale, edt, dE, vocab, accumulate != 0, ws, err,
+                                     (cudaStream_t)stream));
+}
+
+sn_status sn_rmsnorm_fwd(sn_dtype dt, const void *X, int64_t ldx, const void *R, void *H, sn_dtype wdt,
+                         const void *w, int64_t T, int32_t d, float eps, void *Y, sn_stream_t stream)
+{
+    return norm_fwd(dt, X, ldx, R, H, wdt, w, T, d, eps, Y, -1, 0, nullptr, nullptr, (cudaStream_t)stream);
+}
+
+sn_status sn_rmsnorm_fwd_quant(sn_dtype dt, const void *X, int64_t ldx, const void *R, void *H, sn_dtype wdt,
+                               const void *w, int64_t T, int32_t d, float eps, int32_t format, int32_t group,
+                               uint8_t *codes, float *scale, sn_stream_t stream)
+{
+    if ((format != SN_Q_INT8 && format != SN_Q_E4M3) || (group != 0 && group != 32 && group != 64 && group != 128))
+        return SN_ERR_INVALID_ARG;
+    return norm_fwd(dt, X, ldx, R, H, wdt, w, T, d, eps, nullptr, format, group, codes, scale,
+                    (cudaStream_t)stream);
+}
+
+sn_status sn_rmsnorm_bwd_workspace(int64_t T, int32_t d, size_t *bytes)
+{
+    if (!bytes || T < 0 || T >= kMaxRows || d < 1 || d > kMaxWidth)
+        return SN_ERR_INVALID_ARG;
+    *bytes = sn::rmsnorm_bwd_workspace(T, d);
+    return SN_OK;
+}
+
+sn_status sn_rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H, const void *dH, sn_dtype wdt,
+                         const void *w, int64_t T, int32_t d, float eps, void *dX, float *dw, int32_t accumulate,
+                         void *ws, size_t ws_bytes, sn_stream_t stream)
+{
+    const sn_status st = check_norm(dt, wdt, T, d, ldy, eps);
+    if (st != SN_OK || (T == 0 && accumulate))
+        return st;
+    const size_t need = sn::rmsnorm_bwd_workspace(T, d);
+    if (!dw || (T > 0 && (!dY || !H || !w || !dX || !ws || ws_bytes < need)))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(dY, 16) || !aligned(H, 16) || !aligned(dH, 16) || !aligned(w, 16) || !aligned(dX, 16) ||
+        !aligned(dw, 16) || !aligned(ws, 16))
+        return SN_ERR_ALIGNMENT;
+    const size_t es = esize(dt);
+    const Buf y(dY, T, d, ldy, es), h(H, T, d, d, es), r(dH, T, d, d, es), x(dX, T, d, d, es),
+        wb(T > 0 ? w : nullptr, 1, d, d, esize(wdt)), g(dw, 1, d, d, 4), p(T > 0 ? ws : nullptr, 1, need, need, 1);
+    if (clashes_unless_same(x, y, ldy == d) || clashes_unless_same(x, h, true) || clashes_unless_same(x, r, true) ||
+        clashes(x, {wb, g, p}) || clashes(g, {y, h, r, wb, p}) || clashes(p, {y, h, r, wb}) ||
+        !on_device({dY, H, dH, w, dX, dw, ws}))
+        return SN_ERR_INVALID_ARG;
+    if (T == 0)
+        return cuda_status(cudaMemsetAsync(dw, 0, (size_t)d * 4, (cudaStream_t)stream));
+    return cuda_status(sn::rmsnorm_bwd(dt, dY, ldy, H, dH, wdt, w, T, d, eps, dX, dw, accumulate != 0, (float *)ws,
+                                       (cudaStream_t)stream));
+}
+
+namespace {
+sn_status check_logits(sn_dtype dt, int64_t T, int64_t V, int64_t ld, float scale)
+{
+    if (!is_dtype(dt) || T < 0 || T >= kMaxRows || V < 1 || V >= kMaxTokens || ld < V || ld >= kMaxRows ||
+        !(scale > 0.f) || !std::isfinite(scale))
+        return SN_ERR_INVALID_ARG;
+    return SN_OK;
+}
+}  // namespace
+
+sn_status sn_logprob_fwd(sn_basis_t errors, sn_dtype dt, const void *x, int64_t T, int64_t V, int64_t ld,
+                         const int32_t *target, float scale, float *logp, float *lse, float *entropy, int32_t top,
+                         int32_t *top_ids, float *top_logp, sn_stream_t stream)
+{
+    unsigned int *err;
+    sn_status st = error_word(errors, &err);
+    if (st == SN_OK)
+        st = check_logits(dt, T, V, ld, scale);
+    if (st != SN_OK)
+        return st;
+    if (top < 0 || top > 32 || top > V)
+        return SN_ERR_INVALID_ARG;
+    if (T == 0)
+        return SN_OK;
+    if (!x || (target == nullptr) != (logp == nullptr) || (top > 0 && (!top_ids || !top_logp)) ||
+        (!logp && !lse && !entropy && top == 0))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(target, 4) || !aligned(logp, 4) || !aligned(lse, 8) || !aligned(entropy, 4) ||
+        !aligned(top_ids, 4) || !aligned(top_logp, 4))
+        return SN_ERR_ALIGNMENT;
+    if (top == 0)
+        top_ids = nullptr, top_logp = nullptr;
+    const Buf in(x, T, V, ld, esize(dt)), tg(target, 1, T, T, 4), a(logp, 1, T, T, 4), b(lse, T, 2, 2, 4),
+        c(entropy, 1, T, T, 4), i(top_ids, T, top, top, 4), l(top_logp, T, top, top, 4);
+    if (clashes(a, {in, tg, b, c, i, l}) || clashes(b, {in, tg, c, i, l}) || clashes(c, {in, tg, i, l}) ||
+        clashes(i, {in, tg, l}) || clashes(l, {in, tg}) ||
+        !on_device({x, target, logp, lse, entropy, top_ids, top_logp}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::logprob_fwd(dt, x, T, (int)V, ld, target, scale, logp, lse, entropy, top, top_ids,
+                                       top_logp, err, (cudaStream_t)stream));
+}
+
+sn_status sn_logprob_bwd(sn_dtype dt, const void *x, int64_t T, int64_t V, int64_t ld, const int32_t *target,
+                         const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
+                         float scale, void *dx, int64_t ldd, sn_stream_t stream)
+{
+    const sn_status st = check_logits(dt, T, V, ld, scale);
+    if (st != SN_OK)
+        return st;
+    if (ldd < V || ldd >= kMaxRows)
+        return SN_ERR_INVALID_ARG;
+    if (T == 0)
+        return SN_OK;
+    if (!x || !lse || !dx || (target == nullptr) != (dlogp == nullptr) ||
+        (entropy == nullptr) != (dentropy == nullptr) || (!dlogp && !dentropy))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(dx, 16) || !aligned(target, 4) || !aligned(lse, 8) || !aligned(dlogp, 4) ||
+        !aligned(entropy, 4) || !aligned(dentropy, 4))
+        return SN_ERR_ALIGNMENT;
+    const size_t es = esize(dt);
+    const Buf in(x, T, V, ld, es), out(dx, T, V, ldd, es);
+    if (clashes_unless_same(out, in, ld == ldd) ||
+        clashes(out, {Buf(target, 1, T, T, 4), Buf(lse, T, 2, 2, 4), Buf(dlogp, 1, T, T, 4),
+                      Buf(entropy, 1, T, T, 4), Buf(dentropy, 1, T, T, 4)}) ||
+        !on_device({x, target, lse, dlogp, entropy, dentropy, dx}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::logprob_bwd(dt, x, T, (int)V, ld, target, lse, dlogp, entropy, dentropy, scale, dx, ldd,
+                                       (cudaStream_t)stream));
+}
+
+sn_status sn_grads_create(int32_t n, const void *const *src, const sn_dtype *sdt, const int64_t *count,
+                          void *const *dst, const sn_dtype *ddt, sn_grads_t *out, sn_stream_t stream)
+try {
+    if (n < 0 || !out || (n > 0 && (!src || !sdt || !count || !dst || !ddt)))
+        return SN_ERR_INVALID_ARG;
+    // every source and destination as a range of addresses; a destination may meet only
+    // its own source
+    struct Range {
+        uintptr_t at, end;
+        int tensor;
+        bool dst;
+    };
+    std::vector<Range> ranges;
+    for (int i = 0; i < n; ++i) {
+        if (!is_dtype(sdt[i]) || !is_dtype(ddt[i]) || count[i] < 0 || count[i] >= (int64_t)1 << 48)
+            return SN_ERR_INVALID_ARG;
+        if (count[i] == 0)
+            continue;
+        if (!src[i] || !dst[i])
+            return SN_ERR_INVALID_ARG;
+        if (!aligned(src[i], esize(sdt[i])) || !aligned(dst[i], esize(ddt[i])))
+            return SN_ERR_ALIGNMENT;
+        if (!on_device({src[i], dst[i]}) || (src[i] == dst[i] && sdt[i] != ddt[i]))
+            return SN_ERR_INVALID_ARG;
+        const uintptr_t p = (uintptr_t)src[i], q = (uintptr_t)dst[i];
+        if (p != q)
+            ranges.push_back({p, p + (size_t)count[i] * esize(sdt[i]), i, false});
+        ranges.push_back({q, q + (size_t)count[i] * esize(ddt[i]), i, true});
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.at < b.at; });
+    uintptr_t end = 0, dst_end = 0;           // of everything, and of the destinations, so far
+    for (const Range &r : ranges) {
+        if (r.at < (r.dst ? end : dst_end))
+            return SN_ERR_INVALID_ARG;
+        end = std::max(end, r.end);
+        if (r.dst)
+            dst_end = std::max(dst_end, r.end);
+    }
+    return cuda_status(sn::grads_create(n, src, sdt, count, dst, ddt, out, (cudaStream_t)stream));
+} catch (const std::exception &) {
+    return SN_ERR_CUDA;                       // no host memory
+}
+
+sn_status sn_grads_destroy(sn_grads_t g) { return g ? cuda_status(sn::grads_destroy(g)) : SN_OK; }
+
+namespace {
+sn_status check_grads(sn_grads_t g)
+{
+    int dev = -1;
+    if (!g)
+        return SN_ERR_INVALID_ARG;
+    if (cudaGetDevice(&dev) != cudaSuccess)
+        return SN_ERR_CUDA;
+    return dev == sn::grads_device(g) ? SN_OK : SN_ERR_INVALID_ARG;
+}
+}  // namespace
+
+sn_status sn_grads_sumsq(sn_grads_t g, double *sumsq, int32_t accumulate, sn_stream_t stream)
+{
+    const sn_status st = check_grads(g);
+    if (st != SN_OK)
+        return st;
+    if (!sumsq)
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(sumsq, 8))
+        return SN_ERR_ALIGNMENT;
+    if (!on_device({sumsq}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::grads_sumsq(*g, sumsq, accumulate != 0, (cudaStream_t)stream));
+}
+
+sn_status sn_grads_clip(sn_grads_t g, const double *sumsq, float max_norm, float *norm, sn_stream_t stream)
+{
+    const sn_status st = check_grads(g);
+    if (st != SN_OK)
+        return st;
+    if (!sumsq || !norm || !(max_norm > 0.f) || !std::isfinite(max_norm))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(sumsq, 8) || !aligned(norm, 4))
+        return SN_ERR_ALIGNMENT;
+    if (overlap(sumsq, 8, norm, 4) || !on_device({sumsq, norm}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::grads_clip(*g, sumsq, max_norm, norm, (cudaStream_t)stream));
 }
 
 sn_status sn_wire_bytes(sn_basis_t b, sn_dtype dt, int64_t T, size_t *bytes)

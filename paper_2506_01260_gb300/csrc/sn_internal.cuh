@@ -193,6 +193,35 @@ cudaError_t lossy_quant(const void *X, int64_t T, int d, int format, uint8_t *co
                         cudaStream_t s);
 cudaError_t lossy_quant_restore(const uint8_t *codes, const float *scale, int64_t T, int d,
                                 int format, void *out, cudaStream_t s);
+// Embedding lookup and its gradient (err: null or a basis' error word)
+cudaError_t embed_fwd(sn_dtype table_dt, const void *table, int64_t vocab, int d, const int32_t *ids, int64_t T,
+                      float scale, sn_dtype out_dt, void *X, unsigned int *err, cudaStream_t s);
+size_t embed_bwd_workspace(int64_t T, int64_t vocab, int d);
+cudaError_t embed_bwd(sn_dtype dt, const void *G, int64_t ldg, int64_t T, int d, const int32_t *ids, float scale,
+                      sn_dtype grad_dt, void *dE, int64_t vocab, bool accumulate, void *ws, unsigned int *err,
+                      cudaStream_t s);
+// RMS norm with the residual's addition; format < 0: Y, else codes and scales
+cudaError_t rmsnorm_fwd(sn_dtype dt, const void *X, int64_t ldx, const void *R, void *H, sn_dtype wdt,
+                        const void *w, int64_t T, int d, float eps, void *Y, int format, int group,
+                        uint8_t *codes, float *scale, cudaStream_t s);
+size_t rmsnorm_bwd_workspace(int64_t T, int d);
+cudaError_t rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H, const void *dH, sn_dtype wdt,
+                        const void *w, int64_t T, int d, float eps, void *dX, float *dw, bool accumulate,
+                        float *part, cudaStream_t s);
+// Log probabilities of given tokens, entropy and alternatives; their gradient
+cudaError_t logprob_fwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld, const int32_t *target,
+                        float scale, float *logp, float *lse, float *entropy, int top, int32_t *top_ids,
+                        float *top_logp, unsigned int *err, cudaStream_t s);
+cudaError_t logprob_bwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld, const int32_t *target,
+                        const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
+                        float scale, void *dx, int64_t ldd, cudaStream_t s);
+// Global gradient norm and clipping (grads_create may throw std::bad_alloc)
+cudaError_t grads_create(int n, const void *const *src, const sn_dtype *src_dt, const int64_t *count,
+                         void *const *dst, const sn_dtype *dst_dt, sn_grads **out, cudaStream_t s);
+cudaError_t grads_destroy(sn_grads *g);
+int grads_device(const sn_grads *g);
+cudaError_t grads_sumsq(const sn_grads &g, double *sumsq, bool accumulate, cudaStream_t s);
+cudaError_t grads_clip(const sn_grads &g, const double *sumsq, float max_norm, float *norm, cudaStream_t s);
 // C = X U - TU[ids] - PU[pos] (PU may be null)
 cudaError_t tc_compress_projected(const sn_basis &b, const __nv_bfloat16 *X, const int32_t *ids,
                                   const int32_t *pos, int64_t T, int seq_len, const float *TU,

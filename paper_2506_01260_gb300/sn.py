@@ -65,6 +65,21 @@ _sig("sn_sign_compress", [_P, _I64, _I32, _P, _P, _P])
 _sig("sn_sign_restore", [_P, _P, _I64, _I32, _P, _P])
 _sig("sn_quant_compress", [_P, _I64, _I32, _I32, _P, _P, _P])
 _sig("sn_quant_restore", [_P, _P, _I64, _I32, _I32, _P, _P])
+_F = ctypes.c_float
+_sig("sn_embed_fwd", [_P, _ST, _P, _I64, _I32, _P, _I64, _F, _ST, _P, _P])
+_sig("sn_embed_bwd_workspace", [_I64, _I64, _I32, ctypes.POINTER(_SZ)])
+_sig("sn_embed_bwd", [_P, _ST, _P, _I64, _I64, _I32, _P, _F, _ST, _P, _I64, _I32, _P, _SZ, _P])
+_sig("sn_rmsnorm_fwd", [_ST, _P, _I64, _P, _P, _ST, _P, _I64, _I32, _F, _P, _P])
+_sig("sn_rmsnorm_fwd_quant", [_ST, _P, _I64, _P, _P, _ST, _P, _I64, _I32, _F, _I32, _I32, _P, _P,
+                              _P])
+_sig("sn_rmsnorm_bwd_workspace", [_I64, _I32, ctypes.POINTER(_SZ)])
+_sig("sn_rmsnorm_bwd", [_ST, _P, _I64, _P, _P, _ST, _P, _I64, _I32, _F, _P, _P, _I32, _P, _SZ, _P])
+_sig("sn_logprob_fwd", [_P, _ST, _P, _I64, _I64, _I64, _P, _F, _P, _P, _P, _I32, _P, _P, _P])
+_sig("sn_logprob_bwd", [_ST, _P, _I64, _I64, _I64, _P, _P, _P, _P, _P, _F, _P, _I64, _P])
+_sig("sn_grads_create", [_I32, _P, _P, _P, _P, _P, ctypes.POINTER(_P), _P])
+_sig("sn_grads_destroy", [_P])
+_sig("sn_grads_sumsq", [_P, _P, _I32, _P])
+_sig("sn_grads_clip", [_P, _P, _F, _P, _P])
 _sig("sn_wire_bytes", [_P, _ST, _I64, ctypes.POINTER(_SZ)])
 _sig("sn_wire_send", [_P, _P, _SZ, _P])
 _sig("sn_wire_recv", [_P, _P, _SZ, _P])
@@ -82,6 +97,9 @@ EXPORTS = ["sn_basis_create", "sn_basis_destroy", "sn_basis_shape", "sn_compress
            "sn_grassmann_workspace", "sn_grassmann_accumulate", "sn_grassmann_residual",
            "sn_grassmann_step", "sn_adamw_rowconst", "sn_topk_compress", "sn_topk_restore",
            "sn_sign_compress", "sn_sign_restore", "sn_quant_compress", "sn_quant_restore",
+           "sn_embed_fwd", "sn_embed_bwd_workspace", "sn_embed_bwd", "sn_rmsnorm_fwd",
+           "sn_rmsnorm_fwd_quant", "sn_rmsnorm_bwd_workspace", "sn_rmsnorm_bwd", "sn_logprob_fwd",
+           "sn_logprob_bwd", "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
            "sn_wire_bytes", "sn_wire_send",
            "sn_wire_recv", "sn_check_errors", "sn_selftest_wait_timeout",
            "sn_selftest_barrier_timeout", "sn_launch_count",
@@ -469,6 +487,298 @@ def sn_quant_restore(codes, scale, fmt, out=None, stream=None):
     _check(_lib.sn_quant_restore(_ptr(codes), _ptr(scale), T, d, QUANT_FORMATS[fmt], _ptr(out),
                                  _stream(stream)), "sn_quant_restore")
     return out
+
+
+def _rows(t, name, dtype=None):
+    """A 2-D tensor whose columns are contiguous; returns its row stride."""
+    _need(t, name, dtype, contiguous=False)
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be 2-D with unit column stride" % name)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _error_basis(basis):
+    return None if basis is None else basis.handle
+
+
+def sn_embed_fwd(table, ids, scale=1.0, out=None, out_dtype=None, basis=None, stream=None):
+    """X = scale * table[ids] ([T, d], in `out_dtype`, by default the table's).  An id out of
+    range gives zeros and, with a basis, SN_ERR_BAD_ID at its next sn_check_errors."""
+    _need(table, "table")
+    _need(ids, "ids", torch.int32)
+    if table.dim() != 2 or ids.dim() != 1:
+        raise ValueError("table must be [vocab, d] and ids [T]")
+    V, d = table.shape
+    T = ids.shape[0]
+    if out is None:
+        out = torch.empty(T, d, dtype=out_dtype or table.dtype, device=table.device)
+    _need(out, "out", out_dtype)
+    _check_out(out, (T, d))
+    _check(_lib.sn_embed_fwd(_error_basis(basis), _dtype(table), _ptr(table), V, d, _ptr(ids), T,
+                             scale, _dtype(out), _ptr(out), _stream(stream)), "sn_embed_fwd")
+    return out
+
+
+def sn_embed_bwd_workspace(T, vocab, d):
+    n = _SZ()
+    _check(_lib.sn_embed_bwd_workspace(T, vocab, d, ctypes.byref(n)), "sn_embed_bwd_workspace")
+    return n.value
+
+
+def sn_embed_bwd(G, ids, vocab, scale=1.0, out=None, out_dtype=None, accumulate=False, basis=None,
+                 workspace=None, stream=None):
+    """The table's gradient [vocab, d]: scale times the sum of G's rows of each id, zeros for
+    ids without tokens; with accumulate=True added to `out`.  G may be a row-strided view."""
+    ldg = _rows(G, "G")
+    _need(ids, "ids", torch.int32)
+    T, d = G.shape
+    if ids.shape != (T,):
+        raise ValueError("ids must have shape [T]")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate=True needs out")
+        out = torch.empty(vocab, d, dtype=out_dtype or G.dtype, device=G.device)
+    _need(out, "out", out_dtype)
+    _check_out(out, (vocab, d))
+    if workspace is None:
+        workspace = torch.empty(sn_embed_bwd_workspace(T, vocab, d), dtype=torch.uint8,
+                                device=G.device)
+    _need(workspace, "workspace")
+    _check(_lib.sn_embed_bwd(_error_basis(basis), _dtype(G), _ptr(G), ldg, T, d, _ptr(ids), scale,
+                             _dtype(out), _ptr(out), vocab, bool(accumulate), _ptr(workspace),
+                             workspace.numel() * workspace.element_size(), _stream(stream)),
+           "sn_embed_bwd")
+    return out
+
+
+def _norm_inputs(X, w, R, H):
+    """Row stride of X and the tensor that h is stored in (X itself without a residual)."""
+    ldx = _rows(X, "X")
+    _need(w, "w")
+    if w.shape != (X.shape[1],):
+        raise ValueError("w must have shape [d]")
+    if R is not None:
+        _need(R, "R", X.dtype)
+        _check_out(R, X.shape)
+        if H is None:
+            H = torch.empty_like(R)
+    if H is not None:
+        _need(H, "H", X.dtype)
+        _check_out(H, X.shape)
+    return ldx, H
+
+
+def sn_rmsnorm_fwd(X, w, eps, R=None, H=None, out=None, stream=None):
+    """h = X + R, Y = h / sqrt(mean(h^2) + eps) * w; returns (Y, h), h = X without a residual.
+    H may be R (the residual stream updated in place).  X may be a row-strided view."""
+    ldx, H = _norm_inputs(X, w, R, H)
+    T, d = X.shape
+    if out is None:
+        out = torch.empty(T, d, dtype=X.dtype, device=X.device)
+    _need(out, "out", X.dtype)
+    _check_out(out, (T, d))
+    _check(_lib.sn_rmsnorm_fwd(_dtype(X), _ptr(X), ldx, _ptr(R), _ptr(H), _dtype(w), _ptr(w), T, d,
+                               eps, _ptr(out), _stream(stream)), "sn_rmsnorm_fwd")
+    return out, X if H is None else H
+
+
+def sn_rmsnorm_fwd_quant(X, w, eps, fmt, R=None, H=None, group=0, codes=None, scale=None,
+                         stream=None):
+    """The norm's output as 8-bit codes (uint8 [T, d]; fmt "int8" or "e4m3") and fp32 scales, one
+    a row or one for every `group` (32, 64, 128) columns; returns (codes, scale, h)."""
+    ldx, H = _norm_inputs(X, w, R, H)
+    T, d = X.shape
+    shape = (T, -(-d // group)) if group else (T,)
+    if codes is None:
+        codes = torch.empty(T, d, dtype=torch.uint8, device=X.device)
+    if scale is None:
+        scale = torch.empty(shape, dtype=torch.float32, device=X.device)
+    _need(codes, "codes", torch.uint8)
+    _need(scale, "scale", torch.float32)
+    if codes.shape != (T, d) or scale.shape != shape:
+        raise ValueError("codes must be [T, d] and scale %s" % (shape,))
+    _check(_lib.sn_rmsnorm_fwd_quant(_dtype(X), _ptr(X), ldx, _ptr(R), _ptr(H), _dtype(w), _ptr(w),
+                                     T, d, eps, QUANT_FORMATS[fmt], group, _ptr(codes),
+                                     _ptr(scale), _stream(stream)), "sn_rmsnorm_fwd_quant")
+    return codes, scale, X if H is None else H
+
+
+def sn_rmsnorm_bwd_workspace(T, d):
+    n = _SZ()
+    _check(_lib.sn_rmsnorm_bwd_workspace(T, d, ctypes.byref(n)), "sn_rmsnorm_bwd_workspace")
+    return n.value
+
+
+def sn_rmsnorm_bwd(dY, H, w, eps, dH=None, out=None, dw=None, accumulate=False, workspace=None,
+                   stream=None):
+    """(dX, dw) from the forward's h: dX is the gradient of X and of R, dH the gradient that
+    reaches h along the residual stream; dw fp32 [d], added to with accumulate=True."""
+    ldy = _rows(dY, "dY")
+    T, d = dY.shape
+    _need(H, "H", dY.dtype)
+    _check_out(H, (T, d))
+    _need(w, "w")
+    if w.shape != (d,):
+        raise ValueError("w must have shape [d]")
+    if dH is not None:
+        _need(dH, "dH", dY.dtype)
+        _check_out(dH, (T, d))
+    if out is None:
+        out = torch.empty(T, d, dtype=dY.dtype, device=dY.device)
+    _need(out, "out", dY.dtype)
+    _check_out(out, (T, d))
+    if dw is None:
+        if accumulate:
+            raise ValueError("accumulate=True needs dw")
+        dw = torch.empty(d, dtype=torch.float32, device=dY.device)
+    _need(dw, "dw", torch.float32)
+    _check_out(dw, (d,))
+    if workspace is None:
+        workspace = torch.empty(max(16, sn_rmsnorm_bwd_workspace(T, d)), dtype=torch.uint8,
+                                device=dY.device)
+    _need(workspace, "workspace")
+    _check(_lib.sn_rmsnorm_bwd(_dtype(dY), _ptr(dY), ldy, _ptr(H), _ptr(dH), _dtype(w), _ptr(w), T,
+                               d, eps, _ptr(out), _ptr(dw), bool(accumulate), _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream(stream)),
+           "sn_rmsnorm_bwd")
+    return out, dw
+
+
+def sn_logprob_fwd(logits, target=None, scale=1.0, top=0, entropy=True, basis=None, stream=None):
+    """(logp, lse, entropy, top_ids, top_logp) of softmax(scale * logits): logp and entropy fp32
+    [T], the `top` alternatives [T, top] (ids int32), and lse fp32 [T, 2], the log-sum-exp as the
+    largest logit m and ln sum exp(scale * (logits - m)).  logp is None without targets, entropy
+    with entropy=False, the last two with top=0.  A negative target is none.  logits may be a
+    row-strided view."""
+    ld = _rows(logits, "logits")
+    T, V = logits.shape
+    dev = logits.device
+    lse = torch.empty(T, 2, dtype=torch.float32, device=dev)
+    logp = H = ids = alt = None
+    if target is not None:
+        _need(target, "target", torch.int32)
+        if target.shape != (T,):
+            raise ValueError("target must have shape [T]")
+        logp = torch.empty(T, dtype=torch.float32, device=dev)
+    if entropy:
+        H = torch.empty(T, dtype=torch.float32, device=dev)
+    if top:
+        ids = torch.empty(T, top, dtype=torch.int32, device=dev)
+        alt = torch.empty(T, top, dtype=torch.float32, device=dev)
+    _check(_lib.sn_logprob_fwd(_error_basis(basis), _dtype(logits), _ptr(logits), T, V, ld,
+                               _ptr(target), scale, _ptr(logp), _ptr(lse), _ptr(H), top, _ptr(ids),
+                               _ptr(alt), _stream(stream)), "sn_logprob_fwd")
+    return logp, lse, H, ids, alt
+
+
+def sn_logprob_bwd(logits, lse, target=None, dlogp=None, scale=1.0, entropy=None, dentropy=None,
+                   out=None, stream=None):
+    """The logits' gradient from dlogp (with target) and dentropy (with the forward's entropy),
+    each fp32 [T].  `out` may be logits (in place)."""
+    ld = _rows(logits, "logits")
+    T, V = logits.shape
+    _need(lse, "lse", torch.float32)
+    if lse.shape != (T, 2):
+        raise ValueError("lse must have shape [T, 2]")
+    for t, name in ((dlogp, "dlogp"), (entropy, "entropy"), (dentropy, "dentropy")):
+        if t is not None:
+            _need(t, name, torch.float32)
+            if t.shape != (T,):
+                raise ValueError("%s must have shape [T]" % name)
+    if target is not None:
+        _need(target, "target", torch.int32)
+        if target.shape != (T,):
+            raise ValueError("target must have shape [T]")
+    if out is None:
+        out = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
+    ldd = _rows(out, "out", logits.dtype)
+    _check_out(out, (T, V))
+    _check(_lib.sn_logprob_bwd(_dtype(logits), _ptr(logits), T, V, ld, _ptr(target), _ptr(lse),
+                               _ptr(dlogp), _ptr(entropy), _ptr(dentropy), scale, _ptr(out), ldd,
+                               _stream(stream)), "sn_logprob_bwd")
+    return out
+
+
+class GradList:
+    """A list of gradient tensors (bf16 or fp32, contiguous) and where their clipped values go:
+    `out`, as many tensors of the same sizes, by default the gradients themselves.  Made once;
+    holds the tensors."""
+
+    def __init__(self, grads, out=None, stream=None):
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError("out must have as many tensors as grads")
+        for g, o in zip(grads, out):
+            _need(g, "grads")
+            _need(o, "out")
+            if o.numel() != g.numel():
+                raise ValueError("out must have the gradients' sizes")
+        n = len(grads)
+        h = _P()
+        _check(_lib.sn_grads_create(n, (_P * n)(*[_ptr(g) for g in grads]),
+                                    (_ST * n)(*[_dtype(g) for g in grads]),
+                                    (_I64 * n)(*[g.numel() for g in grads]),
+                                    (_P * n)(*[_ptr(o) for o in out]),
+                                    (_ST * n)(*[_dtype(o) for o in out]), ctypes.byref(h),
+                                    _stream(stream)), "sn_grads_create")
+        self._h = h
+        self.grads, self.out = grads, out
+        self.device = grads[0].device if grads else torch.device("cuda",
+                                                                 torch.cuda.current_device())
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise RuntimeError("gradient list destroyed")
+        return self._h
+
+    def destroy(self):
+        if getattr(self, "_h", None) is not None:
+            _check(_lib.sn_grads_destroy(self._h), "sn_grads_destroy")
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def sn_grads_create(grads, out=None, stream=None):
+    return GradList(grads, out, stream)
+
+
+def sn_grads_destroy(grads):
+    grads.destroy()
+
+
+def sn_grads_sumsq(grads, out=None, accumulate=False, stream=None):
+    """The sum of squares of a GradList (device fp64 [1]); with accumulate=True added to out."""
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate=True needs out")
+        out = torch.empty(1, dtype=torch.float64, device=grads.device)
+    _need(out, "out", torch.float64)
+    if out.numel() < 1:
+        raise ValueError("out must have an element")
+    _check(_lib.sn_grads_sumsq(grads.handle, _ptr(out), bool(accumulate), _stream(stream)),
+           "sn_grads_sumsq")
+    return out
+
+
+def sn_grads_clip(grads, sumsq, max_norm, norm=None, stream=None):
+    """Scale a GradList by max_norm / max(norm, max_norm), norm = sqrt(sumsq); returns the norm
+    (device fp32 [1])."""
+    _need(sumsq, "sumsq", torch.float64)
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=grads.device)
+    _need(norm, "norm", torch.float32)
+    if sumsq.numel() < 1 or norm.numel() < 1:
+        raise ValueError("sumsq and norm must have an element")
+    _check(_lib.sn_grads_clip(grads.handle, _ptr(sumsq), max_norm, _ptr(norm), _stream(stream)),
+           "sn_grads_clip")
+    return norm
 
 
 def sn_decompress_fwd(basis, C, ids, tok_emb, seq_len, pos_emb=None, pos=None, out=None,
