@@ -83,25 +83,28 @@ constexpr uint32_t kLowestKey = 0x007fffffu;       // of -infinity
 // The larger logit first, then the lower token
 __device__ __forceinline__ uint64_t rank_key(uint32_t key, int v) { return (uint64_t)key << 32 | (0xffffffffu - (uint32_t)v); }
 
-// A part of a row's softmax sums: the largest logit m, and the sums of e and e * t over
-// e = 2^t, t = x c - base(m), c = scale log2(e).  One fma makes t; the base is m c rounded, which
-// every part and the result agree on.  Where m c overflows (a row masked with the type's lowest
-// value) t is (x - m) c instead.
+// A part of a row's softmax sums: the largest logit m, and the sums of e and e * t over e = 2^t,
+// t = x c - origin(m), c = scale log2(e).  The origin is m c rounded to fp32 (one fma makes t;
+// all that is computed from the sums knows the rounding) as long as that is small; past 2^20,
+// where its rounding would be felt, or where m c overflows (a row masked with the type's lowest
+// value), it is m c itself and t = (x - m) c.
 struct Sums {
     float m, s, a;
 };
 
 // 0 for a part that has no logit above -infinity: its sums are 0
 __device__ __forceinline__ float base_of(float m, float c) { return m == -INFINITY ? 0.f : __fmul_rn(m, c); }
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+__device__ __forceinline__ bool rounded(float base) { return fabsf(base) < 0x1p20f; }
 
-// What t loses when the maximum rises from m0 to m1
+// The change of t where the maximum rises from m0 to m1
 __device__ __forceinline__ float shift(float m0, float m1, float c)
 {
     if (m0 == -INFINITY)
         return 0.f;
     const float b0 = base_of(m0, c), b1 = base_of(m1, c);
-    return finite(b0) && finite(b1) ? b0 - b1 : (m0 - m1) * c;
+    if (rounded(b0))
+        return rounded(b1) ? b0 - b1 : -fmaf(m1, c, -b0);
+    return rounded(b1) ? fmaf(m0, c, -b1) : (m0 - m1) * c;
 }
 
 __device__ __forceinline__ void join(Sums &x, const Sums &y, float c)
@@ -114,13 +117,34 @@ __device__ __forceinline__ void join(Sums &x, const Sums &y, float c)
     x.m = m;
 }
 
+// The sums of a warp's lanes, or of the block's warps, in every lane: the largest m first, so
+// that each lane is rescaled once
+template <int LANES>
+__device__ __forceinline__ void join_lanes(Sums &p, float c)
+{
+    float m = p.m;
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1)
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float d = shift(p.m, m, c), f = ex2(d);
+    p.a = f * fmaf(p.s, fmaxf(d, kFloor), p.a);
+    p.s *= f;
+    p.m = m;
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+        p.s += __shfl_xor_sync(0xffffffffu, p.s, o);
+        p.a += __shfl_xor_sync(0xffffffffu, p.a, o);
+    }
+}
+
 template <int THREADS>
 struct Shared {
     Sums sums[THREADS / 32];
     Sums block;                        // this block's sums, read by the cluster
     uint32_t lane_max[THREADS];
+    uint16_t hot[THREADS];             // threads whose elements reach the bound
     uint32_t bound;
-    int n_cand;
+    int n_hot, n_cand, nan;            // nan: a NaN among the elements
     uint64_t cand[kCand];
     uint64_t best[kMaxTop];            // this block's alternatives in order, read by the cluster
     uint64_t merged[kMaxCluster * kMaxTop];
@@ -157,25 +181,55 @@ __device__ __forceinline__ void each(const RowView<T> &row, int i0, int i1, bool
         }
 }
 
-// sh.cand = this block's elements whose key is at least `from`; how many there are (the list
-// holds the first kCand of them)
+// sh.cand = this block's elements whose key is at least `from`, a key not below the bound; how
+// many there are (the list holds the first kCand of them).  They lie in the hot threads' pieces
+// and among the loose elements; the block's threads read the pieces of all hot threads at once.
 template <typename T, int THREADS>
 __device__ __forceinline__ int collect(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i1, bool ends,
-                                       uint32_t from, uint32_t mine)
+                                       uint32_t from)
 {
-    __syncthreads();
-    if (threadIdx.x == 0)
-        sh.n_cand = 0;
-    __syncthreads();
-    if (mine >= from)
-        each<T, THREADS>(row, i0, i1, ends, [&](float x, int v) {
-            const uint32_t k = key_of(x);
-            if (k >= from) {
-                const int at = atomicAdd(&sh.n_cand, 1);
-                if (at < kCand)
-                    sh.cand[at] = rank_key(k, v);
-            }
-        });
+    constexpr int N = Vec<T>::N;
+    const int per = (i1 - i0 + THREADS - 1) / THREADS;          // pieces of a thread, at most
+    const int log2 = per > 1 ? 32 - __clz(per - 1) : 0;
+    const bool nan = sh.nan;
+    const float least = value_of(from);
+    auto put = [&](float x, int v) {
+        const int at = atomicAdd(&sh.n_cand, 1);
+        if (at < kCand)
+            sh.cand[at] = rank_key(key_of(x), v);
+    };
+    for (int x = threadIdx.x; x < sh.n_hot << log2; x += THREADS) {
+        const int i = i0 + sh.hot[x >> log2] + (x & ((1 << log2) - 1)) * THREADS;
+        if (i >= i1)
+            continue;
+        float f[N];
+        Vec<T>::unpack(row.piece(i), f);
+        uint32_t hits = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            hits |= (f[k] >= least ? 1u : 0u) << k;
+        if (nan) {
+            hits = 0;
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                hits |= (key_of(f[k]) >= from ? 1u : 0u) << k;
+        }
+        while (hits) {
+            const int k = __ffs(hits) - 1;
+            float y = f[0];
+#pragma unroll
+            for (int q = 1; q < N; ++q)
+                y = k == q ? f[q] : y;
+            put(y, row.head + i * N + k);
+            hits &= hits - 1;
+        }
+    }
+    if (ends && (int)threadIdx.x < row.loose()) {
+        const int v = row.loose_at(threadIdx.x);
+        const float x = Vec<T>::one(row.p[v]);
+        if (key_of(x) >= from)
+            put(x, v);
+    }
     __syncthreads();
     return sh.n_cand;
 }
@@ -211,43 +265,69 @@ __device__ void lowest_equal(Shared<THREADS> &sh, const RowView<T> &row, int i0,
     }
 }
 
-// The block's `top` best elements into sh.best, in order.  `mine`: the largest key that this
-// thread saw (0: no element).
+// The block's `top` best elements into sh.best, in order.  sh.lane_max: the largest key that
+// each thread saw (0: no element).
 template <typename T, int THREADS>
 __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i1, bool ends, int top,
                        uint32_t mine, int elements)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    sh.lane_max[threadIdx.x] = mine;
-    __syncthreads();
     if (warp == 0) {
-        // the top-th largest of the threads' maxima, bit by bit
-        uint32_t k[THREADS / 32], b = 0;
+        // the top-th largest of the threads' maxima, bit by bit from the first in which they
+        // differ, until exactly `top` reach it
+        uint32_t k[THREADS / 32], hi = 0, lo = 0xffffffffu;
 #pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i)
+        for (int i = 0; i < THREADS / 32; ++i) {
             k[i] = sh.lane_max[i * 32 + lane];
-        for (int bit = 31; bit >= 0; --bit) {
+            hi = max(hi, k[i]);
+            lo = min(lo, k[i]);
+        }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        lo = __reduce_min_sync(0xffffffffu, lo);
+        const int first = 31 - __clz(hi ^ lo);                // -1: all the same
+        uint32_t b = first < 0 ? hi : hi & ~((2u << first) - 1u);
+        for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {     // bf16 keys end there
             const uint32_t trial = b | 1u << bit;
             int n = 0;
 #pragma unroll
             for (int i = 0; i < THREADS / 32; ++i)
                 n += k[i] >= trial;
-            if (__reduce_add_sync(0xffffffffu, n) >= top)
+            n = __reduce_add_sync(0xffffffffu, n);
+            if (n >= top)
                 b = trial;
+            if (n == top)
+                break;
         }
-        if (lane == 0)
-            sh.bound = max(b, kLowestKey);
+        b = max(b, kLowestKey);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < THREADS / 32; ++i) {
+            const uint32_t hit = __ballot_sync(0xffffffffu, k[i] >= b);
+            if (k[i] >= b)
+                sh.hot[n + __popc(hit & ((1u << lane) - 1u))] = (uint16_t)(i * 32 + lane);
+            n += __popc(hit);
+        }
+        if (lane == 0) {
+            sh.bound = b;
+            sh.n_hot = n;
+            sh.n_cand = 0;
+            sh.nan = hi == 0xffffffffu;
+        }
     }
     __syncthreads();
     const uint32_t bound = sh.bound;
     const int want = min(top, elements);
-    int n = collect<T, THREADS>(sh, row, i0, i1, ends, bound, mine);
+    int n = collect<T, THREADS>(sh, row, i0, i1, ends, bound);
     bool ties = false;
     if (n > kCand) {
         // many equal elements at the bound (a masked row's are -infinity): those above it
         // alone, then the lowest tokens at it
         ties = true;
-        n = bound == 0xffffffffu ? 0 : collect<T, THREADS>(sh, row, i0, i1, ends, bound + 1, mine);
+        __syncthreads();
+        if (threadIdx.x == 0)
+            sh.n_cand = 0;
+        __syncthreads();
+        n = bound == 0xffffffffu ? 0 : collect<T, THREADS>(sh, row, i0, i1, ends, bound + 1);
     }
     if (n <= kCand) {
         for (int i = threadIdx.x; i < n; i += THREADS) {
@@ -304,87 +384,261 @@ __device__ __forceinline__ T ld_remote(const T *p, uint32_t rank)
     return u.v;
 }
 
-template <typename T, int THREADS, bool TOP>
-__global__ void __launch_bounds__(THREADS) k_logprob(const LogpArgs a, int cluster)
+// Asks for the first bytes of a later row's pieces, so that DRAM stays busy while rows' sums meet
+constexpr int kAhead = 32 * 1024;
+__device__ __forceinline__ void prefetch_l2(const void *p, int bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
+// ---- one pass over a thread's pieces ---------------------------------------------------------
+
+// Elements at or below -10^20 count as -10^20 on the short path, where e = 0 whatever they
+// are and t has to stay finite (0 * t = 0); it is taken while |m| < 10^19 and c > 10^-17, so
+// that t is far below the smallest exponent.
+constexpr float kLow = -1e20f;
+constexpr uint32_t kLowPair = 0xE0AEE0AEu;       // bf16, twice
+
+__device__ __forceinline__ bool near(float m, float c)
+{
+    return fabsf(m) < 1e19f && c > 1e-17f && rounded(m * c);
+}
+
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_pair_nan(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Two words of a piece (bf16: 4 elements, fp32: 2): their maximum, and their pairs with the
+// elements below kLow raised to it
+template <typename T>
+struct Words;
+template <>
+struct Words<__nv_bfloat16> {
+    static constexpr uint32_t kNone = 0xFF80FF80u;       // -infinity
+    static constexpr int kPairs = 4;                     // of a piece
+    template <int U>
+    static __device__ __forceinline__ float max_of(const uint4 (&v)[U])
+    {
+        uint32_t m = max_pair(max_pair(v[0].x, v[0].y), max_pair(v[0].z, v[0].w));
+#pragma unroll
+        for (int u = 1; u < U; ++u)
+            m = max_pair(m, max_pair(max_pair(v[u].x, v[u].y), max_pair(v[u].z, v[u].w)));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    }
+    static __device__ __forceinline__ void pairs(uint4 v, float2 (&f)[4])
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = max_pair_nan(w[i], kLowPair);
+            f[i] = make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xFFFF0000u));
+        }
+    }
+};
+template <>
+struct Words<float> {
+    static constexpr uint32_t kNone = 0xFF800000u;
+    static constexpr int kPairs = 2;
+    template <int U>
+    static __device__ __forceinline__ float max_of(const uint4 (&v)[U])
+    {
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(v[u].x), __uint_as_float(v[u].y)),
+                               fmaxf(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
+        return m;
+    }
+    static __device__ __forceinline__ void pairs(uint4 v, float2 (&f)[2])
+    {
+        f[0] = make_float2(max_nan(__uint_as_float(v.x), kLow), max_nan(__uint_as_float(v.y), kLow));
+        f[1] = make_float2(max_nan(__uint_as_float(v.z), kLow), max_nan(__uint_as_float(v.w), kLow));
+    }
+};
+
+// A thread's sums while it walks, over the even and the odd elements.  Their origin is that of
+// an earlier maximum m until the largest logit `top` has risen kRise powers of two above it:
+// with 32 lanes a warp, some lane's maximum rises in almost every step.
+constexpr float kRise = 8.f;
+
+struct Walk {
+    float top, m, b;
+    bool short_;                     // near(m, c)
+    float2 s, a;
+
+    __device__ __forceinline__ Walk() : top(-INFINITY), m(-INFINITY), b(0.f), short_(false), s(both(0.f)), a(both(0.f)) {}
+
+    template <bool ENT>
+    __device__ __forceinline__ void raise(float to, float c)
+    {
+        const float d = shift(m, to, c), r = ex2(d);
+        if (ENT)
+            a = mul2(both(r), fma2(s, both(fmaxf(d, kFloor)), a));
+        s = mul2(both(r), s);
+        m = to;
+        b = base_of(to, c);
+        short_ = near(to, c);
+    }
+    // any element, any m: a product and a difference more
+    template <bool ENT>
+    __device__ __forceinline__ void one(float x, float c)
+    {
+        top = fmaxf(top, x);
+        if (top > m)
+            raise<ENT>(top, c);
+        const float t = rounded(b) ? fmaf(x, c, -b) : (x - m) * c;
+        const float e = ex2(t);
+        s.x += e;
+        if (ENT)
+            a.x = fmaf(e, fmaxf(t, kFloor), a.x);
+    }
+    template <typename T, bool ENT, int U>
+    __device__ __forceinline__ void pieces(const uint4 (&v)[U], float c)
+    {
+        top = fmaxf(top, Words<T>::max_of(v));
+        if (top > m && !(fmaf(top, c, -b) < kRise && short_))
+            raise<ENT>(top, c);
+        if (short_) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float2 f[Words<T>::kPairs];
+                Words<T>::pairs(v[u], f);
+#pragma unroll
+                for (int k = 0; k < Words<T>::kPairs; ++k) {
+                    const float2 t = fma2(f[k], both(c), both(-b));
+                    const float2 e = make_float2(ex2(t.x), ex2(t.y));
+                    s = add2(s, e);
+                    if (ENT)
+                        a = fma2(e, t, a);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < U; ++u) {
+                float f[Vec<T>::N];
+                uint4 w = v[0];
+#pragma unroll
+                for (int k = 1; k < U; ++k)
+                    w = u == k ? v[k] : w;
+                Vec<T>::unpack(w, f);
+#pragma unroll
+                for (int k = 0; k < Vec<T>::N; ++k)
+                    one<ENT>(f[k], c);
+            }
+        }
+    }
+    // the sums from the largest logit on
+    template <bool ENT>
+    __device__ __forceinline__ Sums sums(float c)
+    {
+        if (top > m)
+            raise<ENT>(top, c);
+        return {m, s.x + s.y, a.x + a.y};
+    }
+};
+
+constexpr int kPieces = 4;
+template <typename T, int THREADS>
+struct RowPart : RowView<T> {
+    int i0, i1;
+    __device__ __forceinline__ RowPart(const LogpArgs &a, int64_t t, int rank, int cluster)
+        : RowView<T>((const T *)a.x + t * a.ld, a.V)
+    {
+        const int per = cluster == 1 ? this->nv : (this->nv + cluster - 1) / cluster;
+        i0 = min(this->nv, rank * per);
+        i1 = min(this->nv, i0 + per);
+    }
+    // a thread's step from piece i on; none where the part ends
+    __device__ __forceinline__ void load(int i, uint4 (&v)[kPieces]) const
+    {
+        if (i + (kPieces - 1) * THREADS < i1) {
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u)
+                v[u] = this->piece(i + u * THREADS);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u)
+                v[u] = i + u * THREADS < i1 ? this->piece(i + u * THREADS)
+                                            : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone,
+                                                         Words<T>::kNone);
+        }
+    }
+};
+
+template <typename T, int THREADS, bool TOP, bool ENT>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob(const LogpArgs a, int cluster_log2, int ahead)
 {
     griddep_start();
-    constexpr int N = Vec<T>::N, U = 4;
+    constexpr int N = Vec<T>::N, U = kPieces, W = THREADS / 32;
     __shared__ Shared<THREADS> sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rank = cluster > 1 ? (int)(blockIdx.x % cluster) : 0;
+    const int cluster = 1 << cluster_log2;
+    const int rank = (int)(blockIdx.x & (cluster - 1));
     const float c = a.scale * kLog2e;
-    for (int64_t t = blockIdx.x / cluster; t < a.T; t += gridDim.x / cluster) {
-        const RowView<T> row((const T *)a.x + t * a.ld, a.V);
-        const int per = (row.nv + cluster - 1) / cluster;
-        const int i0 = min(row.nv, rank * per), i1 = min(row.nv, i0 + per);
-        const bool ends = rank == 0;
-        Sums p{-INFINITY, 0.f, 0.f};
-        bool nan = false, saw = i0 + (int)threadIdx.x < i1;
-        auto add = [&](const float *f, int n) {
-            float m = f[0];
-            for (int k = 1; k < n; ++k)
-                m = fmaxf(m, f[k]);
-            if (m > p.m) {
-                const float d = shift(p.m, m, c);
-                const float r = ex2(d);
-                p.a = r * fmaf(p.s, fmaxf(d, kFloor), p.a);
-                p.s *= r;
-                p.m = m;
-            }
-            const float b = base_of(p.m, c);
-            const bool far = !finite(b);
-            for (int k = 0; k < n; ++k) {
-                float t = fmaf(f[k], c, -b);
-                if (far)
-                    t = (f[k] - p.m) * c;
-                const float e = ex2(t);
-                p.s += e;
-                p.a = fmaf(e, fmaxf(t, kFloor), p.a);
-                nan |= f[k] != f[k];
-            }
-        };
-        for (int i = i0 + threadIdx.x; i < i1; i += U * THREADS) {
-            uint4 v[U];
-            float f[U * N];
+    const bool ends = rank == 0;
+    const int64_t stride = gridDim.x >> cluster_log2;
+    for (int64_t t = blockIdx.x >> cluster_log2; t < a.T; t += stride) {
+        const RowPart<T, THREADS> row(a, t, rank, cluster);
+        const bool has_loose = ends && (int)threadIdx.x < row.loose();
+        const float loose = has_loose ? Vec<T>::one(row.p[row.loose_at(threadIdx.x)]) : 0.f;
+        Walk walk;
+        int i = row.i0 + threadIdx.x;
+        uint4 v[U], next[U];
+        row.load(i, v);
+        while (i + U * THREADS < row.i1) {
+            i += U * THREADS;
+            row.load(i, next);
+            walk.pieces<T, ENT>(v, c);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (i + u * THREADS < i1)
-                    v[u] = row.piece(i + u * THREADS);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u * THREADS < i1) {
-                    Vec<T>::unpack(v[u], *(float(*)[N])(f + u * N));
-                } else {
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        f[u * N + k] = -INFINITY;
-                }
-            add(f, U * N);
+                v[u] = next[u];
         }
-        if (ends && (int)threadIdx.x < row.loose()) {
-            const float f = Vec<T>::one(row.p[row.loose_at(threadIdx.x)]);
-            add(&f, 1);
+        if (i < row.i1)
+            walk.pieces<T, ENT>(v, c);
+        if (threadIdx.x == 0 && cluster == 1 && t + ahead < a.T) {
+            const RowView<T> later((const T *)a.x + (t + ahead) * a.ld, a.V);
+            const int bytes = min(later.nv * 16, kAhead);
+            if (bytes > 0)
+                prefetch_l2(later.p + later.head, bytes);
+        }
+        bool saw = row.i0 + (int)threadIdx.x < row.i1;
+        if (has_loose) {
+            walk.one<ENT>(loose, c);
             saw = true;
         }
-        const uint32_t mine = nan ? 0xffffffffu : saw ? key_of(p.m) : 0u;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const Sums q{__shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
-                         __shfl_xor_sync(0xffffffffu, p.a, o)};
-            join(p, q, c);
+        Sums p = walk.sums<ENT>(c);
+        uint32_t mine = 0;
+        if (TOP) {
+            mine = saw ? key_of(p.m) : 0u;
+            if (p.s != p.s) {                     // a NaN among them, or an infinity
+                bool nan = false;
+                each<T, THREADS>(row, row.i0, row.i1, ends, [&](float x, int) { nan |= x != x; });
+                mine = nan ? 0xffffffffu : mine;
+            }
         }
+        join_lanes<32>(p, c);
         __syncthreads();
         if (lane == 0)
             sh.sums[warp] = p;
+        if (TOP)
+            sh.lane_max[threadIdx.x] = mine;
         __syncthreads();
-        p = sh.sums[0];
-        for (int w = 1; w < THREADS / 32; ++w)
-            join(p, sh.sums[w], c);
+        p = sh.sums[lane % W];
+        join_lanes<W>(p, c);
         if (threadIdx.x == 0)
             sh.block = p;
         if (TOP)
-            select<T, THREADS>(sh, row, i0, i1, ends, a.top, mine,
-                               (i1 - i0) * N + (ends ? row.loose() : 0));
+            select<T, THREADS>(sh, row, row.i0, row.i1, ends, a.top, mine,
+                               (row.i1 - row.i0) * N + (ends ? row.loose() : 0));
         if (cluster > 1) {
             cluster_sync();
             if (rank == 0) {
@@ -413,11 +667,11 @@ __global__ void __launch_bounds__(THREADS) k_logprob(const LogpArgs a, int clust
             const bool empty = p.m == -INFINITY && p.s == 0.f;
             const float b = base_of(p.m, c), l2 = empty ? -INFINITY : log2f(p.s);
             // ln S for the sums of 2^((x - m) c): the base's rounding taken out again
-            const float ln = empty ? -INFINITY : kLn2 * (finite(b) ? l2 - fmaf(p.m, c, -b) : l2);
+            const float ln = empty ? -INFINITY : kLn2 * (rounded(b) ? l2 - fmaf(p.m, c, -b) : l2);
             if (threadIdx.x == 0) {
                 if (a.lse)
                     *(float2 *)(a.lse + 2 * t) = make_float2(p.m, ln);
-                if (a.entropy)
+                if (ENT)
                     a.entropy[t] = empty ? 0.f : kLn2 * (l2 - p.a / p.s);
                 if (a.logp) {
                     const int v = a.target[t];
@@ -453,7 +707,6 @@ struct LogpBwdArgs {
     const int32_t *target;
     const float *lse, *entropy, *dlogp, *dentropy;   // target with dlogp, entropy with dentropy
     float scale;
-    int segments;                                     // blocks of a row
 };
 
 constexpr int kBwdThreads = 256, kBwdPieces = 4;
@@ -462,17 +715,12 @@ constexpr int kBwdThreads = 256, kBwdPieces = 4;
 struct RowCoef {
     float m, c, l2, a, b, k;       // log2 p = (x - m) c - l2;  b for log2 p
     int target;
-    bool empty;
-    __device__ __forceinline__ float at(float x, int v) const
+    bool near_, empty;
+    // without the target's term
+    __device__ __forceinline__ float at(float x) const
     {
         const float t = fmaf(x - m, c, -l2);
-        const float p = ex2(t);
-        float g = p * fmaf(-b, fmaxf(t, kFloor), k);
-        if (t != t)
-            g = t;
-        if (v == target)
-            g += a;
-        return empty ? 0.f : g;
+        return empty ? 0.f : ex2(t) * fmaf(-b, t < kFloor ? kFloor : t, k);
     }
 };
 
@@ -481,9 +729,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a
 {
     griddep_start();
     constexpr int N = Vec<T>::N, U = kBwdPieces;
-    for (int64_t blk = blockIdx.x; blk < a.T * a.segments; blk += gridDim.x) {
-        const int64_t t = blk / a.segments;
-        const int seg = (int)(blk - t * a.segments);
+    const int seg = blockIdx.x;
+    for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
         const RowView<T> row((const T *)a.x + t * a.ld, a.V);
         T *out = (T *)a.dx + t * a.ldd;
         RowCoef q;
@@ -493,7 +740,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a
         q.l2 = lse.y * kLog2e;
         q.empty = lse.y == -INFINITY;
         q.target = a.dlogp ? a.target[t] : -1;
-        q.a = a.dlogp && q.target >= 0 && q.target < a.V ? a.dlogp[t] * a.scale : 0.f;
+        q.near_ = !q.empty && near(q.m, q.c);
+        q.a = !q.empty && a.dlogp && q.target >= 0 && q.target < a.V ? a.dlogp[t] * a.scale : 0.f;
         const float b = a.dentropy ? a.dentropy[t] * a.scale : 0.f;
         q.k = -q.a - (a.dentropy ? b * a.entropy[t] : 0.f);
         q.b = b * kLn2;
@@ -511,10 +759,26 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a
                 continue;
             const int c0 = row.head + i * N;
             float f[N];
-            Vec<T>::unpack(v[u], f);
+            if (q.near_) {
+                float2 x[N / 2];
+                Words<T>::pairs(v[u], x);
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                f[k] = q.at(f[k], c0 + k);
+                for (int k = 0; k < N / 2; ++k) {
+                    const float2 z = fma2(add2(x[k], both(-q.m)), both(q.c), both(-q.l2));
+                    const float2 g = mul2(make_float2(ex2(z.x), ex2(z.y)), fma2(both(-q.b), z, both(q.k)));
+                    f[2 * k] = g.x;
+                    f[2 * k + 1] = g.y;
+                }
+            } else {
+                Vec<T>::unpack(v[u], f);
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    f[k] = q.at(f[k]);
+            }
+            if ((uint32_t)(q.target - c0) < (uint32_t)N)
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    f[k] += q.target - c0 == k ? q.a : 0.f;
             if (wide) {
                 *(uint4 *)(out + c0) = Vec<T>::pack(f);
             } else {
@@ -525,24 +789,32 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a
         }
         if (seg == 0 && (int)threadIdx.x < row.loose()) {
             const int c = row.loose_at(threadIdx.x);
-            out[c] = Vec<T>::round(q.at(Vec<T>::one(row.p[c]), c));
+            out[c] = Vec<T>::round(q.at(Vec<T>::one(row.p[c])) + (c == q.target ? q.a : 0.f));
         }
     }
+}
+
+template <typename T, int THREADS, bool TOP, bool ENT>
+cudaError_t fwd_launch(const LogpArgs &a, int cluster, cudaStream_t s)
+{
+    const int64_t rows = std::min<int64_t>(a.T, ((int64_t)1 << 30) / cluster);
+    int log2 = 0;
+    while (1 << log2 < cluster)
+        ++log2;
+    count_launch();
+    const cudaError_t e = launch_clusters(k_logprob<T, THREADS, TOP, ENT>, cluster, dim3((unsigned)(rows * cluster)),
+                                          dim3(THREADS), 0, s, a, log2, device_sms() * (1024 / THREADS));
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <typename T, int THREADS>
 cudaError_t fwd(const LogpArgs &a, int cluster, cudaStream_t s)
 {
-    const int64_t rows = std::min<int64_t>(a.T, ((int64_t)1 << 30) / cluster);
-    count_launch();
-    cudaError_t e;
-    if (a.top > 0)
-        e = launch_clusters(k_logprob<T, THREADS, true>, cluster, dim3((unsigned)(rows * cluster)), dim3(THREADS),
-                            0, s, a, cluster);
-    else
-        e = launch_clusters(k_logprob<T, THREADS, false>, cluster, dim3((unsigned)(rows * cluster)), dim3(THREADS),
-                            0, s, a, cluster);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    if (a.entropy)
+        return a.top > 0 ? fwd_launch<T, THREADS, true, true>(a, cluster, s)
+                         : fwd_launch<T, THREADS, false, true>(a, cluster, s);
+    return a.top > 0 ? fwd_launch<T, THREADS, true, false>(a, cluster, s)
+                     : fwd_launch<T, THREADS, false, false>(a, cluster, s);
 }
 
 template <typename T>
@@ -551,11 +823,13 @@ cudaError_t fwd_type(const LogpArgs &a, cudaStream_t s)
     const int nv = a.V / Vec<T>::N;
     if (nv <= 1024)
         return fwd<T, 128>(a, 1, s);
+    const int sms = device_sms();
+    if (a.T >= 2 * sms)
+        return fwd<T, 256>(a, 1, s);
     // few rows: blocks of a cluster share one, as long as each has a piece a thread; on a
     // part of the GPU's SMs clusters may have no place
     int cluster = 1;
-    const int sms = device_sms();
-    while (cluster < kMaxCluster && a.T * cluster * 2 <= sms && nv >= cluster * 2 * 512)
+    while (cluster < kMaxCluster && a.T * cluster <= sms && nv >= cluster * 2 * 512)
         cluster *= 2;
     if (cluster > 1 && stream_sms(s) < sms)
         cluster = 1;
@@ -563,13 +837,13 @@ cudaError_t fwd_type(const LogpArgs &a, cudaStream_t s)
 }
 
 template <typename T>
-cudaError_t bwd_type(LogpBwdArgs a, cudaStream_t s)
+cudaError_t bwd_type(const LogpBwdArgs &a, cudaStream_t s)
 {
     constexpr int per = Vec<T>::N * kBwdPieces * kBwdThreads;
-    a.segments = (a.V + per - 1) / per;
     count_launch();
     const cudaError_t e = launch_dependent(k_logprob_bwd<T>,
-                                           dim3((unsigned)std::min<int64_t>(a.T * a.segments, (int64_t)1 << 30)),
+                                           dim3((unsigned)((a.V + per - 1) / per),
+                                                (unsigned)std::min<int64_t>(a.T, 65535)),
                                            dim3(kBwdThreads), 0, s, a);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -588,7 +862,7 @@ cudaError_t logprob_bwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld
                         const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
                         float scale, void *dx, int64_t ldd, cudaStream_t s)
 {
-    const LogpBwdArgs a{x, dx, T, ld, ldd, V, target, lse, entropy, dlogp, dentropy, scale, 1};
+    const LogpBwdArgs a{x, dx, T, ld, ldd, V, target, lse, entropy, dlogp, dentropy, scale};
     return dt == SN_BF16 ? bwd_type<__nv_bfloat16>(a, s) : bwd_type<float>(a, s);
 }
 

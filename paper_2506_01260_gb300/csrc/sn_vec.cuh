@@ -91,6 +91,13 @@ __device__ __forceinline__ V warp_sum(V v)
     return v;
 }
 
+// ---- fp32 pairs: one instruction for two (the intrinsics on float2 compile to one; 64-bit
+// integers through inline PTX took 2.5, moves among them) ------------------------------------
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // max that keeps a NaN
 __device__ __forceinline__ float max_nan(float a, float b)
 {

@@ -99,6 +99,39 @@ def test_masks(sn, dt, T, V):
 
 
 @pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("size", [1e-30, 1e6, 2e7, 1e19, 1e25, 3e37])
+@pytest.mark.parametrize("scale", [1.0, 1e-18, 30.0])
+def test_logits_of_any_size(sn, dt, size, scale):
+    """Differences of logits that the type still tells apart, however large or small they are.  The
+    exponent's rounding counts here: z is right to 2^-22 of itself where p matters (|z| < 40)."""
+    g = gen(11)
+    T, V = 6, 3000
+    x = (size * torch.randn(T, V, generator=g, device="cuda")).to(DT[dt])
+    x[1] = -x[1].abs() - size
+    x[2, 5:] = x[2, 4]                                       # many at the maximum
+    x[2, :5] = -x[2, 4].abs()
+    target = x.argmax(1).int()
+    logp, lse, H, ids, alt = sn.sn_logprob_fwd(x, target, scale=scale, top=4)
+    s64 = float(torch.tensor(scale, dtype=torch.float32))
+    q = torch.log_softmax(x.double() * s64, 1)
+    p = q.exp()
+    assert torch.equal(ids.long(), best(x, 4))
+    within(logp, q.gather(1, target.long()[:, None])[:, 0], S_REL)
+    at = q.gather(1, ids.long())
+    near = at > -40
+    within(alt[near], at[near], S_REL + 40 * 2.0 ** -22)
+    within(H, -torch.where(p > 0, p * q, 0.0).sum(1), 2 * S_REL * (math.log(V) + 1) + 2.0 ** -19)
+    one = torch.ones(T, device="cuda")
+    dx = sn.sn_logprob_bwd(x, lse, target, one, scale=scale, entropy=H, dentropy=one)
+    hot = torch.zeros_like(p).scatter_(1, target.long()[:, None], 1.0)
+    qf = torch.where(p > 0, q, 0.0)
+    ent = -(p * qf).sum(1, keepdim=True)
+    ref = s64 * (hot - p - p * (qf + ent))
+    within(dx, ref, s64 * (p * (2 + 2 * qf.abs() + ent + math.log(V)) * 2.0 ** -13 + hot * 2.0 ** -23 + 2.0 ** -60)
+           + ref.abs() * UNIT[DT[dt]] * 1.02)
+
+
+@pytest.mark.parametrize("dt", DT)
 @pytest.mark.parametrize("T,V", [(3, 9), (2, 5000), (2, 40000), (200, 9001)])
 def test_rows_without_a_token(sn, dt, T, V):
     g = gen(V + 1)
