@@ -386,10 +386,6 @@ __device__ __forceinline__ T ld_remote(const T *p, uint32_t rank)
 
 // Asks for the first bytes of a later row's pieces, so that DRAM stays busy while rows' sums meet
 constexpr int kAhead = 32 * 1024;
-__device__ __forceinline__ void prefetch_l2(const void *p, int bytes)
-{
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
-}
 
 // ---- one pass over a thread's pieces ---------------------------------------------------------
 
@@ -608,7 +604,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob(const LogpA
             const RowView<T> later((const T *)a.x + (t + ahead) * a.ld, a.V);
             const int bytes = min(later.nv * 16, kAhead);
             if (bytes > 0)
-                prefetch_l2(later.p + later.head, bytes);
+                prefetch_l2(later.p + later.head, (uint32_t)bytes);
         }
         bool saw = row.i0 + (int)threadIdx.x < row.i1;
         if (has_loose) {

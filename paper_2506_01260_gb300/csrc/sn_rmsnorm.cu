@@ -19,44 +19,54 @@
 namespace sn {
 namespace {
 
-// A row of d elements, in `nv` 16-byte pieces: lane l of the G that share the row has the
-// pieces l, l + G, ... (C of them).  Up to 32 lanes lie in one warp and sum by shuffles (a
-// block of 256 threads then takes several rows); more lanes are the whole block.
-template <int G>
-struct Lanes {
-    static constexpr int kThreads = G < 256 && G <= 32 ? 256 : G;
-    static constexpr int kRows = kThreads / G;
+// A row of d elements, in `nv` 16-byte pieces, is shared by G lanes: lane l has the pieces l,
+// l + G, ... (at most C).  Narrow rows are a warp's each (S = 32: a block of 256 threads takes
+// eight), wider ones a block's of G <= S threads, G a multiple of 32, so that no width leaves
+// more than a few lanes without work.
+// EXACT: G is S, and the indices are constants (codes of 16384 rows of 4096: 73 us, 80 without).
+template <int S, bool EXACT = false>
+struct Shape {
+    static constexpr int kThreads = S == 32 ? 256 : S;      // at most
+    static constexpr int kRows = S == 32 ? 8 : 1;
+    static __device__ __forceinline__ int lanes() { return S == 32 || EXACT ? S : (int)blockDim.x; }
 };
 
-// The sums of K values over the lanes of a row, in every lane; `red`: 2 * K * 32 floats
-// that calls alternate between (`turn`), so one barrier a call is enough.
-template <int G, int K, bool MAX>
+// The sums (or maxima) of K values over the lanes of a row, in every lane.  `red`: 2 * K * 32
+// floats that calls alternate between (`turn`), so one barrier a call is enough.
+template <int S, int K, bool MAX, bool EXACT = false>
 __device__ __forceinline__ void row_reduce(float (&v)[K], float *red, int &turn)
 {
 #pragma unroll
-    for (int o = (G < 32 ? G : 32) / 2; o > 0; o >>= 1)
+    for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const float x = __shfl_xor_sync(0xffffffffu, v[k], o);
             v[k] = MAX ? max_nan(v[k], x) : v[k] + x;
         }
-    if (G <= 32)
+    if (S == 32)
         return;
-    constexpr int W = G / 32;
+    const int warps = Shape<S, EXACT>::lanes() / 32;
     float *at = red + turn * (K * 32);
     turn ^= 1;
-    if (threadIdx.x % 32 == 0)
+    // (lanes 1 to 3 of the last warp fill up to a multiple of four)
+    const int slot = (int)threadIdx.x / 32 + (int)threadIdx.x % 32;
+    if (threadIdx.x % 32 == 0 || (threadIdx.x % 32 < 4 && slot >= warps && slot < 32))
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            at[k * 32 + threadIdx.x / 32] = v[k];
+            at[k * 32 + slot] = threadIdx.x % 32 == 0 ? v[k] : 0.f;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        float s = at[k * 32];
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 1; w < W; ++w)
-            s = MAX ? max_nan(s, at[k * 32 + w]) : s + at[k * 32 + w];
-        v[k] = s;
+        for (int w = 0; w < S / 32; w += 4) {
+            if (!EXACT && w >= warps)
+                break;
+            const float4 x = *(const float4 *)(at + k * 32 + w);
+            s = MAX ? make_float4(max_nan(s.x, x.x), max_nan(s.y, x.y), max_nan(s.z, x.z), max_nan(s.w, x.w))
+                    : make_float4(s.x + x.x, s.y + x.y, s.z + x.z, s.w + x.w);
+        }
+        v[k] = MAX ? max_nan(max_nan(s.x, s.y), max_nan(s.z, s.w)) : (s.x + s.y) + (s.z + s.w);
     }
 }
 
@@ -86,7 +96,8 @@ struct NormArgs {
     void *Y;
     uint8_t *codes;
     float *scale;
-    int group;              // columns that share a scale; 0: the row
+    int group_log2;         // columns that share a scale: 2^group_log2; 0: the row
+    int ahead;              // rows that are in flight on the GPU at once; 0: no prefetch
 };
 
 // The smallest magnitude that a group's scale is made for: its reciprocal stays finite.
@@ -106,30 +117,66 @@ __device__ __forceinline__ float reciprocal_of(float a)
     return a == 0.f ? 0.f : qmax_of<FMT>() / (a < kTiny ? kTiny : a);
 }
 
-// One code: int8 rounds half to even and clamps, e4m3 rounds to nearest even and saturates
+// Four codes of y * rec, the first in the lowest byte: int8 rounds half to even (adding
+// 1.5 * 2^23 leaves the rounded value in the low byte; |y * rec| <= 127 (1 + 2^-22)), e4m3
+// rounds to nearest even and saturates.  What a NaN or an infinity gives does not matter: its
+// scale is none.
 template <int FMT>
-__device__ __forceinline__ uint32_t code_of(float x)
+__device__ __forceinline__ uint32_t codes_of(float2 y0, float2 y1, float rec)
 {
-    if (FMT == SN_Q_INT8)
-        return (uint32_t)max(-127, min(127, __float2int_rn(x))) & 0xFFu;
-    return (uint32_t)__nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+    const float2 x0 = mul2(y0, both(rec)), x1 = mul2(y1, both(rec));
+    if (FMT == SN_Q_INT8) {
+        const float2 q0 = add2(x0, both(12582912.f)), q1 = add2(x1, both(12582912.f));
+        return __byte_perm(__byte_perm(__float_as_uint(q0.x), __float_as_uint(q0.y), 0x0040),
+                           __byte_perm(__float_as_uint(q1.x), __float_as_uint(q1.y), 0x0040), 0x5410);
+    }
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(x0, __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(x1, __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+}
+template <int FMT>
+__device__ __forceinline__ uint8_t code_of(float y, float rec)
+{
+    return (uint8_t)codes_of<FMT>(make_float2(y, 0.f), both(0.f), rec);
 }
 
 // ---- forward, rows in registers ------------------------------------------------------------
 
-template <typename T, int G, int C, int FMT>
-__global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm(const NormArgs a)
+// The largest magnitude of a piece, a NaN if it holds one (or infinities of both signs)
+template <int P>
+__device__ __forceinline__ float magnitude(const float2 (&f)[P])
+{
+    float m = 0.f;
+    float2 sum = both(0.f);
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        m = fmaxf(m, fmaxf(fabsf(f[k].x), fabsf(f[k].y)));
+        sum = add2(sum, f[k]);
+    }
+    const float z = sum.x + sum.y;
+    return z != z ? z : m;
+}
+
+// Threads of an SM that registers are kept low enough for.  Codes from bf16 rows want 113
+// registers at 4 pieces a lane: capped at 80 for 768 threads they spill (16384 rows of 4096: 95
+// us instead of 73).
+template <typename T, int S, int C, int FMT>
+constexpr int kResident = S > 256 ? S : C == 1 ? 1536 : C == 2 ? 1024 : FMT < 0 || sizeof(T) == 4 ? 768 : 512;
+
+template <typename T, int S, bool EXACT, int C, int FMT>
+__global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / Shape<S>::kThreads)
+    k_rmsnorm(const NormArgs a)
 {
     griddep_start();
-    constexpr int N = Vec<T>::N;
-    __shared__ float red[2 * 32];
+    constexpr int N = Vec<T>::N, P = N / 2, kRows = Shape<S>::kRows;
+    __shared__ __align__(16) float red[2 * 32];
     int turn = 0;
-    const int lane = threadIdx.x % G;
+    const int G = Shape<S, EXACT>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
     const int nv = a.d / N;
     const T *X = (const T *)a.X, *R = (const T *)a.R;
     T *H = (T *)a.H, *Y = (T *)a.Y;
-    for (int64_t t0 = (int64_t)blockIdx.x * Lanes<G>::kRows; t0 < a.T; t0 += (int64_t)gridDim.x * Lanes<G>::kRows) {
-        const int64_t t = t0 + threadIdx.x / G;
+    for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
+        const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
         const bool live = t < a.T;
         uint4 xv[C], rv[C];
 #pragma unroll
@@ -139,25 +186,31 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm(const NormArgs a
             xv[i] = in ? *((const uint4 *)(X + t * a.ldx) + j) : make_uint4(0, 0, 0, 0);
             rv[i] = in && R ? *((const uint4 *)(R + t * a.d) + j) : make_uint4(0, 0, 0, 0);
         }
-        float h[C][N], s[1] = {0.f};
+        if (FMT >= 0 && a.ahead > 0 && threadIdx.x < 2 && t0 + a.ahead + kRows <= a.T) {
+            const T *p = threadIdx.x == 0 ? X + (t0 + a.ahead) * a.ldx : R ? R + (t0 + a.ahead) * a.d : nullptr;
+            if (p)
+                prefetch_l2(p, (uint32_t)(kRows * a.d * sizeof(T)));
+        }
+        float2 h[C][P], sq = both(0.f);
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            Vec<T>::unpack(xv[i], h[i]);
+            unpack_pairs(xv[i], h[i]);
             if (R) {
-                float r[N];
-                Vec<T>::unpack(rv[i], r);
+                float2 r[P];
+                unpack_pairs(rv[i], r);
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    h[i][k] += r[k];
+                for (int k = 0; k < P; ++k)
+                    h[i][k] = add2(h[i][k], r[k]);
             }
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                s[0] = fmaf(h[i][k], h[i][k], s[0]);
+            for (int k = 0; k < P; ++k)
+                sq = fma2(h[i][k], h[i][k], sq);
             const int j = lane + G * i;
             if (H && live && j < nv)
-                *((uint4 *)(H + t * a.d) + j) = Vec<T>::pack(h[i]);
+                *((uint4 *)(H + t * a.d) + j) = pack_pairs(h[i]);
         }
-        row_reduce<G, 1, false>(s, red, turn);
+        float s[1] = {sq.x + sq.y};
+        row_reduce<S, 1, false, EXACT>(s, red, turn);
         const float rs = rsqrtf(s[0] / (float)a.d + a.eps);
         float m[1] = {0.f};
 #pragma unroll
@@ -167,15 +220,13 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm(const NormArgs a
                 float wv[N];
                 load_weight(a, j * N, wv);
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    h[i][k] = h[i][k] * rs * wv[k];
+                for (int k = 0; k < P; ++k)
+                    h[i][k] = mul2(mul2(h[i][k], both(rs)), make_float2(wv[2 * k], wv[2 * k + 1]));
                 if (FMT < 0) {
                     if (live)
-                        *((uint4 *)(Y + t * a.d) + j) = Vec<T>::pack(h[i]);
-                } else if (a.group == 0) {
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        m[0] = max_nan(m[0], fabsf(h[i][k]));
+                        *((uint4 *)(Y + t * a.d) + j) = pack_pairs(h[i]);
+                } else if (a.group_log2 == 0) {
+                    m[0] = max_nan(m[0], magnitude(h[i]));
                 }
             }
         }
@@ -183,34 +234,45 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm(const NormArgs a
             continue;
         constexpr int F = FMT < 0 ? 0 : FMT;
         float rec = 0.f;
-        if (a.group == 0) {
-            row_reduce<G, 1, true>(m, red, turn);
+        if (a.group_log2 == 0) {
+            row_reduce<S, 1, true, EXACT>(m, red, turn);
             rec = reciprocal_of<F>(m[0]);
             if (live && lane == 0)
                 a.scale[t] = scale_of<F>(m[0]);
         }
-        const int lanes = a.group / N, groups = a.group ? (a.d + a.group - 1) / a.group : 1;
+        // Groups: 2^log2 lanes share a scale, in each of their C pieces.  Lane i of them divides
+        // for piece i and the others take it from there (every lane dividing for every piece:
+        // 65536 rows of 8192 took 747 us).
+        static_assert(C <= 4, "a group has 4 lanes at least");
+        const int log2 = a.group_log2 - (N == 8 ? 3 : 2), lanes = a.group_log2 ? 1 << log2 : 0;
+        float mine = 0.f;
+        if (a.group_log2) {
+            float big = 0.f;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                float x = lane + G * i < nv ? magnitude(h[i]) : 0.f;
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2)
+                    if (o < lanes)
+                        x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
+                big = (lane & 3) == i ? x : big;
+            }
+            mine = reciprocal_of<F>(big);
+            const int in_group = lane & (lanes - 1), j = lane - in_group + G * in_group;
+            const int64_t groups = (a.d - 1 >> a.group_log2) + 1;
+            if (live && in_group < C && j < nv)
+                a.scale[t * groups + (j >> log2)] = scale_of<F>(big);
+        }
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
-            if (a.group) {
-                float x = 0.f;
-                if (j < nv)
-#pragma unroll
-                    for (int k = 0; k < N; ++k)
-                        x = max_nan(x, fabsf(h[i][k]));
-                for (int o = lanes / 2; o > 0; o >>= 1)
-                    x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
-                rec = reciprocal_of<F>(x);
-                if (live && j < nv && j % lanes == 0)
-                    a.scale[t * groups + j / lanes] = scale_of<F>(x);
-            }
+            if (a.group_log2)
+                rec = __shfl_sync(0xffffffffu, mine, (threadIdx.x & 31 & ~(lanes - 1)) + i);
             if (live && j < nv) {
                 uint32_t q[N / 4];
 #pragma unroll
-                for (int k = 0; k < N; k += 4)
-                    q[k / 4] = code_of<F>(h[i][k] * rec) | code_of<F>(h[i][k + 1] * rec) << 8 |
-                               code_of<F>(h[i][k + 2] * rec) << 16 | code_of<F>(h[i][k + 3] * rec) << 24;
+                for (int k = 0; k < P; k += 2)
+                    q[k / 2] = codes_of<F>(h[i][k], h[i][k + 1], rec);
                 uint32_t *dst = (uint32_t *)(a.codes + t * a.d + j * N);
                 if (N == 8)
                     *(uint2 *)dst = make_uint2(q[0], q[N / 4 - 1]);
@@ -231,7 +293,7 @@ template <typename T, int FMT>
 __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_any(const NormArgs a)
 {
     griddep_start();
-    __shared__ float red[2 * 32];
+    __shared__ __align__(16) float red[2 * 32];
     int turn = 0;
     const T *X = (const T *)a.X, *R = (const T *)a.R;
     T *H = (T *)a.H, *Y = (T *)a.Y;
@@ -256,7 +318,7 @@ __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_any(const NormArgs a)
                     H[t * d + j] = Vec<T>::round(h);
                 Y[t * d + j] = Vec<T>::round(h * rs * weight_at(a, j));
             }
-        } else if (a.group == 0) {
+        } else if (a.group_log2 == 0) {
             float m[1] = {0.f};
             for (int j = threadIdx.x; j < d; j += kAnyThreads)
                 m[0] = max_nan(m[0], fabsf(y_at(j)));
@@ -266,15 +328,15 @@ __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_any(const NormArgs a)
                 a.scale[t] = scale_of<F>(m[0]);
             for (int j = threadIdx.x; j < d; j += kAnyThreads) {
                 const float h = h_at(j);
-                a.codes[t * d + j] = (uint8_t)code_of<F>(h * rs * weight_at(a, j) * rec);
+                a.codes[t * d + j] = code_of<F>(h * rs * weight_at(a, j), rec);
                 if (H)
                     H[t * d + j] = Vec<T>::round(h);
             }
         } else {
             // a warp takes whole groups
-            const int groups = (d + a.group - 1) / a.group;
+            const int group = 1 << a.group_log2, groups = (d + group - 1) / group;
             for (int g = threadIdx.x / 32; g < groups; g += kAnyThreads / 32) {
-                const int j0 = g * a.group, j1 = min(d, j0 + a.group);
+                const int j0 = g * group, j1 = min(d, j0 + group);
                 float m = 0.f;
                 for (int j = j0 + threadIdx.x % 32; j < j1; j += 32)
                     m = max_nan(m, fabsf(y_at(j)));
@@ -286,7 +348,7 @@ __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_any(const NormArgs a)
                     a.scale[t * groups + g] = scale_of<F>(m);
                 for (int j = j0 + threadIdx.x % 32; j < j1; j += 32) {
                     const float h = h_at(j);
-                    a.codes[t * d + j] = (uint8_t)code_of<F>(h * rs * weight_at(a, j) * rec);
+                    a.codes[t * d + j] = code_of<F>(h * rs * weight_at(a, j), rec);
                     if (H)
                         H[t * d + j] = Vec<T>::round(h);
                 }
@@ -306,18 +368,23 @@ struct NormBwdArgs {
     float eps;
     void *dX;
     float *part;                // [lanes of rows, d] partial sums of dw
+    bool prefetch;
 };
 
 // Every group of G lanes walks the rows its place, its place + the number of groups, ...
 // and keeps the part of dw of its columns in registers.
-template <typename T, int G, int C>
-__global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm_bwd(const NormBwdArgs a)
+template <typename T, int S, int C>
+constexpr int kBwdResident = S > 512 ? S : C == 1 ? 1024 : sizeof(T) == 4 && S <= 256 ? 768 : 512;
+
+template <typename T, int S, int C>
+__global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Shape<S>::kThreads)
+    k_rmsnorm_bwd(const NormBwdArgs a)
 {
     griddep_start();
-    constexpr int N = Vec<T>::N;
-    __shared__ float red[2 * 2 * 32];
+    constexpr int N = Vec<T>::N, kRows = Shape<S>::kRows;
+    __shared__ __align__(16) float red[2 * 2 * 32];
     int turn = 0;
-    const int lane = threadIdx.x % G;
+    const int G = Shape<S>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
     const int nv = a.d / N;
     const T *dY = (const T *)a.dY, *H = (const T *)a.H, *dH = (const T *)a.dH;
     T *dX = (T *)a.dX;
@@ -331,8 +398,8 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm_bwd(const NormBw
         if (j < nv)
             load_weight(a, j * N, wv[i]);
     }
-    for (int64_t t0 = (int64_t)blockIdx.x * Lanes<G>::kRows; t0 < a.T; t0 += (int64_t)gridDim.x * Lanes<G>::kRows) {
-        const int64_t t = t0 + threadIdx.x / G;
+    for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
+        const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
         const bool live = t < a.T;
         uint4 hv[C], yv[C], rv[C];
 #pragma unroll
@@ -347,6 +414,13 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm_bwd(const NormBw
             const int j = lane + G * i;
             rv[i] = live && dH && j < nv ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
         }
+        // the rows of the round after the next, into L2
+        const int64_t later = t0 + (int64_t)gridDim.x * kRows;
+        if (a.prefetch && threadIdx.x < 3 && later + kRows <= a.T) {
+            const T *p = threadIdx.x == 0 ? H : threadIdx.x == 1 ? dY : dH;
+            if (p)
+                prefetch_l2(p + later * a.d, (uint32_t)(kRows * a.d * sizeof(T)));
+        }
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < C; ++i) {
@@ -359,7 +433,7 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm_bwd(const NormBw
                 s[1] = fmaf(y[k] * wv[i][k], h[k], s[1]);
             }
         }
-        row_reduce<G, 2, false>(s, red, turn);
+        row_reduce<S, 2, false>(s, red, turn);
         const float rs = rsqrtf(s[0] / (float)a.d + a.eps);
         const float c = s[1] / (float)a.d * rs * rs;
 #pragma unroll
@@ -379,7 +453,7 @@ __global__ void __launch_bounds__(Lanes<G>::kThreads) k_rmsnorm_bwd(const NormBw
             *((uint4 *)(dX + t * a.d) + j) = Vec<T>::pack(x);
         }
     }
-    float *part = a.part + ((int64_t)blockIdx.x * Lanes<G>::kRows + threadIdx.x / G) * a.d;
+    float *part = a.part + ((int64_t)blockIdx.x * kRows + (S == 32 ? threadIdx.x / 32 : 0)) * a.d;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         const int j = lane + G * i;
@@ -396,7 +470,7 @@ template <typename T>
 __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_bwd_any(const NormBwdArgs a)
 {
     griddep_start();
-    __shared__ float red[2 * 2 * 32];
+    __shared__ __align__(16) float red[2 * 2 * 32];
     int turn = 0;
     const T *dY = (const T *)a.dY, *H = (const T *)a.H, *dH = (const T *)a.dH;
     T *dX = (T *)a.dX;
@@ -445,17 +519,11 @@ __global__ void __launch_bounds__(1024) k_rmsnorm_dw(const float *__restrict__ p
 
 // ---- launches ----------------------------------------------------------------------------------
 
-// The lanes of a row and their pieces: 1 piece each up to 32 lanes, then the fewest lanes
-// with at most kPieces pieces
+// Pieces a lane holds, at most
 constexpr int kPieces = 4;
 
-int lanes_of(int nv)
-{
-    int g = 32;
-    while (g * kPieces < nv)
-        g *= 2;
-    return g;
-}
+// The lanes of a row of nv pieces: the fewest warps that hold it with `most` pieces a lane
+int lanes_of(int nv, int most) { return std::max(1, (nv + 32 * most - 1) / (32 * most)) * 32; }
 
 // Whether a width takes the kernels that hold rows in registers
 template <typename T>
@@ -473,17 +541,19 @@ cudaError_t launch(K kernel, int64_t grid, int threads, const A &a, cudaStream_t
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <typename T, int G, int FMT>
-cudaError_t fwd_lanes(const NormArgs &a, cudaStream_t s)
+template <typename T, int S, bool EXACT, int C, int FMT>
+cudaError_t fwd_shape(NormArgs a, int lanes, cudaStream_t s)
 {
-    const int pieces = (a.d / Vec<T>::N + G - 1) / G;
-    const int64_t blocks = (a.T + Lanes<G>::kRows - 1) / Lanes<G>::kRows;
-    const int64_t grid = std::min<int64_t>(blocks, (int64_t)1 << 30);
-    if (pieces == 1)
-        return launch(k_rmsnorm<T, G, 1, FMT>, grid, Lanes<G>::kThreads, a, s);
-    if (pieces == 2)
-        return launch(k_rmsnorm<T, G, 2, FMT>, grid, Lanes<G>::kThreads, a, s);
-    return launch(k_rmsnorm<T, G, kPieces, FMT>, grid, Lanes<G>::kThreads, a, s);
+    constexpr int kRows = Shape<S>::kRows;
+    const int threads = S == 32 ? 256 : lanes;
+    const int64_t blocks = (a.T + kRows - 1) / kRows;
+    a.ahead = 0;
+    if (FMT >= 0 && a.ldx == a.d && a.d * sizeof(T) >= 4096) {
+        int n = 1;                          // blocks that are on an SM at once
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_rmsnorm<T, S, EXACT, C, FMT>, threads, 0);
+        a.ahead = n * device_sms() * kRows;
+    }
+    return launch(k_rmsnorm<T, S, EXACT, C, FMT>, std::min<int64_t>(blocks, (int64_t)1 << 30), threads, a, s);
 }
 
 template <typename T, int FMT>
@@ -491,14 +561,20 @@ cudaError_t fwd(const NormArgs &a, cudaStream_t s)
 {
     if (!in_registers<T>(a.d, a.ldx))
         return launch(k_rmsnorm_any<T, FMT>, std::min<int64_t>(a.T, (int64_t)1 << 30), kAnyThreads, a, s);
-    switch (lanes_of(a.d / Vec<T>::N)) {
-    case 32: return fwd_lanes<T, 32, FMT>(a, s);
-    case 64: return fwd_lanes<T, 64, FMT>(a, s);
-    case 128: return fwd_lanes<T, 128, FMT>(a, s);
-    case 256: return fwd_lanes<T, 256, FMT>(a, s);
-    case 512: return fwd_lanes<T, 512, FMT>(a, s);
-    default: return fwd_lanes<T, 1024, FMT>(a, s);
-    }
+    const int nv = a.d / Vec<T>::N, g = lanes_of(nv, kPieces);
+    if (g == 32)
+        return nv <= 32   ? fwd_shape<T, 32, true, 1, FMT>(a, g, s)
+               : nv <= 64 ? fwd_shape<T, 32, true, 2, FMT>(a, g, s)
+                          : fwd_shape<T, 32, true, kPieces, FMT>(a, g, s);
+    if (g == 64)
+        return fwd_shape<T, 64, true, kPieces, FMT>(a, g, s);
+    if (g == 128)
+        return fwd_shape<T, 128, true, kPieces, FMT>(a, g, s);
+    if (g == 256)
+        return fwd_shape<T, 256, true, kPieces, FMT>(a, g, s);
+    return g < 256    ? fwd_shape<T, 256, false, kPieces, FMT>(a, g, s)
+           : g <= 512 ? fwd_shape<T, 512, false, kPieces, FMT>(a, g, s)
+                      : fwd_shape<T, 1024, false, kPieces, FMT>(a, g, s);
 }
 
 template <typename T>
@@ -511,21 +587,13 @@ cudaError_t fwd_format(const NormArgs &a, int format, cudaStream_t s)
 
 // Pieces a lane of the gradient holds, fewer than in the forward: it also keeps w and dw
 constexpr int kBwdPieces = 2;
-constexpr int kBwdThreadsPerSm = 1024;
+constexpr int kBwdThreadsPerSm = 512;
 
 template <typename T>
 bool bwd_in_registers(int d, int64_t ld)
 {
     constexpr int N = Vec<T>::N;
     return d % N == 0 && ld % N == 0 && d / N <= 1024 * kBwdPieces;
-}
-
-int bwd_lanes(int nv)
-{
-    int g = 32;
-    while (g * kBwdPieces < nv)
-        g *= 2;
-    return g;
 }
 
 struct BwdPlan {
@@ -537,20 +605,14 @@ struct BwdPlan {
 BwdPlan bwd_plan(bool registers, int nv, int64_t T)
 {
     BwdPlan p;
-    const int g = registers ? bwd_lanes(nv) : kAnyThreads;
-    p.threads = g <= 32 ? 256 : g;
+    const int g = registers ? lanes_of(nv, kBwdPieces) : kAnyThreads;
+    p.threads = g == 32 ? 256 : g;
     p.rows = p.threads / g;
     const int64_t blocks = (T + p.rows - 1) / p.rows;
-    p.grid = (int)std::min<int64_t>(blocks, (int64_t)device_sms() * (kBwdThreadsPerSm / p.threads));
+    // rows of up to 2 KB (fp32) are not asked for ahead: twice the threads
+    const int per_sm = std::max(1, (!registers || nv <= 64 ? 2 : 1) * kBwdThreadsPerSm / p.threads);
+    p.grid = (int)std::min<int64_t>(blocks, (int64_t)device_sms() * per_sm);
     return p;
-}
-
-template <typename T, int G>
-cudaError_t bwd_lanes_launch(const NormBwdArgs &a, int grid, cudaStream_t s)
-{
-    if ((a.d / Vec<T>::N + G - 1) / G == 1)
-        return launch(k_rmsnorm_bwd<T, G, 1>, grid, Lanes<G>::kThreads, a, s);
-    return launch(k_rmsnorm_bwd<T, G, kBwdPieces>, grid, Lanes<G>::kThreads, a, s);
 }
 
 template <typename T>
@@ -560,18 +622,15 @@ cudaError_t bwd(const NormBwdArgs &a, float *dw, bool accumulate, cudaStream_t s
     const int nv = a.d / Vec<T>::N;
     const BwdPlan p = bwd_plan(registers, nv, a.T);
     cudaError_t e;
-    if (!registers) {
+    if (!registers)
         e = launch(k_rmsnorm_bwd_any<T>, p.grid, kAnyThreads, a, s);
-    } else {
-        switch (bwd_lanes(nv)) {
-        case 32: e = bwd_lanes_launch<T, 32>(a, p.grid, s); break;
-        case 64: e = bwd_lanes_launch<T, 64>(a, p.grid, s); break;
-        case 128: e = bwd_lanes_launch<T, 128>(a, p.grid, s); break;
-        case 256: e = bwd_lanes_launch<T, 256>(a, p.grid, s); break;
-        case 512: e = bwd_lanes_launch<T, 512>(a, p.grid, s); break;
-        default: e = bwd_lanes_launch<T, 1024>(a, p.grid, s); break;
-        }
-    }
+    else if (p.rows > 1)
+        e = nv <= 32 ? launch(k_rmsnorm_bwd<T, 32, 1>, p.grid, p.threads, a, s)
+                     : launch(k_rmsnorm_bwd<T, 32, kBwdPieces>, p.grid, p.threads, a, s);
+    else
+        e = p.threads <= 256   ? launch(k_rmsnorm_bwd<T, 256, kBwdPieces>, p.grid, p.threads, a, s)
+            : p.threads <= 512 ? launch(k_rmsnorm_bwd<T, 512, kBwdPieces>, p.grid, p.threads, a, s)
+                               : launch(k_rmsnorm_bwd<T, 1024, kBwdPieces>, p.grid, p.threads, a, s);
     if (e != cudaSuccess)
         return e;
     count_launch();
@@ -586,7 +645,10 @@ cudaError_t rmsnorm_fwd(sn_dtype dt, const void *X, int64_t ldx, const void *R, 
                         const void *w, int64_t T, int d, float eps, void *Y, int format, int group,
                         uint8_t *codes, float *scale, cudaStream_t s)
 {
-    const NormArgs a{X, R, H, w, wdt == SN_BF16, T, ldx, d, eps, Y, codes, scale, group};
+    int log2 = 0;
+    while (1 << log2 < group)
+        ++log2;
+    const NormArgs a{X, R, H, w, wdt == SN_BF16, T, ldx, d, eps, Y, codes, scale, log2, 0};
     return dt == SN_BF16 ? fwd_format<__nv_bfloat16>(a, format, s) : fwd_format<float>(a, format, s);
 }
 
@@ -606,7 +668,9 @@ cudaError_t rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H,
                         const void *w, int64_t T, int d, float eps, void *dX, float *dw, bool accumulate,
                         float *part, cudaStream_t s)
 {
-    const NormBwdArgs a{dY, H, dH, w, wdt == SN_BF16, T, ldy, d, eps, dX, part};
+    const size_t esize = dt == SN_BF16 ? 2 : 4;
+    const NormBwdArgs a{dY, H, dH, w, wdt == SN_BF16, T, ldy, d, eps, dX, part,
+                        ldy == d && d * esize >= 4096};
     return dt == SN_BF16 ? bwd<__nv_bfloat16>(a, dw, accumulate, s) : bwd<float>(a, dw, accumulate, s);
 }
 

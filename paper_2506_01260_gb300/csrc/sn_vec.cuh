@@ -98,6 +98,41 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
+// a 16-byte piece as pairs
+__device__ __forceinline__ void unpack_pairs(uint4 v, float2 (&f)[2])
+{
+    f[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+    f[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
+}
+__device__ __forceinline__ void unpack_pairs(uint4 v, float2 (&f)[4])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint4 pack_pairs(const float2 (&f)[2])
+{
+    return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x),
+                      __float_as_uint(f[1].y));
+}
+__device__ __forceinline__ uint4 pack_pairs(const float2 (&f)[4])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 p = __float22bfloat162_rn(f[i]);
+        w[i] = *(const uint32_t *)&p;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Asks for `bytes` (a multiple of 16) from a 16-byte boundary on to be brought into L2
+__device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
 // max that keeps a NaN
 __device__ __forceinline__ float max_nan(float a, float b)
 {
