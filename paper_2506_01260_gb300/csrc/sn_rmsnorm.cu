@@ -398,24 +398,39 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
         if (j < nv)
             load_weight(a, j * N, wv[i]);
     }
-    for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
-        const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
-        const bool live = t < a.T;
-        uint4 hv[C], yv[C], rv[C];
+    const int64_t stride = (int64_t)gridDim.x * kRows;
+    auto load = [&](int64_t t, uint4 (&hv)[C], uint4 (&yv)[C], uint4 (&rv)[C]) {
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
-            const bool in = live && j < nv;
+            const bool in = t < a.T && j < nv;
             hv[i] = in ? *((const uint4 *)(H + t * a.d) + j) : make_uint4(0, 0, 0, 0);
             yv[i] = in ? *((const uint4 *)(dY + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
+            rv[i] = in && dH ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
         }
+    };
+    // The next row's loads run before this row's sums meet, where registers allow (65536 rows of
+    // 8192: 604 us, 632 without; 4173 rows of 2056 in fp32: 29.6, 35.1); rows of 4 KB and more
+    // are asked for into L2 before that.
+    constexpr bool kEarly = S <= 512 && C > 1;
+    uint4 hv[C], yv[C], rv[C], hn[C], yn[C], rn[C];
+    if (kEarly)
+        load((int64_t)blockIdx.x * kRows + (S == 32 ? threadIdx.x / 32 : 0), hn, yn, rn);
+    for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += stride) {
+        const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
+        const bool live = t < a.T;
+        if (kEarly) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int j = lane + G * i;
-            rv[i] = live && dH && j < nv ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < C; ++i) {
+                hv[i] = hn[i];
+                yv[i] = yn[i];
+                rv[i] = rn[i];
+            }
+            load(t + stride, hn, yn, rn);
+        } else {
+            load(t, hv, yv, rv);
         }
-        // the rows of the round after the next, into L2
-        const int64_t later = t0 + (int64_t)gridDim.x * kRows;
+        const int64_t later = t0 + (kEarly ? 2 : 1) * stride;
         if (a.prefetch && threadIdx.x < 3 && later + kRows <= a.T) {
             const T *p = threadIdx.x == 0 ? H : threadIdx.x == 1 ? dY : dH;
             if (p)
@@ -507,8 +522,9 @@ __global__ void __launch_bounds__(1024) k_rmsnorm_dw(const float *__restrict__ p
     const int j = blockIdx.x * 32 + threadIdx.x, per = (parts + 31) / 32;
     float s = 0.f;
     if (j < d)
+#pragma unroll 8
         for (int p = threadIdx.y * per, end = min(parts, p + per); p < end; ++p)
-            s += part[(int64_t)p * d + j];
+            s += __ldg(part + (int64_t)p * d + j);
     red[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
     s = warp_sum(red[threadIdx.x][threadIdx.y]);       // row y of the transpose: column y
@@ -587,7 +603,7 @@ cudaError_t fwd_format(const NormArgs &a, int format, cudaStream_t s)
 
 // Pieces a lane of the gradient holds, fewer than in the forward: it also keeps w and dw
 constexpr int kBwdPieces = 2;
-constexpr int kBwdThreadsPerSm = 512;
+constexpr int kBwdThreadsPerSm = 1024;
 
 template <typename T>
 bool bwd_in_registers(int d, int64_t ld)
@@ -596,23 +612,29 @@ bool bwd_in_registers(int d, int64_t ld)
     return d % N == 0 && ld % N == 0 && d / N <= 1024 * kBwdPieces;
 }
 
-struct BwdPlan {
-    int threads, rows;       // of a block
-    int grid;
-    int parts() const { return grid * rows; }
+// Threads and rows of a block
+struct BwdShape {
+    int threads, rows;
 };
-
-BwdPlan bwd_plan(bool registers, int nv, int64_t T)
+BwdShape bwd_shape(bool registers, int nv)
 {
-    BwdPlan p;
     const int g = registers ? lanes_of(nv, kBwdPieces) : kAnyThreads;
-    p.threads = g == 32 ? 256 : g;
-    p.rows = p.threads / g;
-    const int64_t blocks = (T + p.rows - 1) / p.rows;
-    // rows of up to 2 KB (fp32) are not asked for ahead: twice the threads
-    const int per_sm = std::max(1, (!registers || nv <= 64 ? 2 : 1) * kBwdThreadsPerSm / p.threads);
-    p.grid = (int)std::min<int64_t>(blocks, (int64_t)device_sms() * per_sm);
-    return p;
+    return g == 32 ? BwdShape{256, 8} : BwdShape{g, 1};
+}
+
+// The gradient's grid: the blocks that are on the GPU at once, at most kBwdThreadsPerSm
+// threads an SM
+template <typename K>
+cudaError_t bwd_launch(K kernel, BwdShape p, NormBwdArgs a, int &parts, cudaStream_t s)
+{
+    int n = 1;
+    cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, p.threads, 0);
+    if (e != cudaSuccess)
+        return e;
+    n = std::max(1, std::min(n, kBwdThreadsPerSm / p.threads));
+    const int64_t grid = std::min<int64_t>((a.T + p.rows - 1) / p.rows, (int64_t)device_sms() * n);
+    parts = (int)grid * p.rows;
+    return launch(kernel, grid, p.threads, a, s);
 }
 
 template <typename T>
@@ -620,22 +642,23 @@ cudaError_t bwd(const NormBwdArgs &a, float *dw, bool accumulate, cudaStream_t s
 {
     const bool registers = bwd_in_registers<T>(a.d, a.ldy);
     const int nv = a.d / Vec<T>::N;
-    const BwdPlan p = bwd_plan(registers, nv, a.T);
+    const BwdShape p = bwd_shape(registers, nv);
+    int parts = 0;
     cudaError_t e;
     if (!registers)
-        e = launch(k_rmsnorm_bwd_any<T>, p.grid, kAnyThreads, a, s);
+        e = bwd_launch(k_rmsnorm_bwd_any<T>, p, a, parts, s);
     else if (p.rows > 1)
-        e = nv <= 32 ? launch(k_rmsnorm_bwd<T, 32, 1>, p.grid, p.threads, a, s)
-                     : launch(k_rmsnorm_bwd<T, 32, kBwdPieces>, p.grid, p.threads, a, s);
+        e = nv <= 32 ? bwd_launch(k_rmsnorm_bwd<T, 32, 1>, p, a, parts, s)
+                     : bwd_launch(k_rmsnorm_bwd<T, 32, kBwdPieces>, p, a, parts, s);
     else
-        e = p.threads <= 256   ? launch(k_rmsnorm_bwd<T, 256, kBwdPieces>, p.grid, p.threads, a, s)
-            : p.threads <= 512 ? launch(k_rmsnorm_bwd<T, 512, kBwdPieces>, p.grid, p.threads, a, s)
-                               : launch(k_rmsnorm_bwd<T, 1024, kBwdPieces>, p.grid, p.threads, a, s);
+        e = p.threads <= 256   ? bwd_launch(k_rmsnorm_bwd<T, 256, kBwdPieces>, p, a, parts, s)
+            : p.threads <= 512 ? bwd_launch(k_rmsnorm_bwd<T, 512, kBwdPieces>, p, a, parts, s)
+                               : bwd_launch(k_rmsnorm_bwd<T, 1024, kBwdPieces>, p, a, parts, s);
     if (e != cudaSuccess)
         return e;
     count_launch();
-    e = launch_dependent(k_rmsnorm_dw, dim3((unsigned)((a.d - 1) / 32 + 1)), dim3(32, 32), 0, s, a.part,
-                         p.parts(), a.d, dw, (int)accumulate);
+    e = launch_dependent(k_rmsnorm_dw, dim3((unsigned)((a.d - 1) / 32 + 1)), dim3(32, 32), 0, s, a.part, parts,
+                         a.d, dw, (int)accumulate);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -655,13 +678,17 @@ cudaError_t rmsnorm_fwd(sn_dtype dt, const void *X, int64_t ldx, const void *R, 
 size_t rmsnorm_bwd_workspace(int64_t T, int d)
 {
     // the most parts that any type and alignment of this width take
-    size_t parts = 0;
-    for (int n = 4; n <= 8; n += 4) {
-        parts = std::max<size_t>(parts, bwd_plan(false, 0, T).parts());
+    int64_t parts = 0;
+    auto most = [&](BwdShape p) {
+        const int64_t blocks = (T + p.rows - 1) / p.rows;
+        const int64_t grid = (int64_t)device_sms() * std::max(1, kBwdThreadsPerSm / p.threads);
+        parts = std::max(parts, std::min(blocks, grid) * p.rows);
+    };
+    most(bwd_shape(false, 0));
+    for (int n = 4; n <= 8; n += 4)
         if (d % n == 0 && d / n <= 1024 * kBwdPieces)
-            parts = std::max<size_t>(parts, bwd_plan(true, d / n, T).parts());
-    }
-    return parts * (size_t)d * sizeof(float);
+            most(bwd_shape(true, d / n));
+    return (size_t)parts * d * sizeof(float);
 }
 
 cudaError_t rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H, const void *dH, sn_dtype wdt,
