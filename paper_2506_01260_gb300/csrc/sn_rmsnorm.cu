@@ -11,6 +11,7 @@
 // piece until it is written (`Row` below gives the lanes and pieces of a width).  Sums are
 // fp32 in every type; y is computed from the unrounded h and rounded once, the stored h once.
 #include <algorithm>
+#include <atomic>
 
 #include <cuda_fp8.h>
 
@@ -549,6 +550,22 @@ bool in_registers(int d, int64_t ld)
     return d % N == 0 && ld % N == 0 && d / N <= 1024 * kPieces;
 }
 
+// Blocks of `threads` that are on an SM at once, asked for once for each kernel and size (a
+// property of the code, the same on every GPU it runs on)
+template <auto KERNEL>
+int resident(int threads)
+{
+    static std::atomic<int> known[33];
+    std::atomic<int> &slot = known[threads / 32];
+    int n = slot.load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERNEL, threads, 0) != cudaSuccess)
+            return 1;
+        slot.store(n = std::max(n, 1), std::memory_order_relaxed);
+    }
+    return n;
+}
+
 template <typename K, typename A>
 cudaError_t launch(K kernel, int64_t grid, int threads, const A &a, cudaStream_t s)
 {
@@ -565,9 +582,7 @@ cudaError_t fwd_shape(NormArgs a, int lanes, cudaStream_t s)
     const int64_t blocks = (a.T + kRows - 1) / kRows;
     a.ahead = 0;
     if (FMT >= 0 && a.ldx == a.d && a.d * sizeof(T) >= 4096) {
-        int n = 1;                          // blocks that are on an SM at once
-        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_rmsnorm<T, S, EXACT, C, FMT>, threads, 0);
-        a.ahead = n * device_sms() * kRows;
+        a.ahead = resident<k_rmsnorm<T, S, EXACT, C, FMT>>(threads) * device_sms() * kRows;
     }
     return launch(k_rmsnorm<T, S, EXACT, C, FMT>, std::min<int64_t>(blocks, (int64_t)1 << 30), threads, a, s);
 }
@@ -624,17 +639,13 @@ BwdShape bwd_shape(bool registers, int nv)
 
 // The gradient's grid: the blocks that are on the GPU at once, at most kBwdThreadsPerSm
 // threads an SM
-template <typename K>
-cudaError_t bwd_launch(K kernel, BwdShape p, NormBwdArgs a, int &parts, cudaStream_t s)
+template <auto KERNEL>
+cudaError_t bwd_launch(BwdShape p, NormBwdArgs a, int &parts, cudaStream_t s)
 {
-    int n = 1;
-    cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, p.threads, 0);
-    if (e != cudaSuccess)
-        return e;
-    n = std::max(1, std::min(n, kBwdThreadsPerSm / p.threads));
+    const int n = std::max(1, std::min(resident<KERNEL>(p.threads), kBwdThreadsPerSm / p.threads));
     const int64_t grid = std::min<int64_t>((a.T + p.rows - 1) / p.rows, (int64_t)device_sms() * n);
     parts = (int)grid * p.rows;
-    return launch(kernel, grid, p.threads, a, s);
+    return launch(KERNEL, grid, p.threads, a, s);
 }
 
 template <typename T>
@@ -646,14 +657,14 @@ cudaError_t bwd(const NormBwdArgs &a, float *dw, bool accumulate, cudaStream_t s
     int parts = 0;
     cudaError_t e;
     if (!registers)
-        e = bwd_launch(k_rmsnorm_bwd_any<T>, p, a, parts, s);
+        e = bwd_launch<k_rmsnorm_bwd_any<T>>(p, a, parts, s);
     else if (p.rows > 1)
-        e = nv <= 32 ? bwd_launch(k_rmsnorm_bwd<T, 32, 1>, p, a, parts, s)
-                     : bwd_launch(k_rmsnorm_bwd<T, 32, kBwdPieces>, p, a, parts, s);
+        e = nv <= 32 ? bwd_launch<k_rmsnorm_bwd<T, 32, 1>>(p, a, parts, s)
+                     : bwd_launch<k_rmsnorm_bwd<T, 32, kBwdPieces>>(p, a, parts, s);
     else
-        e = p.threads <= 256   ? bwd_launch(k_rmsnorm_bwd<T, 256, kBwdPieces>, p, a, parts, s)
-            : p.threads <= 512 ? bwd_launch(k_rmsnorm_bwd<T, 512, kBwdPieces>, p, a, parts, s)
-                               : bwd_launch(k_rmsnorm_bwd<T, 1024, kBwdPieces>, p, a, parts, s);
+        e = p.threads <= 256   ? bwd_launch<k_rmsnorm_bwd<T, 256, kBwdPieces>>(p, a, parts, s)
+            : p.threads <= 512 ? bwd_launch<k_rmsnorm_bwd<T, 512, kBwdPieces>>(p, a, parts, s)
+                               : bwd_launch<k_rmsnorm_bwd<T, 1024, kBwdPieces>>(p, a, parts, s);
     if (e != cudaSuccess)
         return e;
     count_launch();

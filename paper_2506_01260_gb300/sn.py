@@ -8,6 +8,7 @@ host memory and streams.  There is no fallback: importing this module fails
 loudly when the library has not been built.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -492,9 +493,24 @@ def sn_quant_restore(codes, scale, fmt, out=None, stream=None):
 def _rows(t, name, dtype=None):
     """A 2-D tensor whose columns are contiguous; returns its row stride."""
     _need(t, name, dtype, contiguous=False)
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be 2-D with unit column stride" % name)
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    if t.dim() == 2:
+        if t.is_contiguous():
+            return t.shape[1]
+        if t.stride(1) == 1 or t.shape[1] <= 1:
+            return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    raise ValueError("%s must be 2-D with unit column stride" % name)
+
+
+def _given(t, name, shape, dtype):
+    """A contiguous tensor of the caller's, of this shape and type."""
+    _need(t, name, dtype)
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+
+
+def _stream_of(t, stream):
+    """As _stream; by default the current stream of t's device."""
+    return _raw_stream(t.get_device()) if stream is None else _stream(stream)
 
 
 def _error_basis(basis):
@@ -511,14 +527,16 @@ def sn_embed_fwd(table, ids, scale=1.0, out=None, out_dtype=None, basis=None, st
     V, d = table.shape
     T = ids.shape[0]
     if out is None:
-        out = torch.empty(T, d, dtype=out_dtype or table.dtype, device=table.device)
-    _need(out, "out", out_dtype)
-    _check_out(out, (T, d))
-    _check(_lib.sn_embed_fwd(_error_basis(basis), _dtype(table), _ptr(table), V, d, _ptr(ids), T,
-                             scale, _dtype(out), _ptr(out), _stream(stream)), "sn_embed_fwd")
+        out = torch.empty((T, d), dtype=out_dtype or table.dtype, device=table.device)
+    else:
+        _given(out, "out", (T, d), out_dtype)
+    _check(_lib.sn_embed_fwd(_error_basis(basis), _dtype(table), table.data_ptr(), V, d,
+                             ids.data_ptr(), T, scale, _dtype(out), out.data_ptr(),
+                             _stream_of(table, stream)), "sn_embed_fwd")
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def sn_embed_bwd_workspace(T, vocab, d):
     n = _SZ()
     _check(_lib.sn_embed_bwd_workspace(T, vocab, d, ctypes.byref(n)), "sn_embed_bwd_workspace")
@@ -530,41 +548,37 @@ def sn_embed_bwd(G, ids, vocab, scale=1.0, out=None, out_dtype=None, accumulate=
     """The table's gradient [vocab, d]: scale times the sum of G's rows of each id, zeros for
     ids without tokens; with accumulate=True added to `out`.  G may be a row-strided view."""
     ldg = _rows(G, "G")
-    _need(ids, "ids", torch.int32)
     T, d = G.shape
-    if ids.shape != (T,):
-        raise ValueError("ids must have shape [T]")
+    _given(ids, "ids", (T,), torch.int32)
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
-        out = torch.empty(vocab, d, dtype=out_dtype or G.dtype, device=G.device)
-    _need(out, "out", out_dtype)
-    _check_out(out, (vocab, d))
+        out = torch.empty((vocab, d), dtype=out_dtype or G.dtype, device=G.device)
+    else:
+        _given(out, "out", (vocab, d), out_dtype)
     if workspace is None:
-        workspace = torch.empty(sn_embed_bwd_workspace(T, vocab, d), dtype=torch.uint8,
-                                device=G.device)
-    _need(workspace, "workspace")
-    _check(_lib.sn_embed_bwd(_error_basis(basis), _dtype(G), _ptr(G), ldg, T, d, _ptr(ids), scale,
-                             _dtype(out), _ptr(out), vocab, bool(accumulate), _ptr(workspace),
-                             workspace.numel() * workspace.element_size(), _stream(stream)),
-           "sn_embed_bwd")
+        nbytes = sn_embed_bwd_workspace(T, vocab, d)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=G.device)
+    else:
+        _need(workspace, "workspace")
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(_lib.sn_embed_bwd(_error_basis(basis), _dtype(G), G.data_ptr(), ldg, T, d,
+                             ids.data_ptr(), scale, _dtype(out), out.data_ptr(), vocab,
+                             bool(accumulate), workspace.data_ptr(), nbytes,
+                             _stream_of(G, stream)), "sn_embed_bwd")
     return out
 
 
 def _norm_inputs(X, w, R, H):
-    """Row stride of X and the tensor that h is stored in (X itself without a residual)."""
+    """Row stride of X and the tensor that h is stored in (None without a residual)."""
     ldx = _rows(X, "X")
-    _need(w, "w")
-    if w.shape != (X.shape[1],):
-        raise ValueError("w must have shape [d]")
+    _given(w, "w", X.shape[1:], None)
     if R is not None:
-        _need(R, "R", X.dtype)
-        _check_out(R, X.shape)
+        _given(R, "R", X.shape, X.dtype)
         if H is None:
-            H = torch.empty_like(R)
+            return ldx, torch.empty_like(R)
     if H is not None:
-        _need(H, "H", X.dtype)
-        _check_out(H, X.shape)
+        _given(H, "H", X.shape, X.dtype)
     return ldx, H
 
 
@@ -574,11 +588,12 @@ def sn_rmsnorm_fwd(X, w, eps, R=None, H=None, out=None, stream=None):
     ldx, H = _norm_inputs(X, w, R, H)
     T, d = X.shape
     if out is None:
-        out = torch.empty(T, d, dtype=X.dtype, device=X.device)
-    _need(out, "out", X.dtype)
-    _check_out(out, (T, d))
-    _check(_lib.sn_rmsnorm_fwd(_dtype(X), _ptr(X), ldx, _ptr(R), _ptr(H), _dtype(w), _ptr(w), T, d,
-                               eps, _ptr(out), _stream(stream)), "sn_rmsnorm_fwd")
+        out = torch.empty((T, d), dtype=X.dtype, device=X.device)
+    else:
+        _given(out, "out", (T, d), X.dtype)
+    _check(_lib.sn_rmsnorm_fwd(_dtype(X), X.data_ptr(), ldx, _ptr(R), _ptr(H), _dtype(w),
+                               w.data_ptr(), T, d, eps, out.data_ptr(), _stream_of(X, stream)),
+           "sn_rmsnorm_fwd")
     return out, X if H is None else H
 
 
@@ -590,19 +605,21 @@ def sn_rmsnorm_fwd_quant(X, w, eps, fmt, R=None, H=None, group=0, codes=None, sc
     T, d = X.shape
     shape = (T, -(-d // group)) if group else (T,)
     if codes is None:
-        codes = torch.empty(T, d, dtype=torch.uint8, device=X.device)
+        codes = torch.empty((T, d), dtype=torch.uint8, device=X.device)
+    else:
+        _given(codes, "codes", (T, d), torch.uint8)
     if scale is None:
         scale = torch.empty(shape, dtype=torch.float32, device=X.device)
-    _need(codes, "codes", torch.uint8)
-    _need(scale, "scale", torch.float32)
-    if codes.shape != (T, d) or scale.shape != shape:
-        raise ValueError("codes must be [T, d] and scale %s" % (shape,))
-    _check(_lib.sn_rmsnorm_fwd_quant(_dtype(X), _ptr(X), ldx, _ptr(R), _ptr(H), _dtype(w), _ptr(w),
-                                     T, d, eps, QUANT_FORMATS[fmt], group, _ptr(codes),
-                                     _ptr(scale), _stream(stream)), "sn_rmsnorm_fwd_quant")
+    else:
+        _given(scale, "scale", shape, torch.float32)
+    _check(_lib.sn_rmsnorm_fwd_quant(_dtype(X), X.data_ptr(), ldx, _ptr(R), _ptr(H), _dtype(w),
+                                     w.data_ptr(), T, d, eps, QUANT_FORMATS[fmt], group,
+                                     codes.data_ptr(), scale.data_ptr(), _stream_of(X, stream)),
+           "sn_rmsnorm_fwd_quant")
     return codes, scale, X if H is None else H
 
 
+@functools.lru_cache(maxsize=256)
 def sn_rmsnorm_bwd_workspace(T, d):
     n = _SZ()
     _check(_lib.sn_rmsnorm_bwd_workspace(T, d, ctypes.byref(n)), "sn_rmsnorm_bwd_workspace")
@@ -615,32 +632,30 @@ def sn_rmsnorm_bwd(dY, H, w, eps, dH=None, out=None, dw=None, accumulate=False, 
     reaches h along the residual stream; dw fp32 [d], added to with accumulate=True."""
     ldy = _rows(dY, "dY")
     T, d = dY.shape
-    _need(H, "H", dY.dtype)
-    _check_out(H, (T, d))
-    _need(w, "w")
-    if w.shape != (d,):
-        raise ValueError("w must have shape [d]")
+    _given(H, "H", (T, d), dY.dtype)
+    _given(w, "w", (d,), None)
     if dH is not None:
-        _need(dH, "dH", dY.dtype)
-        _check_out(dH, (T, d))
+        _given(dH, "dH", (T, d), dY.dtype)
     if out is None:
-        out = torch.empty(T, d, dtype=dY.dtype, device=dY.device)
-    _need(out, "out", dY.dtype)
-    _check_out(out, (T, d))
+        out = torch.empty((T, d), dtype=dY.dtype, device=dY.device)
+    else:
+        _given(out, "out", (T, d), dY.dtype)
     if dw is None:
         if accumulate:
             raise ValueError("accumulate=True needs dw")
-        dw = torch.empty(d, dtype=torch.float32, device=dY.device)
-    _need(dw, "dw", torch.float32)
-    _check_out(dw, (d,))
+        dw = torch.empty((d,), dtype=torch.float32, device=dY.device)
+    else:
+        _given(dw, "dw", (d,), torch.float32)
     if workspace is None:
-        workspace = torch.empty(max(16, sn_rmsnorm_bwd_workspace(T, d)), dtype=torch.uint8,
-                                device=dY.device)
-    _need(workspace, "workspace")
-    _check(_lib.sn_rmsnorm_bwd(_dtype(dY), _ptr(dY), ldy, _ptr(H), _ptr(dH), _dtype(w), _ptr(w), T,
-                               d, eps, _ptr(out), _ptr(dw), bool(accumulate), _ptr(workspace),
-                               workspace.numel() * workspace.element_size(), _stream(stream)),
-           "sn_rmsnorm_bwd")
+        nbytes = max(16, sn_rmsnorm_bwd_workspace(T, d))
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dY.device)
+    else:
+        _need(workspace, "workspace")
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(_lib.sn_rmsnorm_bwd(_dtype(dY), dY.data_ptr(), ldy, H.data_ptr(), _ptr(dH), _dtype(w),
+                               w.data_ptr(), T, d, eps, out.data_ptr(), dw.data_ptr(),
+                               bool(accumulate), workspace.data_ptr(), nbytes,
+                               _stream_of(dY, stream)), "sn_rmsnorm_bwd")
     return out, dw
 
 
@@ -653,21 +668,20 @@ def sn_logprob_fwd(logits, target=None, scale=1.0, top=0, entropy=True, basis=No
     ld = _rows(logits, "logits")
     T, V = logits.shape
     dev = logits.device
-    lse = torch.empty(T, 2, dtype=torch.float32, device=dev)
+    lse = torch.empty((T, 2), dtype=torch.float32, device=dev)
     logp = H = ids = alt = None
     if target is not None:
-        _need(target, "target", torch.int32)
-        if target.shape != (T,):
-            raise ValueError("target must have shape [T]")
-        logp = torch.empty(T, dtype=torch.float32, device=dev)
+        _given(target, "target", (T,), torch.int32)
+        logp = torch.empty((T,), dtype=torch.float32, device=dev)
     if entropy:
-        H = torch.empty(T, dtype=torch.float32, device=dev)
+        H = torch.empty((T,), dtype=torch.float32, device=dev)
     if top:
-        ids = torch.empty(T, top, dtype=torch.int32, device=dev)
-        alt = torch.empty(T, top, dtype=torch.float32, device=dev)
-    _check(_lib.sn_logprob_fwd(_error_basis(basis), _dtype(logits), _ptr(logits), T, V, ld,
-                               _ptr(target), scale, _ptr(logp), _ptr(lse), _ptr(H), top, _ptr(ids),
-                               _ptr(alt), _stream(stream)), "sn_logprob_fwd")
+        ids = torch.empty((T, top), dtype=torch.int32, device=dev)
+        alt = torch.empty((T, top), dtype=torch.float32, device=dev)
+    _check(_lib.sn_logprob_fwd(_error_basis(basis), _dtype(logits), logits.data_ptr(), T, V, ld,
+                               _ptr(target), scale, _ptr(logp), lse.data_ptr(), _ptr(H), top,
+                               _ptr(ids), _ptr(alt), _stream_of(logits, stream)),
+           "sn_logprob_fwd")
     return logp, lse, H, ids, alt
 
 
@@ -677,25 +691,21 @@ def sn_logprob_bwd(logits, lse, target=None, dlogp=None, scale=1.0, entropy=None
     each fp32 [T].  `out` may be logits (in place)."""
     ld = _rows(logits, "logits")
     T, V = logits.shape
-    _need(lse, "lse", torch.float32)
-    if lse.shape != (T, 2):
-        raise ValueError("lse must have shape [T, 2]")
+    _given(lse, "lse", (T, 2), torch.float32)
     for t, name in ((dlogp, "dlogp"), (entropy, "entropy"), (dentropy, "dentropy")):
         if t is not None:
-            _need(t, name, torch.float32)
-            if t.shape != (T,):
-                raise ValueError("%s must have shape [T]" % name)
+            _given(t, name, (T,), torch.float32)
     if target is not None:
-        _need(target, "target", torch.int32)
-        if target.shape != (T,):
-            raise ValueError("target must have shape [T]")
+        _given(target, "target", (T,), torch.int32)
     if out is None:
-        out = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
-    ldd = _rows(out, "out", logits.dtype)
-    _check_out(out, (T, V))
-    _check(_lib.sn_logprob_bwd(_dtype(logits), _ptr(logits), T, V, ld, _ptr(target), _ptr(lse),
-                               _ptr(dlogp), _ptr(entropy), _ptr(dentropy), scale, _ptr(out), ldd,
-                               _stream(stream)), "sn_logprob_bwd")
+        out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        ldd = V
+    else:
+        ldd = _rows(out, "out", logits.dtype)
+        _check_out(out, (T, V))
+    _check(_lib.sn_logprob_bwd(_dtype(logits), logits.data_ptr(), T, V, ld, _ptr(target),
+                               lse.data_ptr(), _ptr(dlogp), _ptr(entropy), _ptr(dentropy), scale,
+                               out.data_ptr(), ldd, _stream_of(logits, stream)), "sn_logprob_bwd")
     return out
 
 
@@ -758,12 +768,13 @@ def sn_grads_sumsq(grads, out=None, accumulate=False, stream=None):
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
-        out = torch.empty(1, dtype=torch.float64, device=grads.device)
-    _need(out, "out", torch.float64)
-    if out.numel() < 1:
-        raise ValueError("out must have an element")
-    _check(_lib.sn_grads_sumsq(grads.handle, _ptr(out), bool(accumulate), _stream(stream)),
-           "sn_grads_sumsq")
+        out = torch.empty((1,), dtype=torch.float64, device=grads.device)
+    else:
+        _need(out, "out", torch.float64)
+        if out.numel() < 1:
+            raise ValueError("out must have an element")
+    _check(_lib.sn_grads_sumsq(grads.handle, out.data_ptr(), bool(accumulate),
+                               _stream_of(out, stream)), "sn_grads_sumsq")
     return out
 
 
@@ -772,12 +783,13 @@ def sn_grads_clip(grads, sumsq, max_norm, norm=None, stream=None):
     (device fp32 [1])."""
     _need(sumsq, "sumsq", torch.float64)
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device=grads.device)
-    _need(norm, "norm", torch.float32)
+        norm = torch.empty((1,), dtype=torch.float32, device=grads.device)
+    else:
+        _need(norm, "norm", torch.float32)
     if sumsq.numel() < 1 or norm.numel() < 1:
         raise ValueError("sumsq and norm must have an element")
-    _check(_lib.sn_grads_clip(grads.handle, _ptr(sumsq), max_norm, _ptr(norm), _stream(stream)),
-           "sn_grads_clip")
+    _check(_lib.sn_grads_clip(grads.handle, sumsq.data_ptr(), max_norm, norm.data_ptr(),
+                              _stream_of(sumsq, stream)), "sn_grads_clip")
     return norm
 
 
