@@ -27,6 +27,20 @@ struct Raw {
         for (int i = 0; i < kWords; ++i)
             v[i] = __ldg((const uint4 *)p + i);
     }
+    // `n` elements one by one, zeros after them
+    __device__ __forceinline__ void load_single(const S *p, int n)
+    {
+        union {
+            uint4 w[kWords];
+            S x[8];
+        } u;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            u.x[k] = k < n ? p[k] : Vec<S>::round(0.f);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            v[i] = u.w[i];
+    }
     __device__ __forceinline__ void get(float2 (&f)[4]) const
     {
 #pragma unroll
@@ -380,35 +394,43 @@ struct SumArgs {
     const int32_t *order, *sorted, *places;
     const uint32_t *used;
     int window, windows, slices;   // places of a window; blocks along a row
-    float *part;                   // [windows][2][d]: sums of a first and a last id that go on in other windows
+    float *part;                   // [windows][2][dp]: sums of a first and a last id that go on in other windows
+    int dp;                        // d rounded up to 8
 };
 
 constexpr int kMaxWindow = 128;
 
-// 8 columns of a row of dE: the sum times the scale, in addition to what is there
-template <typename D>
-__device__ __forceinline__ void write_piece(D *dst, const float (&acc)[8], float scale, bool accumulate)
+// n <= 8 columns of a row of dE: the sum times the scale, in addition to what is there.  VEC: all
+// 8, on a 16-byte boundary.
+template <typename D, bool VEC>
+__device__ __forceinline__ void write_piece(D *dst, int n, const float2 (&acc)[4], float scale, bool accumulate)
 {
-    float f[8];
+    float2 f[4];
     if (accumulate) {
-        load_floats(dst, f);
+        Raw<D> old;
+        if (VEC)
+            old.load(dst);
+        else
+            old.load_single(dst, n);
+        old.get(f);
+    }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            f[k] = fmaf(acc[k], scale, f[k]);
+    for (int k = 0; k < 4; ++k)
+        f[k] = accumulate ? fma2(acc[k], both(scale), f[k]) : mul2(acc[k], both(scale));
+    if (VEC) {
+        put_piece(dst, f);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            f[k] = acc[k] * scale;
+            if (k < n)
+                dst[k] = Vec<D>::round(k % 2 ? f[k / 2].y : f[k / 2].x);
     }
-#pragma unroll
-    for (int k = 0; k < 8; k += Vec<D>::N)
-        *(uint4 *)(dst + k) = Vec<D>::pack(*(const float(*)[Vec<D>::N])(f + k));
 }
 
-__device__ __forceinline__ void write_part(float *dst, const float (&acc)[8])
+__device__ __forceinline__ void write_part(float *dst, const float2 (&acc)[4])
 {
-    *(float4 *)dst = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    *(float4 *)(dst + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    *(float4 *)dst = make_float4(acc[0].x, acc[0].y, acc[1].x, acc[1].y);
+    *(float4 *)(dst + 4) = make_float4(acc[2].x, acc[2].y, acc[3].x, acc[3].y);
 }
 
 // Blocks [0, windows * slices) sum; the others, 32 ids each, write the rows without tokens.
@@ -417,12 +439,12 @@ __device__ __forceinline__ void write_part(float *dst, const float (&acc)[8])
 // flight.
 enum { WRITE = 0, ADD_AHEAD = 1, ADD = 2 };
 
-template <typename S, typename D, int MODE>
+template <typename S, typename D, int MODE, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
 {
     griddep_start();
     constexpr bool ACC = MODE == ADD_AHEAD;
-    const int nv = a.d / 8;
+    const int nv = a.dp / 8;
     D *dE = (D *)a.dE;
     if ((int64_t)blockIdx.x >= (int64_t)a.windows * a.slices) {
         const int64_t word = (int64_t)blockIdx.x - (int64_t)a.windows * a.slices;
@@ -431,9 +453,13 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
         const int n = (int)min((int64_t)32, a.vocab - v0);
         for (int i = 0; i < n; ++i)
             if (!((used >> i) & 1u)) {
-                uint4 *row = (uint4 *)(dE + (v0 + i) * a.d);
-                for (int j = threadIdx.x; j < a.d / Vec<D>::N; j += kThreads)
-                    row[j] = make_uint4(0, 0, 0, 0);
+                D *row = dE + (v0 + i) * a.d;
+                if (VEC)
+                    for (int j = threadIdx.x; j < a.d / Vec<D>::N; j += kThreads)
+                        ((uint4 *)row)[j] = make_uint4(0, 0, 0, 0);
+                else
+                    for (int j = threadIdx.x; j < a.d; j += kThreads)
+                        row[j] = Vec<D>::round(0.f);
             }
         return;
     }
@@ -480,7 +506,11 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (i0 + u < n) {
-                    g[u].load(G + (int64_t)tokens[i0 + u] * a.ldg + j * 8);
+                    const S *src = G + (int64_t)tokens[i0 + u] * a.ldg + j * 8;
+                    if (VEC)
+                        g[u].load(src);
+                    else
+                        g[u].load_single(src, a.d - j * 8);
                     if (ACC && ids[i0 + u + 2] != ids[i0 + u + 1])
                         old[ACC ? u : 0].load(dE + (int64_t)ids[i0 + u + 1] * a.d + j * 8);
                 }
@@ -498,19 +528,16 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
                 if (!ends && i0 + u + 1 < n)
                     continue;
                 if (first || !ends) {
-                    const float f[8] = {acc[0].x, acc[0].y, acc[1].x, acc[1].y, acc[2].x, acc[2].y, acc[3].x, acc[3].y};
-                    write_part(a.part + ((int64_t)w * 2 + !first) * a.d + j * 8, f);
-                } else if (MODE == ADD) {
-                    const float f[8] = {acc[0].x, acc[0].y, acc[1].x, acc[1].y, acc[2].x, acc[2].y, acc[3].x, acc[3].y};
-                    write_piece(dE + (int64_t)id * a.d + j * 8, f, a.scale, true);
-                } else {
+                    write_part(a.part + ((int64_t)w * 2 + !first) * a.dp + j * 8, acc);
+                } else if (ACC) {
                     float2 sum[4];
-                    if (ACC)
-                        old[ACC ? u : 0].get(sum);
+                    old[ACC ? u : 0].get(sum);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        sum[k] = ACC ? fma2(acc[k], both(a.scale), sum[k]) : mul2(acc[k], both(a.scale));
+                        sum[k] = fma2(acc[k], both(a.scale), sum[k]);
                     put_piece(dE + (int64_t)id * a.d + j * 8, sum);
+                } else {
+                    write_piece<D, VEC>(dE + (int64_t)id * a.d + j * 8, a.d - j * 8, acc, a.scale, MODE == ADD);
                 }
                 first = false;
 #pragma unroll
@@ -526,7 +553,7 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
 // their sums are added in the warps' order.
 constexpr int kJoin = 8;
 
-template <typename D>
+template <typename D, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_join_rows(const SumArgs a)
 {
     griddep_start();
@@ -562,26 +589,29 @@ __global__ void __launch_bounds__(kThreads) k_join_rows(const SumArgs a)
             if (n < kThreads)
                 break;
         }
-        float acc[8];
+        float2 acc[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            acc[k] = 0.f;
+        for (int k = 0; k < 4; ++k)
+            acc[k] = both(0.f);
         if (j < a.d) {
             // part 0: the last of window w, parts 1 to `more`: the first of those after it
             for (int v0 = warp; v0 <= more; v0 += U * kWarps8) {
-                float f[U][8];
+                Raw<float> f[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int v = v0 + u * kWarps8;
                     if (v <= more)
-                        load_floats(a.part + ((int64_t)(w + v) * 2 + (v == 0)) * a.d + j, f[u]);
+                        f[u].load(a.part + ((int64_t)(w + v) * 2 + (v == 0)) * a.dp + j);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (v0 + u * kWarps8 <= more)
+                    if (v0 + u * kWarps8 <= more) {
+                        float2 x[4];
+                        f[u].get(x);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            acc[k] += f[u][k];
+                        for (int k = 0; k < 4; ++k)
+                            acc[k] = add2(acc[k], x[k]);
+                    }
             }
         }
         write_part(&sums[warp][lane * 8], acc);
@@ -589,50 +619,11 @@ __global__ void __launch_bounds__(kThreads) k_join_rows(const SumArgs a)
         if (warp == 0 && j < a.d) {
             for (int v = 1; v < kWarps8; ++v)
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    acc[k] += sums[v][lane * 8 + k];
-            write_piece((D *)a.dE + (int64_t)id * a.d + j, acc, a.scale, a.accumulate);
+                for (int k = 0; k < 4; ++k)
+                    acc[k] = add2(acc[k], *(const float2 *)&sums[v][lane * 8 + 2 * k]);
+            write_piece<D, VEC>((D *)a.dE + (int64_t)id * a.d + j, a.d - j, acc, a.scale, a.accumulate);
         }
         __syncthreads();
-    }
-}
-
-// Widths that are no multiple of 8, gradients off the alignment: a block sums the runs that
-// start in its window by single elements, to their ends.
-template <typename S, typename D>
-__global__ void __launch_bounds__(kThreads) k_sum_rows_any(const SumArgs a)
-{
-    griddep_start();
-    D *dE = (D *)a.dE;
-    const S *G = (const S *)a.G;
-    if ((int64_t)blockIdx.x >= a.windows) {
-        const int64_t v0 = ((int64_t)blockIdx.x - a.windows) * 32;
-        const uint32_t used = a.used[v0 / 32];
-        const int n = (int)min((int64_t)32, a.vocab - v0);
-        for (int i = 0; i < n; ++i)
-            if (!((used >> i) & 1u))
-                for (int j = threadIdx.x; j < a.d; j += kThreads)
-                    dE[(v0 + i) * a.d + j] = Vec<D>::round(0.f);
-        return;
-    }
-    const int places = *a.places;
-    const int p0 = blockIdx.x * a.window, p1 = min(places, p0 + a.window);
-    int p = p0;
-    while (p < p1 && p > 0 && a.sorted[p] == a.sorted[p - 1])
-        ++p;
-    while (p < p1) {
-        const int id = a.sorted[p];
-        int end = p + 1;
-        while (end < places && a.sorted[end] == id)
-            ++end;
-        for (int j = threadIdx.x; j < a.d; j += kThreads) {
-            float acc = 0.f;
-            for (int q = p; q < end; ++q)
-                acc += Vec<S>::one(G[(int64_t)a.order[q] * a.ldg + j]);
-            D *dst = dE + (int64_t)id * a.d + j;
-            *dst = Vec<D>::round(a.accumulate ? fmaf(acc, a.scale, Vec<D>::one(*dst)) : acc * a.scale);
-        }
-        p = end;
     }
 }
 
@@ -690,31 +681,34 @@ Layout layout_of(int64_t T, int64_t vocab, int d)
     l.used = at;
     at += up256((size_t)((vocab + 31) / 32) * 4);
     l.part = at;
-    at += up256((size_t)l.windows * 2 * d * sizeof(float));
+    at += up256((size_t)l.windows * 2 * ((d + 7) / 8 * 8) * sizeof(float));
     l.total = at;
     return l;
+}
+
+template <typename S, typename D, int MODE, bool VEC>
+cudaError_t sum_and_join(const SumArgs &a, cudaStream_t s)
+{
+    const int64_t grid = (int64_t)a.windows * a.slices + (MODE == WRITE ? (a.vocab + 31) / 32 : 0);
+    cudaError_t e = grid > 0 ? launch(k_sum_rows<S, D, MODE, VEC>, grid, kThreads, 0, s, a) : cudaSuccess;
+    if (e == cudaSuccess && a.windows > 1)
+        e = launch(k_join_rows<D, VEC>, (int64_t)(a.windows - 1 + kJoin - 1) / kJoin * ((a.d + 255) / 256), kThreads,
+                   0, s, a);
+    return e;
 }
 
 template <typename S, typename D>
 cudaError_t sum_rows(const SumArgs &a, cudaStream_t s)
 {
-    const int64_t fill = a.accumulate ? 0 : (a.vocab + 31) / 32;
+    // rows that are no whole 16-byte pieces: single elements
     if (a.d % 8 != 0 || a.ldg % 8 != 0)
-        return a.windows + fill == 0 ? cudaSuccess
-                                     : launch(k_sum_rows_any<S, D>, a.windows + fill, kThreads, 0, s, a);
-    cudaError_t e = cudaSuccess;
-    if ((int64_t)a.windows * a.slices + fill > 0)
-        // fewer tokens than ids: most ids have one token or two, and a batch ends in several
-        // rows of dE (16384 tokens of 128256 ids: 78 us, 102 without the loads ahead); more
-        // tokens than ids: they cost rows of G in flight (65536 of 32000: 370 us, 320 without)
-        e = !a.accumulate ? launch(k_sum_rows<S, D, WRITE>, (int64_t)a.windows * a.slices + fill, kThreads, 0, s, a)
-            : a.T < a.vocab
-                ? launch(k_sum_rows<S, D, ADD_AHEAD>, (int64_t)a.windows * a.slices, kThreads, 0, s, a)
-                : launch(k_sum_rows<S, D, ADD>, (int64_t)a.windows * a.slices, kThreads, 0, s, a);
-    if (e == cudaSuccess && a.windows > 1)
-        e = launch(k_join_rows<D>, (int64_t)(a.windows - 1 + kJoin - 1) / kJoin * ((a.d + 255) / 256), kThreads, 0, s,
-                   a);
-    return e;
+        return a.accumulate ? sum_and_join<S, D, ADD, false>(a, s) : sum_and_join<S, D, WRITE, false>(a, s);
+    if (!a.accumulate)
+        return sum_and_join<S, D, WRITE, true>(a, s);
+    // fewer tokens than ids: most ids have one token or two, and a batch ends in several rows
+    // of dE (16384 tokens of 128256 ids: 78 us, 102 without the loads ahead); more tokens than
+    // ids: they cost rows of G in flight (65536 of 32000: 370 us, 320 without)
+    return a.T < a.vocab ? sum_and_join<S, D, ADD_AHEAD, true>(a, s) : sum_and_join<S, D, ADD, true>(a, s);
 }
 
 }  // namespace
@@ -755,7 +749,8 @@ cudaError_t embed_bwd(sn_dtype gdt, const void *G, int64_t ldg, int64_t T, int d
     if (e != cudaSuccess)
         return e;
     const SumArgs a{G, ldg, T, vocab, d, scale, dE, accumulate, q.order, q.sorted, q.places, q.used,
-                    l.window, l.windows, std::min(64, (d + 8 * kThreads - 1) / (8 * kThreads)), (float *)(m + l.part)};
+                    l.window, l.windows, std::min(64, (d + 8 * kThreads - 1) / (8 * kThreads)), (float *)(m + l.part),
+                    (d + 7) / 8 * 8};
     if (gdt == SN_BF16)
         return edt == SN_BF16 ? sum_rows<__nv_bfloat16, __nv_bfloat16>(a, s) : sum_rows<__nv_bfloat16, float>(a, s);
     return edt == SN_BF16 ? sum_rows<float, __nv_bfloat16>(a, s) : sum_rows<float, float>(a, s);
