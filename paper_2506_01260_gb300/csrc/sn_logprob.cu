@@ -11,10 +11,12 @@
 // Sums are fp32.  A row is one block's, or, where rows are few, that of a cluster of blocks
 // that join their sums in shared memory.
 //
-// The alternatives come out of the same pass: each thread keeps the largest logit it saw,
-// and the n-th largest of those bounds the row's n-th largest from below, so only the few
-// elements at or above the bound are looked at again (in L2) and ranked by value, the lower
-// token first among equals.
+// The alternatives come out of the same pass: each thread keeps the largest logit it saw, the
+// step that it was in and the largest of its other steps.  The n-th largest of the maxima of 64
+// groups of threads bounds the row's n-th largest from below, so only the steps that reach the
+// bound are read again, one or two for each alternative, and the few elements found there are
+// ranked by value, the lower token first among equals.  Reading whole threads' pieces again
+// instead costs 14 us at 4096 rows of 128256 bf16 (the rows in flight pass L2).
 #include <algorithm>
 
 #include "sn_vec.cuh"
@@ -25,7 +27,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxTop = 32;
 constexpr int kCand = 1024;             // elements at or above the bound that a block ranks
+constexpr int kGroups = 64;             // of a block's threads: at least kMaxTop
+constexpr int kSpare = 2;               // groups that the bound may let in beside those asked for
 constexpr int kMaxCluster = 8;
+constexpr int kPieces = 4;              // of a thread's step
 // 2^t below 2^-200 is 0 in fp32; clamped there, 0 * t is 0 where t is -infinity
 constexpr float kFloor = -200.f;
 
@@ -107,16 +112,6 @@ __device__ __forceinline__ float shift(float m0, float m1, float c)
     return rounded(b1) ? fmaf(m0, c, -b1) : (m0 - m1) * c;
 }
 
-__device__ __forceinline__ void join(Sums &x, const Sums &y, float c)
-{
-    const float m = fmaxf(x.m, y.m);
-    const float dx = shift(x.m, m, c), dy = shift(y.m, m, c);
-    const float fx = ex2(dx), fy = ex2(dy);
-    x.a = fx * fmaf(x.s, fmaxf(dx, kFloor), x.a) + fy * fmaf(y.s, fmaxf(dy, kFloor), y.a);
-    x.s = fx * x.s + fy * y.s;
-    x.m = m;
-}
-
 // The sums of a warp's lanes, or of the block's warps, in every lane: the largest m first, so
 // that each lane is rescaled once
 template <int LANES>
@@ -141,10 +136,10 @@ template <int THREADS>
 struct Shared {
     Sums sums[THREADS / 32];
     Sums block;                        // this block's sums, read by the cluster
-    uint32_t lane_max[THREADS];
-    uint16_t hot[THREADS];             // threads whose elements reach the bound
+    __align__(16) uint32_t keys[kGroups];  // the largest key that each group of threads saw, 0: none
+    int step[THREADS];                 // of each warp, those that `collect` reads
     uint32_t bound;
-    int n_hot, n_cand, nan;            // nan: a NaN among the elements
+    int n_cand, nan;                   // nan: a NaN among the elements
     uint64_t cand[kCand];
     uint64_t best[kMaxTop];            // this block's alternatives in order, read by the cluster
     uint64_t merged[kMaxCluster * kMaxTop];
@@ -181,16 +176,23 @@ __device__ __forceinline__ void each(const RowView<T> &row, int i0, int i1, bool
         }
 }
 
+// What a thread knows of the elements it saw: the largest key (0: no element), the step that it
+// is in (its first piece, -1: none), and the largest key of its other steps
+struct Best {
+    uint32_t key, next;
+    int at;
+};
+
 // sh.cand = this block's elements whose key is at least `from`, a key not below the bound; how
-// many there are (the list holds the first kCand of them).  They lie in the hot threads' pieces
-// and among the loose elements; the block's threads read the pieces of all hot threads at once.
+// many there are (the list holds the first kCand of them).  They lie in the best steps of the
+// threads that saw such an element, in more of their pieces where `next` reaches it too, and
+// among the loose elements.  The lanes of a warp share its threads' pieces.
 template <typename T, int THREADS>
 __device__ __forceinline__ int collect(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i1, bool ends,
-                                       uint32_t from)
+                                       const Best &mine, uint32_t from)
 {
     constexpr int N = Vec<T>::N;
-    const int per = (i1 - i0 + THREADS - 1) / THREADS;          // pieces of a thread, at most
-    const int log2 = per > 1 ? 32 - __clz(per - 1) : 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool nan = sh.nan;
     const float least = value_of(from);
     auto put = [&](float x, int v) {
@@ -198,8 +200,30 @@ __device__ __forceinline__ int collect(Shared<THREADS> &sh, const RowView<T> &ro
         if (at < kCand)
             sh.cand[at] = rank_key(key_of(x), v);
     };
-    for (int x = threadIdx.x; x < sh.n_hot << log2; x += THREADS) {
-        const int i = i0 + sh.hot[x >> log2] + (x & ((1 << log2) - 1)) * THREADS;
+    uint32_t hot = __ballot_sync(0xffffffffu, mine.key >= from);
+    uint32_t wide = __ballot_sync(0xffffffffu, mine.key >= from && (mine.next >= from || mine.at < 0));
+    hot &= ~wide;
+    if (hot >> lane & 1)
+        sh.step[warp * 32 + __popc(hot & ((1u << lane) - 1u))] = mine.at;
+    __syncwarp();
+    int n = __popc(hot);
+    const int *step = &sh.step[warp * 32 + lane / kPieces];
+    int w = i1;                        // the next piece of the thread whose pieces are all looked at
+    while (n > 0 || wide) {
+        int i = i1;
+        if (n > 0) {                   // a step each of up to eight threads
+            if (lane / kPieces < n)
+                i = *step + lane % kPieces * THREADS;
+            step += 32 / kPieces;
+            n -= 32 / kPieces;
+        } else {
+            if (w >= i1)
+                w = i0 + warp * 32 + __ffs(wide) - 1;
+            i = w + lane * THREADS;
+            w += 32 * THREADS;
+            if (w >= i1)
+                wide &= wide - 1;
+        }
         if (i >= i1)
             continue;
         float f[N];
@@ -265,51 +289,52 @@ __device__ void lowest_equal(Shared<THREADS> &sh, const RowView<T> &row, int i0,
     }
 }
 
-// The block's `top` best elements into sh.best, in order.  sh.lane_max: the largest key that
-// each thread saw (0: no element).
+// out[r] = the key of rank r < top among n different ones (0: no key): eight lanes count those
+// above each
+template <int THREADS>
+__device__ __forceinline__ void place(const uint64_t *keys, int n, int top, uint64_t *out)
+{
+    const int sub = threadIdx.x % 8;
+    for (int i0 = threadIdx.x / 32 * 4; i0 < n; i0 += THREADS / 8) {
+        const int i = i0 + threadIdx.x % 32 / 8;
+        const uint64_t k = i < n ? keys[i] : 0;
+        int r = 0;
+        for (int j = sub; j < n; j += 8)
+            r += keys[j] > k;
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1)
+            r += __shfl_xor_sync(0xffffffffu, r, o);
+        if (sub == 0 && k != 0 && r < top)
+            out[r] = k;
+    }
+}
+
+// The block's `top` best elements into sh.best, in order
 template <typename T, int THREADS>
 __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i1, bool ends, int top,
-                       uint32_t mine, int elements)
+                       const Best &mine, int elements)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (warp == 0) {
-        // the top-th largest of the threads' maxima, bit by bit from the first in which they
-        // differ, until exactly `top` reach it
-        uint32_t k[THREADS / 32], hi = 0, lo = 0xffffffffu;
-#pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) {
-            k[i] = sh.lane_max[i * 32 + lane];
-            hi = max(hi, k[i]);
-            lo = min(lo, k[i]);
-        }
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        lo = __reduce_min_sync(0xffffffffu, lo);
+        // close below the top-th largest of the groups' maxima: bit by bit from the first in
+        // which they differ, until `top` or a few more reach it
+        static_assert(kGroups == 64, "two a lane");
+        const uint2 k = *(const uint2 *)&sh.keys[2 * lane];
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, max(k.x, k.y));
+        const uint32_t lo = __reduce_min_sync(0xffffffffu, min(k.x, k.y));
         const int first = 31 - __clz(hi ^ lo);                // -1: all the same
         uint32_t b = first < 0 ? hi : hi & ~((2u << first) - 1u);
         for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {     // bf16 keys end there
             const uint32_t trial = b | 1u << bit;
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < THREADS / 32; ++i)
-                n += k[i] >= trial;
-            n = __reduce_add_sync(0xffffffffu, n);
-            if (n >= top)
+            const int n = __popc(__ballot_sync(0xffffffffu, k.x >= trial)) + __popc(__ballot_sync(0xffffffffu, k.y >= trial));
+            if (n >= top) {
                 b = trial;
-            if (n == top)
-                break;
-        }
-        b = max(b, kLowestKey);
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) {
-            const uint32_t hit = __ballot_sync(0xffffffffu, k[i] >= b);
-            if (k[i] >= b)
-                sh.hot[n + __popc(hit & ((1u << lane) - 1u))] = (uint16_t)(i * 32 + lane);
-            n += __popc(hit);
+                if (n <= top + kSpare)
+                    break;
+            }
         }
         if (lane == 0) {
-            sh.bound = b;
-            sh.n_hot = n;
+            sh.bound = max(b, kLowestKey);
             sh.n_cand = 0;
             sh.nan = hi == 0xffffffffu;
         }
@@ -317,7 +342,7 @@ __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i
     __syncthreads();
     const uint32_t bound = sh.bound;
     const int want = min(top, elements);
-    int n = collect<T, THREADS>(sh, row, i0, i1, ends, bound);
+    int n = collect<T, THREADS>(sh, row, i0, i1, ends, mine, bound);
     bool ties = false;
     if (n > kCand) {
         // many equal elements at the bound (a masked row's are -infinity): those above it
@@ -327,17 +352,10 @@ __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i
         if (threadIdx.x == 0)
             sh.n_cand = 0;
         __syncthreads();
-        n = bound == 0xffffffffu ? 0 : collect<T, THREADS>(sh, row, i0, i1, ends, bound + 1);
+        n = bound == 0xffffffffu ? 0 : collect<T, THREADS>(sh, row, i0, i1, ends, mine, bound + 1);
     }
     if (n <= kCand) {
-        for (int i = threadIdx.x; i < n; i += THREADS) {
-            const uint64_t k = sh.cand[i];
-            int r = 0;
-            for (int j = 0; j < n; ++j)
-                r += sh.cand[j] > k;
-            if (r < top)
-                sh.best[r] = k;
-        }
+        place<THREADS>(sh.cand, n, top, sh.best);
         if (ties)
             lowest_equal<T, THREADS>(sh, row, i0, i1, ends, bound, n, want);
     } else {
@@ -346,7 +364,7 @@ __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i
         uint64_t last = ~0ull;
         for (int r = 0; r < want; ++r) {
             uint64_t b = 0;
-            if (mine >= bound)
+            if (mine.key >= bound)
                 each<T, THREADS>(row, i0, i1, ends, [&](float x, int v) {
                     const uint64_t k = rank_key(key_of(x), v);
                     b = k < last && k > b ? k : b;
@@ -385,7 +403,9 @@ __device__ __forceinline__ T ld_remote(const T *p, uint32_t rank)
 }
 
 // Asks for the first bytes of a later row's pieces, so that DRAM stays busy while rows' sums meet
-constexpr int kAhead = 32 * 1024;
+// (8192 rows of 32000 bf16 with 8 alternatives: 107 us, 112 with half as much; with twice as much,
+// longer rows push each other out of L2)
+constexpr int kAhead = 64 * 1024;
 
 // ---- one pass over a thread's pieces ---------------------------------------------------------
 
@@ -470,8 +490,11 @@ struct Walk {
     float top, m, b;
     bool short_;                     // near(m, c)
     float2 s, a;
+    float next;                      // the largest logit of the steps but the one that `top` is in,
+    int at;                          // whose first piece is `at`
 
-    __device__ __forceinline__ Walk() : top(-INFINITY), m(-INFINITY), b(0.f), short_(false), s(both(0.f)), a(both(0.f)) {}
+    __device__ __forceinline__ Walk()
+        : top(-INFINITY), m(-INFINITY), b(0.f), short_(false), s(both(0.f)), a(both(0.f)), next(-INFINITY), at(-1) {}
 
     template <bool ENT>
     __device__ __forceinline__ void raise(float to, float c)
@@ -497,10 +520,15 @@ struct Walk {
         if (ENT)
             a.x = fmaf(e, fmaxf(t, kFloor), a.x);
     }
-    template <typename T, bool ENT, int U>
-    __device__ __forceinline__ void pieces(const uint4 (&v)[U], float c)
+    template <typename T, bool TOP, bool ENT, int U>
+    __device__ __forceinline__ void pieces(const uint4 (&v)[U], int i, float c)
     {
-        top = fmaxf(top, Words<T>::max_of(v));
+        const float most = Words<T>::max_of(v);
+        if (TOP) {
+            next = fmaxf(next, fminf(top, most));
+            at = most > top ? i : at;
+        }
+        top = fmaxf(top, most);
         if (top > m && !(fmaf(top, c, -b) < kRise && short_))
             raise<ENT>(top, c);
         if (short_) {
@@ -542,7 +570,6 @@ struct Walk {
     }
 };
 
-constexpr int kPieces = 4;
 template <typename T, int THREADS>
 struct RowPart : RowView<T> {
     int i0, i1;
@@ -591,15 +618,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob(const LogpA
         uint4 v[U], next[U];
         row.load(i, v);
         while (i + U * THREADS < row.i1) {
+            row.load(i + U * THREADS, next);
+            walk.pieces<T, TOP, ENT>(v, i, c);
             i += U * THREADS;
-            row.load(i, next);
-            walk.pieces<T, ENT>(v, c);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 v[u] = next[u];
         }
         if (i < row.i1)
-            walk.pieces<T, ENT>(v, c);
+            walk.pieces<T, TOP, ENT>(v, i, c);
         if (threadIdx.x == 0 && cluster == 1 && t + ahead < a.T) {
             const RowView<T> later((const T *)a.x + (t + ahead) * a.ld, a.V);
             const int bytes = min(later.nv * 16, kAhead);
@@ -612,21 +639,31 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob(const LogpA
             saw = true;
         }
         Sums p = walk.sums<ENT>(c);
-        uint32_t mine = 0;
+        Best mine = {0, 0, walk.at};
         if (TOP) {
-            mine = saw ? key_of(p.m) : 0u;
+            if (saw) {
+                mine.key = key_of(p.m);
+                mine.next = key_of(walk.next);
+            }
             if (p.s != p.s) {                     // a NaN among them, or an infinity
                 bool nan = false;
                 each<T, THREADS>(row, row.i0, row.i1, ends, [&](float x, int) { nan |= x != x; });
-                mine = nan ? 0xffffffffu : mine;
+                if (nan)
+                    mine = {0xffffffffu, 0, -1};
             }
         }
         join_lanes<32>(p, c);
         __syncthreads();
         if (lane == 0)
             sh.sums[warp] = p;
-        if (TOP)
-            sh.lane_max[threadIdx.x] = mine;
+        if (TOP) {
+            uint32_t k = mine.key;
+#pragma unroll
+            for (int o = THREADS / kGroups / 2; o > 0; o >>= 1)
+                k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+            if (threadIdx.x % (THREADS / kGroups) == 0)
+                sh.keys[threadIdx.x / (THREADS / kGroups)] = k;
+        }
         __syncthreads();
         p = sh.sums[lane % W];
         join_lanes<W>(p, c);
@@ -638,20 +675,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob(const LogpA
         if (cluster > 1) {
             cluster_sync();
             if (rank == 0) {
-                for (int r = 1; r < cluster; ++r)
-                    join(p, ld_remote(&sh.block, r), c);
+                p = {-INFINITY, 0.f, 0.f};
+                if (lane % kMaxCluster < cluster)
+                    p = ld_remote(&sh.block, lane % kMaxCluster);
+                join_lanes<kMaxCluster>(p, c);
                 if (TOP) {
                     for (int i = threadIdx.x; i < cluster * a.top; i += THREADS)
                         sh.merged[i] = ld_remote(&sh.best[i % a.top], i / a.top);
                     __syncthreads();
-                    for (int i = threadIdx.x; i < cluster * a.top; i += THREADS) {
-                        const uint64_t k = sh.merged[i];
-                        int r = 0;
-                        for (int j = 0; j < cluster * a.top; ++j)
-                            r += sh.merged[j] > k;
-                        if (k != 0 && r < a.top)
-                            sh.cand[r] = k;
-                    }
+                    place<THREADS>(sh.merged, cluster * a.top, a.top, sh.cand);
                     __syncthreads();
                 }
             }

@@ -191,6 +191,29 @@ def test_selection_of_many_equal_or_clustered(sn, dt, T, kind):
 
 
 @pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("T,V", [(320, 9001), (320, 40000), (320, 1000), (20, 60000)])
+@pytest.mark.parametrize("top", [1, 8, 32])
+def test_alternatives_that_few_threads_hold(sn, dt, T, V, top):
+    """The best elements at the same place of one, two or five steps of a row, of any number of
+    threads a row, with a few equal ones, -infinities and a row's ends among them."""
+    g = gen(V + top)
+    x = logits(T, V, dt, g).clone()
+    per = 16 // x.element_size()
+    for t in range(T):
+        piece = 37 * t % (V // per)
+        step = (512, 1024, 2048, 4096, 2048 + 256)[t % 5]
+        cols = (piece * per + t % per + torch.arange(1 + t % 40, device="cuda") * step * per) % V
+        x[t, cols] = 40 + torch.randint(6, cols.shape, generator=g, device="cuda").to(x.dtype)
+        if t % 7 == 0:
+            x[t, :9] = 41
+            x[t, -9:] = 43
+        if t % 11 == 0:
+            x[t, 50:] = -math.inf
+    _, _, _, ids, _ = sn.sn_logprob_fwd(x, top=top)
+    assert torch.equal(ids.long(), best(x, top))
+
+
+@pytest.mark.parametrize("dt", DT)
 @pytest.mark.parametrize("T,V,pad,opad,scale", [
     (1, 1, 0, 0, 1.0), (3, 7, 0, 0, 1.0), (9, 33, 2, 2, 0.5), (40, 1000, 0, 3, 1.0), (6, 50257, 0, 0, 1.25),
     (5, 50257, 7, 7, 1.0), (4, 8200, 8, 0, 2.0), (300, 257, 0, 0, 1.0)])
