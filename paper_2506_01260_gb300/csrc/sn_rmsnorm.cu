@@ -143,26 +143,54 @@ __device__ __forceinline__ uint8_t code_of(float y, float rec)
 
 // ---- forward, rows in registers ------------------------------------------------------------
 
-// The largest magnitude of a piece, a NaN if it holds one (or infinities of both signs)
+__device__ __forceinline__ float max_magnitude(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+    return r;
+}
+
+// The largest magnitude of a piece, a NaN if it holds one
 template <int P>
 __device__ __forceinline__ float magnitude(const float2 (&f)[P])
 {
     float m = 0.f;
-    float2 sum = both(0.f);
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        m = fmaxf(m, fmaxf(fabsf(f[k].x), fabsf(f[k].y)));
-        sum = add2(sum, f[k]);
-    }
-    const float z = sum.x + sum.y;
-    return z != z ? z : m;
+    for (int k = 0; k < P; ++k)
+        m = max_magnitude(m, f[k].x, f[k].y);
+    return m;
 }
 
-// Threads of an SM that registers are kept low enough for.  Codes from bf16 rows want 113
+// The maximum over 2^n neighbouring lanes (`lanes` of them, >= 4) of each of C values: lane i
+// gets that of value i mod 4.  Two halvings, then one value a lane: 5 shuffles for 4 values of
+// 16 lanes, not 16 (65536 rows of 8192 with 128 columns a scale: 576 us, 652).
+template <int C>
+__device__ __forceinline__ float max_of_lanes(const float (&v)[C], int lane, int lanes)
+{
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[i] = i < C ? v[i < C ? i : 0] : 0.f;
+    const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+    for (int i = 0; i < 4; i += 2)
+        if (i < C)
+            x[i] = max_nan(odd ? x[i + 1] : x[i], __shfl_xor_sync(0xffffffffu, odd ? x[i] : x[i + 1], 1));
+    float m = max_nan(high ? x[2] : x[0], __shfl_xor_sync(0xffffffffu, high ? x[0] : x[2], 2));
+#pragma unroll
+    for (int o = 4; o < 32; o *= 2)
+        if (o < lanes)
+            m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+    return m;
+}
+
+// Threads of an SM that registers are kept low enough for.  Codes from bf16 rows want 110
 // registers at 4 pieces a lane: capped at 80 for 768 threads they spill (16384 rows of 4096: 95
-// us instead of 73).
+// us, 73 as it is).  Blocks of 512 are two an SM even where they spill (8192 rows of 16384
+// bf16: 163 us, 230 with one block).
 template <typename T, int S, int C, int FMT>
-constexpr int kResident = S > 256 ? S : C == 1 ? 1536 : C == 2 ? 1024 : FMT < 0 || sizeof(T) == 4 ? 768 : 512;
+constexpr int kResident = S > 512 ? S : S == 512 ? 1024 : C == 1 ? 1536 : C == 2 ? 1024
+                        : FMT < 0 || sizeof(T) == 4 ? 768 : 512;
 
 template <typename T, int S, bool EXACT, int C, int FMT>
 __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / Shape<S>::kThreads)
@@ -248,16 +276,11 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / 
         const int log2 = a.group_log2 - (N == 8 ? 3 : 2), lanes = a.group_log2 ? 1 << log2 : 0;
         float mine = 0.f;
         if (a.group_log2) {
-            float big = 0.f;
+            float each[C];
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                float x = lane + G * i < nv ? magnitude(h[i]) : 0.f;
-#pragma unroll
-                for (int o = 1; o < 32; o *= 2)
-                    if (o < lanes)
-                        x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
-                big = (lane & 3) == i ? x : big;
-            }
+            for (int i = 0; i < C; ++i)
+                each[i] = lane + G * i < nv ? magnitude(h[i]) : 0.f;
+            const float big = max_of_lanes(each, lane, lanes);
             mine = reciprocal_of<F>(big);
             const int in_group = lane & (lanes - 1), j = lane - in_group + G * in_group;
             const int64_t groups = (a.d - 1 >> a.group_log2) + 1;
