@@ -112,6 +112,26 @@ __device__ __forceinline__ float shift(float m0, float m1, float c)
     return rounded(b1) ? fmaf(m0, c, -b1) : (m0 - m1) * c;
 }
 
+// What a row's sums give: ln S, and from it log probabilities and the entropy.  A row whose
+// logits are all -infinity: S = 0, lse = -infinity, every probability is 0 and so is the entropy.
+struct Result {
+    bool empty;
+    float l2, ln;
+    __device__ __forceinline__ Result(const Sums &p, float c)
+    {
+        empty = p.m == -INFINITY && p.s == 0.f;
+        const float b = base_of(p.m, c);
+        l2 = empty ? -INFINITY : log2f(p.s);
+        // ln S for the sums of 2^((x - m) c): the base's rounding taken out again
+        ln = empty ? -INFINITY : kLn2 * (rounded(b) ? l2 - fmaf(p.m, c, -b) : l2);
+    }
+    __device__ __forceinline__ float entropy(const Sums &p) const { return empty ? 0.f : kLn2 * (l2 - p.a / p.s); }
+    __device__ __forceinline__ float logp(float x, const Sums &p, float scale) const
+    {
+        return empty ? -INFINITY : fmaf(x - p.m, scale, -ln);
+    }
+};
+
 // The sums of a warp's lanes, or of the block's warps, in every lane: the largest m first, so
 // that each lane is rescaled once
 template <int LANES>
@@ -176,6 +196,36 @@ __device__ __forceinline__ void each(const RowView<T> &row, int i0, int i1, bool
         }
 }
 
+// `put(value, column)` for the elements of a piece whose key is at least `from`; nan: one of the
+// row's is a NaN
+template <typename T, typename F>
+__device__ __forceinline__ void reaching(uint4 piece, int column, uint32_t from, bool nan, F put)
+{
+    constexpr int N = Vec<T>::N;
+    const float least = value_of(from);
+    float f[N];
+    Vec<T>::unpack(piece, f);
+    uint32_t hits = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        hits |= (f[k] >= least ? 1u : 0u) << k;
+    if (nan) {
+        hits = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            hits |= (key_of(f[k]) >= from ? 1u : 0u) << k;
+    }
+    while (hits) {
+        const int k = __ffs(hits) - 1;
+        float y = f[0];
+#pragma unroll
+        for (int q = 1; q < N; ++q)
+            y = k == q ? f[q] : y;
+        put(y, column + k);
+        hits &= hits - 1;
+    }
+}
+
 // What a thread knows of the elements it saw: the largest key (0: no element), the step that it
 // is in (its first piece, -1: none), and the largest key of its other steps
 struct Best {
@@ -194,7 +244,6 @@ __device__ __forceinline__ int collect(Shared<THREADS> &sh, const RowView<T> &ro
     constexpr int N = Vec<T>::N;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool nan = sh.nan;
-    const float least = value_of(from);
     auto put = [&](float x, int v) {
         const int at = atomicAdd(&sh.n_cand, 1);
         if (at < kCand)
@@ -226,27 +275,7 @@ __device__ __forceinline__ int collect(Shared<THREADS> &sh, const RowView<T> &ro
         }
         if (i >= i1)
             continue;
-        float f[N];
-        Vec<T>::unpack(row.piece(i), f);
-        uint32_t hits = 0;
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            hits |= (f[k] >= least ? 1u : 0u) << k;
-        if (nan) {
-            hits = 0;
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                hits |= (key_of(f[k]) >= from ? 1u : 0u) << k;
-        }
-        while (hits) {
-            const int k = __ffs(hits) - 1;
-            float y = f[0];
-#pragma unroll
-            for (int q = 1; q < N; ++q)
-                y = k == q ? f[q] : y;
-            put(y, row.head + i * N + k);
-            hits &= hits - 1;
-        }
+        reaching<T>(row.piece(i), row.head + i * N, from, nan, put);
     }
     if (ends && (int)threadIdx.x < row.loose()) {
         const int v = row.loose_at(threadIdx.x);
@@ -309,6 +338,38 @@ __device__ __forceinline__ void place(const uint64_t *keys, int n, int top, uint
     }
 }
 
+// A key close below the top-th largest of a warp's K keys a lane (0: no element), at least that
+// of -infinity: bit by bit from the first in which they differ, until `top` or a few more reach
+// it.  nan: the largest is that of a NaN.
+template <typename T, int K>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&k)[K], int top, bool &nan)
+{
+    uint32_t hi = k[0], lo = k[0];
+#pragma unroll
+    for (int i = 1; i < K; ++i) {
+        hi = max(hi, k[i]);
+        lo = min(lo, k[i]);
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    nan = hi == 0xffffffffu;
+    const int first = 31 - __clz(hi ^ lo);                // -1: all the same
+    uint32_t b = first < 0 ? hi : hi & ~((2u << first) - 1u);
+    for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {         // bf16 keys end there
+        const uint32_t trial = b | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            n += __popc(__ballot_sync(0xffffffffu, k[i] >= trial));
+        if (n >= top) {
+            b = trial;
+            if (n <= top + kSpare)
+                break;
+        }
+    }
+    return max(b, kLowestKey);
+}
+
 // The block's `top` best elements into sh.best, in order
 template <typename T, int THREADS>
 __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i1, bool ends, int top,
@@ -316,27 +377,14 @@ __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (warp == 0) {
-        // close below the top-th largest of the groups' maxima: bit by bit from the first in
-        // which they differ, until `top` or a few more reach it
         static_assert(kGroups == 64, "two a lane");
-        const uint2 k = *(const uint2 *)&sh.keys[2 * lane];
-        const uint32_t hi = __reduce_max_sync(0xffffffffu, max(k.x, k.y));
-        const uint32_t lo = __reduce_min_sync(0xffffffffu, min(k.x, k.y));
-        const int first = 31 - __clz(hi ^ lo);                // -1: all the same
-        uint32_t b = first < 0 ? hi : hi & ~((2u << first) - 1u);
-        for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {     // bf16 keys end there
-            const uint32_t trial = b | 1u << bit;
-            const int n = __popc(__ballot_sync(0xffffffffu, k.x >= trial)) + __popc(__ballot_sync(0xffffffffu, k.y >= trial));
-            if (n >= top) {
-                b = trial;
-                if (n <= top + kSpare)
-                    break;
-            }
-        }
+        const uint32_t k[2] = {sh.keys[2 * lane], sh.keys[2 * lane + 1]};
+        bool nan;
+        const uint32_t b = bound_of<T>(k, top, nan);
         if (lane == 0) {
-            sh.bound = max(b, kLowestKey);
+            sh.bound = b;
             sh.n_cand = 0;
-            sh.nan = hi == 0xffffffffu;
+            sh.nan = nan;
         }
     }
     __syncthreads();
@@ -359,15 +407,15 @@ __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i
         if (ties)
             lowest_equal<T, THREADS>(sh, row, i0, i1, ends, bound, n, want);
     } else {
-        // more than the list holds lie in fewer than `top` threads' elements: the best below
-        // the last one, `want` times over
-        uint64_t last = ~0ull;
+        // more than the list holds lie in fewer than `top` threads' elements: the best that is
+        // not above `most`, `want` times over
+        uint64_t most = ~0ull;
         for (int r = 0; r < want; ++r) {
             uint64_t b = 0;
             if (mine.key >= bound)
                 each<T, THREADS>(row, i0, i1, ends, [&](float x, int v) {
                     const uint64_t k = rank_key(key_of(x), v);
-                    b = k < last && k > b ? k : b;
+                    b = k <= most && k > b ? k : b;
                 });
             b = warp_max64(b);
             __syncthreads();
@@ -379,7 +427,7 @@ __device__ void select(Shared<THREADS> &sh, const RowView<T> &row, int i0, int i
                 b = sh.found[w] > b ? sh.found[w] : b;
             if (threadIdx.x == 0)
                 sh.best[r] = b;
-            last = b;
+            most = b - 1;
         }
     }
     for (int i = want + threadIdx.x; i < top; i += THREADS)
@@ -690,38 +738,217 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_logprob(const LogpA
         }
         if (rank == 0) {
             const uint64_t *best = TOP && cluster > 1 ? sh.cand : sh.best;
-            // a row whose logits are all -infinity: S = 0, lse = -infinity, every
-            // probability is 0 and so is the entropy
-            const bool empty = p.m == -INFINITY && p.s == 0.f;
-            const float b = base_of(p.m, c), l2 = empty ? -INFINITY : log2f(p.s);
-            // ln S for the sums of 2^((x - m) c): the base's rounding taken out again
-            const float ln = empty ? -INFINITY : kLn2 * (rounded(b) ? l2 - fmaf(p.m, c, -b) : l2);
+            const Result z(p, c);
             if (threadIdx.x == 0) {
                 if (a.lse)
-                    *(float2 *)(a.lse + 2 * t) = make_float2(p.m, ln);
+                    *(float2 *)(a.lse + 2 * t) = make_float2(p.m, z.ln);
                 if (ENT)
-                    a.entropy[t] = empty ? 0.f : kLn2 * (l2 - p.a / p.s);
+                    a.entropy[t] = z.entropy(p);
                 if (a.logp) {
                     const int v = a.target[t];
                     if (v >= a.V && a.err)
                         atomicOr(a.err, SN_EBIT_BAD_ID);
-                    float lp = 0.f;
-                    if (v >= 0 && v < a.V)
-                        lp = empty ? -INFINITY : fmaf(Vec<T>::one(row.p[v]) - p.m, a.scale, -ln);
-                    a.logp[t] = lp;
+                    a.logp[t] = v >= 0 && v < a.V ? z.logp(Vec<T>::one(row.p[v]), p, a.scale) : 0.f;
                 }
             }
             if (TOP && (int)threadIdx.x < a.top) {
                 const uint64_t k = best[threadIdx.x];
                 a.top_ids[t * a.top + threadIdx.x] = (int32_t)(0xffffffffu - (uint32_t)k);
-                const float x = value_of((uint32_t)(k >> 32));
-                a.top_logp[t * a.top + threadIdx.x] = empty ? -INFINITY : fmaf(x - p.m, a.scale, -ln);
+                a.top_logp[t * a.top + threadIdx.x] = z.logp(value_of((uint32_t)(k >> 32)), p, a.scale);
             }
         }
         if (cluster > 1)
             cluster_sync();             // the others' shared memory was read
         else if (TOP)
             __syncthreads();
+    }
+}
+
+// ---- narrow rows -----------------------------------------------------------------------------
+// A warp has a whole row of at most kNarrow elements in registers, so its sums start from the
+// row's maximum and the alternatives are found without reading again.  16384 rows of 1024 bf16:
+// 10.3 us, 36 with a block of 128 threads a row; with 8 alternatives 25 and 69.
+
+constexpr int kNarrow = 1024, kNarrowWarps = 8, kNarrowCand = 192;
+
+template <typename T, bool TOP, bool ENT>
+__global__ void __launch_bounds__(32 * kNarrowWarps, 4) k_logprob_narrow(const LogpArgs a)
+{
+    griddep_start();
+    constexpr int N = Vec<T>::N, C = kNarrow / (32 * N), K = 4;
+    __shared__ uint64_t cands[TOP ? kNarrowWarps : 1][TOP ? kNarrowCand : 1];
+    __shared__ int counts[kNarrowWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float c = a.scale * kLog2e;
+    for (int64_t t = (int64_t)blockIdx.x * kNarrowWarps + warp; t < a.T; t += (int64_t)gridDim.x * kNarrowWarps) {
+        const RowView<T> row((const T *)a.x + t * a.ld, a.V);
+        uint4 v[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            v[i] = lane + 32 * i < row.nv ? row.piece(lane + 32 * i)
+                                          : make_uint4(Words<T>::kNone, Words<T>::kNone, Words<T>::kNone, Words<T>::kNone);
+        const bool has_loose = lane < row.loose();
+        const float loose = has_loose ? Vec<T>::one(row.p[row.loose_at(lane)]) : -INFINITY;
+        const int target = a.logp ? a.target[t] : -1;
+        const float at_target = target >= 0 && target < a.V ? Vec<T>::one(row.p[target]) : 0.f;
+        const float own = fmaxf(Words<T>::max_of(v), loose);
+        Walk walk;
+        walk.top = own;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            walk.top = fmaxf(walk.top, __shfl_xor_sync(0xffffffffu, walk.top, o));
+        walk.pieces<T, false, ENT>(v, 0, c);
+        if (has_loose)
+            walk.one<ENT>(loose, c);
+        Sums p = {walk.m, walk.s.x + walk.s.y, walk.a.x + walk.a.y};       // the same m in every lane
+        const bool none = p.s != p.s;                   // NaN, or an infinity
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            p.s += __shfl_xor_sync(0xffffffffu, p.s, o);
+            if (ENT)
+                p.a += __shfl_xor_sync(0xffffffffu, p.a, o);
+        }
+        const Result z(p, c);
+        if (lane == 0) {
+            if (a.lse)
+                *(float2 *)(a.lse + 2 * t) = make_float2(p.m, z.ln);
+            if (ENT)
+                a.entropy[t] = z.entropy(p);
+            if (a.logp) {
+                if (target >= a.V && a.err)
+                    atomicOr(a.err, SN_EBIT_BAD_ID);
+                a.logp[t] = target >= 0 && target < a.V ? z.logp(at_target, p, a.scale) : 0.f;
+            }
+        }
+        if (!TOP)
+            continue;
+        // fn(value, column, piece) for each of this lane's elements
+        const auto each = [&](auto fn) {
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                if (lane + 32 * i >= row.nv)
+                    continue;
+                float f[N];
+                Vec<T>::unpack(v[i], f);
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    fn(f[k], row.head + (lane + 32 * i) * N + k, i);
+            }
+            if (has_loose)
+                fn(loose, row.loose_at(lane), 0);
+        };
+        // the largest keys of this lane's pieces, C / K of them at a time
+        uint32_t key[K];
+#pragma unroll
+        for (int g = 0; g < K; ++g) {
+            uint4 u[C / K];
+#pragma unroll
+            for (int i = 0; i < C / K; ++i)
+                u[i] = v[g * (C / K) + i];
+            key[g] = lane + 32 * g * (C / K) < row.nv ? key_of(Words<T>::max_of(u)) : 0u;
+        }
+        if (has_loose)
+            key[0] = max(key[0], key_of(loose));
+        if (none)
+            each([&](float x, int, int i) { key[i * K / C] = x != x ? 0xffffffffu : key[i * K / C]; });
+        bool nan;
+        const uint32_t bound = bound_of<T>(key, a.top, nan);
+        uint64_t *cand = cands[warp];
+        // the elements whose key is at least `from`: how many, the first kNarrowCand in the list
+        const auto collect_from = [&](uint32_t from) {
+            __syncwarp();
+            if (lane == 0)
+                counts[warp] = 0;
+            __syncwarp();
+            const auto put = [&](float x, int col) {
+                const int at = atomicAdd(&counts[warp], 1);
+                if (at < kNarrowCand)
+                    cand[at] = rank_key(key_of(x), col);
+            };
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                if (lane + 32 * i < row.nv && key[i * K / C] >= from)
+                    reaching<T>(v[i], row.head + (lane + 32 * i) * N, from, nan, put);
+            if (has_loose && key_of(loose) >= from)
+                put(loose, row.loose_at(lane));
+            __syncwarp();
+            return counts[warp];
+        };
+        const auto write = [&](int r, uint64_t k) {
+            a.top_ids[t * a.top + r] = (int32_t)(0xffffffffu - (uint32_t)k);
+            a.top_logp[t * a.top + r] = z.logp(value_of((uint32_t)(k >> 32)), p, a.scale);
+        };
+        int n = collect_from(bound);
+        bool ties = false;
+        if (n > kNarrowCand) {
+            // many equal ones at the bound: those above it, then the lowest tokens at it
+            ties = true;
+            n = bound == 0xffffffffu ? 0 : collect_from(bound + 1);
+        }
+        if (n <= kNarrowCand) {
+            for (int i = lane; i < n; i += 32) {
+                const uint64_t k = cand[i];
+                int r = 0;
+                for (int j = 0; j < n; ++j)
+                    r += cand[j] > k;
+                if (r < a.top)
+                    write(r, k);
+            }
+            if (!ties)
+                continue;
+            // in the order of the columns: the loose ones in front, the pieces, the last ones
+            const uint32_t before = (1u << lane) - 1u;
+            const uint32_t ends = __ballot_sync(0xffffffffu, has_loose && key_of(loose) == bound);
+            const uint32_t front = ends & ((1u << row.head) - 1u);
+            const bool mine = ends >> lane & 1;
+            if (mine && lane < row.head && n + __popc(front & before) < a.top)
+                write(n + __popc(front & before), rank_key(bound, row.loose_at(lane)));
+            n += __popc(front);
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                if (n >= a.top)
+                    break;
+                float f[N];
+                Vec<T>::unpack(v[i], f);
+                int same = 0;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    same += lane + 32 * i < row.nv && key_of(f[k]) == bound;
+                int r = same;                              // and those of the lanes before
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const int x = __shfl_up_sync(0xffffffffu, r, o);
+                    r += lane >= o ? x : 0;
+                }
+                const int all = __shfl_sync(0xffffffffu, r, 31);
+                r += n - same;
+                if (same)
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (key_of(f[k]) == bound) {
+                            if (r < a.top)
+                                write(r, rank_key(bound, row.head + (lane + 32 * i) * N + k));
+                            ++r;
+                        }
+                n += all;
+            }
+            if (mine && lane >= row.head && n + __popc(ends & ~front & before) < a.top)
+                write(n + __popc(ends & ~front & before), rank_key(bound, row.loose_at(lane)));
+            continue;
+        }
+        // more than the list holds lie in few lanes' pieces: the best that is not above `most`
+        uint64_t most = ~0ull;
+        for (int r = 0; r < a.top; ++r) {
+            uint64_t b = 0;
+            each([&](float x, int col, int) {
+                const uint64_t k = rank_key(key_of(x), col);
+                b = k <= most && k > b ? k : b;
+            });
+            b = warp_max64(b);
+            most = b - 1;
+            if (lane == 0)
+                write(r, b);
+        }
     }
 }
 
@@ -752,13 +979,15 @@ struct RowCoef {
     }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a)
+// LANES threads share a row's step: a block has one row's, or several narrow rows' (16384 rows of
+// 1024 bf16: 12 us, 33 with a block a row)
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArgs a)
 {
     griddep_start();
-    constexpr int N = Vec<T>::N, U = kBwdPieces;
-    const int seg = blockIdx.x;
-    for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
+    constexpr int N = Vec<T>::N, U = kBwdPieces, kRows = kBwdThreads / LANES;
+    const int seg = blockIdx.x, lane = threadIdx.x % LANES;
+    for (int64_t t = (int64_t)blockIdx.y * kRows + threadIdx.x / LANES; t < a.T; t += (int64_t)gridDim.y * kRows) {
         const RowView<T> row((const T *)a.x + t * a.ld, a.V);
         T *out = (T *)a.dx + t * a.ldd;
         RowCoef q;
@@ -777,14 +1006,14 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a
         // marked to leave L2 first, coming and going: 8191 rows of 50257 took 275 us without, now
         // 253, 4096 of 128256 322, now 295; with either mark alone less was gained, or nothing
         uint4 v[U];
-        const int i0 = seg * U * kBwdThreads + threadIdx.x;
+        const int i0 = seg * U * LANES + lane;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i0 + u * kBwdThreads < row.nv)
-                v[u] = __ldcs((const uint4 *)(row.p + row.head) + i0 + u * kBwdThreads);
+            if (i0 + u * LANES < row.nv)
+                v[u] = __ldcs((const uint4 *)(row.p + row.head) + i0 + u * LANES);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * kBwdThreads;
+            const int i = i0 + u * LANES;
             if (i >= row.nv)
                 continue;
             const int c0 = row.head + i * N;
@@ -817,8 +1046,8 @@ __global__ void __launch_bounds__(kBwdThreads) k_logprob_bwd(const LogpBwdArgs a
                     out[c0 + k] = Vec<T>::round(f[k]);
             }
         }
-        if (seg == 0 && (int)threadIdx.x < row.loose()) {
-            const int c = row.loose_at(threadIdx.x);
+        if (seg == 0 && lane < row.loose()) {
+            const int c = row.loose_at(lane);
             out[c] = Vec<T>::round(q.at(Vec<T>::one(row.p[c])) + (c == q.target ? q.a : 0.f));
         }
     }
@@ -847,9 +1076,24 @@ cudaError_t fwd(const LogpArgs &a, int cluster, cudaStream_t s)
                      : fwd_launch<T, THREADS, false, false>(a, cluster, s);
 }
 
+template <typename T, bool TOP, bool ENT>
+cudaError_t narrow_launch(const LogpArgs &a, cudaStream_t s)
+{
+    const int64_t blocks = std::min<int64_t>((a.T + kNarrowWarps - 1) / kNarrowWarps, (int64_t)1 << 30);
+    count_launch();
+    const cudaError_t e = launch_dependent(k_logprob_narrow<T, TOP, ENT>, dim3((unsigned)blocks),
+                                           dim3(32 * kNarrowWarps), 0, s, a);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
 template <typename T>
 cudaError_t fwd_type(const LogpArgs &a, cudaStream_t s)
 {
+    if (a.V <= kNarrow) {
+        if (a.entropy)
+            return a.top > 0 ? narrow_launch<T, true, true>(a, s) : narrow_launch<T, false, true>(a, s);
+        return a.top > 0 ? narrow_launch<T, true, false>(a, s) : narrow_launch<T, false, false>(a, s);
+    }
     const int nv = a.V / Vec<T>::N;
     if (nv <= 1024)
         return fwd<T, 128>(a, 1, s);
@@ -866,16 +1110,26 @@ cudaError_t fwd_type(const LogpArgs &a, cudaStream_t s)
     return fwd<T, 512>(a, cluster, s);
 }
 
+template <typename T, int LANES>
+cudaError_t bwd_launch(const LogpBwdArgs &a, cudaStream_t s)
+{
+    constexpr int per = Vec<T>::N * kBwdPieces * LANES, kRows = kBwdThreads / LANES;
+    count_launch();
+    const cudaError_t e = launch_dependent(k_logprob_bwd<T, LANES>,
+                                           dim3((unsigned)((a.V + per - 1) / per),
+                                                (unsigned)std::min<int64_t>((a.T + kRows - 1) / kRows, 65535)),
+                                           dim3(kBwdThreads), 0, s, a);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
 template <typename T>
 cudaError_t bwd_type(const LogpBwdArgs &a, cudaStream_t s)
 {
-    constexpr int per = Vec<T>::N * kBwdPieces * kBwdThreads;
-    count_launch();
-    const cudaError_t e = launch_dependent(k_logprob_bwd<T>,
-                                           dim3((unsigned)((a.V + per - 1) / per),
-                                                (unsigned)std::min<int64_t>(a.T, 65535)),
-                                           dim3(kBwdThreads), 0, s, a);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    const int lanes = (a.V / Vec<T>::N + kBwdPieces - 1) / kBwdPieces;
+    return lanes <= 32    ? bwd_launch<T, 32>(a, s)
+           : lanes <= 64  ? bwd_launch<T, 64>(a, s)
+           : lanes <= 128 ? bwd_launch<T, 128>(a, s)
+                          : bwd_launch<T, kBwdThreads>(a, s);
 }
 
 }  // namespace

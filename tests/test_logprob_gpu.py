@@ -214,6 +214,41 @@ def test_alternatives_that_few_threads_hold(sn, dt, T, V, top):
 
 
 @pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("V,pad", [(5, 0), (12, 3), (40, 1), (259, 0), (1000, 5), (1024, 0), (1024, 3), (1025, 0)])
+@pytest.mark.parametrize("kind", ["constant", "few values", "some above a tie", "masked", "rising", "NaN", "one lane's"])
+def test_alternatives_of_narrow_rows(sn, dt, V, pad, kind):
+    """Rows that a warp holds, from below one 16-byte piece to the widest, on and off the
+    alignment: ties, masks and values that are no numbers, at each number of alternatives."""
+    g = gen(V + pad)
+    T = 37
+    x = logits(T, V, dt, g, pad)
+    new = x.clone()
+    if kind == "constant":
+        new[:] = torch.randn(T, 1, generator=g, device="cuda").to(x.dtype)
+    elif kind == "few values":
+        new[:] = torch.randint(3, (T, V), generator=g, device="cuda").to(x.dtype)
+    elif kind == "some above a tie":
+        new[:] = torch.where(torch.rand(T, V, generator=g, device="cuda") < 9 / V, 1.0, -2.0).to(x.dtype)
+    elif kind == "masked":
+        new[torch.rand(T, V, generator=g, device="cuda") < torch.linspace(0.5, 1, T, device="cuda")[:, None]] = -math.inf
+        new[::3] = new[::3].clamp(min=torch.finfo(x.dtype).min)
+    elif kind == "rising":
+        new[:] = torch.linspace(-5, 5, V, device="cuda").to(x.dtype)
+    elif kind == "NaN":
+        new[torch.rand(T, V, generator=g, device="cuda") < torch.linspace(0, 1, T, device="cuda")[:, None]] = math.nan
+        new[::4, 0] = math.nan
+    else:
+        per = 16 // x.element_size()
+        new[:, (torch.arange(V, device="cuda") // per) % 32 < 2] += 40
+    x.copy_(new)
+    for top in {1, min(V, 7), min(V, 32)}:
+        _, _, _, ids, _ = sn.sn_logprob_fwd(x, top=top)
+        # NaN first, then by value
+        key = torch.where(x.isnan(), math.inf, x.double() + 0.0)
+        assert torch.equal(ids.long(), torch.sort(key, dim=1, descending=True, stable=True).indices[:, :top])
+
+
+@pytest.mark.parametrize("dt", DT)
 @pytest.mark.parametrize("T,V,pad,opad,scale", [
     (1, 1, 0, 0, 1.0), (3, 7, 0, 0, 1.0), (9, 33, 2, 2, 0.5), (40, 1000, 0, 3, 1.0), (6, 50257, 0, 0, 1.25),
     (5, 50257, 7, 7, 1.0), (4, 8200, 8, 0, 2.0), (300, 257, 0, 0, 1.0)])
