@@ -38,6 +38,10 @@ constexpr int kThreads = 256;
 // 8 loads of 16 bytes a thread (bf16 chunks of half as much: 524 us for 3.5 GB, now 469)
 constexpr int kChunkBytes = 32768;
 constexpr int kPerSm = 8;
+// Clipping, blocks an SM of a list with kMany chunks an SM or more: 3.5 GB of bf16 take 1000 us,
+// 1024 with 8 (fewer rounds of the same blocks write in step).  Below that the blocks would not
+// have the same number of chunks (0.34 GB: 108 us with 8, 115 with 32).
+constexpr int kPerSmMany = 32, kMany = 128;
 enum { SRC_BF16 = 1, DST_BF16 = 2, ALIGNED = 4, IN_PLACE = 8 };
 
 // Squares below 2^-126 lose bits and above 2^128 overflow: a thread whose fp32 sum lies
@@ -165,7 +169,7 @@ __device__ __forceinline__ void scale_chunk(const sn_grad_chunk &c, float f)
     D *dst = (D *)c.dst;
     int done = 0;
     if (c.flags & ALIGNED) {
-        constexpr int N = 8, U = 4;                       // 8 elements a step, either type
+        constexpr int N = 8, U = sizeof(S) == 2 ? 4 : 2;  // 8 elements, 64 bytes of loads in flight
         const int nv = c.n / N;
         for (int i = threadIdx.x; i < nv; i += U * kThreads) {
             uint4 v[U][N / Vec<S>::N];
@@ -197,7 +201,9 @@ __device__ __forceinline__ void scale_chunk(const sn_grad_chunk &c, float f)
         dst[i] = Vec<D>::round(Vec<S>::one(src[i]) * f);
 }
 
-__global__ void __launch_bounds__(kThreads) k_clip(const sn_grad_chunk *__restrict__ table,
+// Three blocks an SM: 64 bytes of loads a thread in flight for either type fit 78 registers (two
+// blocks of 123 registers: 3.5 GB of bf16 1104 us).
+__global__ void __launch_bounds__(kThreads, 3) k_clip(const sn_grad_chunk *__restrict__ table,
                                                     int64_t chunks, const double *sumsq, float max_norm,
                                                     float *norm_out)
 {
@@ -228,9 +234,9 @@ __global__ void __launch_bounds__(kThreads) k_clip(const sn_grad_chunk *__restri
     }
 }
 
-int grid_of(const sn_grads &g)
+int grid_of(const sn_grads &g, int per_sm)
 {
-    return (int)std::max<int64_t>(1, std::min<int64_t>(g.chunks, (int64_t)g.sms * kPerSm));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(g.chunks, (int64_t)g.sms * per_sm));
 }
 
 }  // namespace
@@ -299,15 +305,16 @@ int grads_device(const sn_grads *g) { return g->device; }
 cudaError_t grads_sumsq(const sn_grads &g, double *sumsq, bool accumulate, cudaStream_t s)
 {
     count_launch();
-    const cudaError_t e = launch_dependent(k_sumsq, dim3(grid_of(g)), dim3(kThreads), 0, s, g.table, g.chunks,
+    const cudaError_t e = launch_dependent(k_sumsq, dim3(grid_of(g, kPerSm)), dim3(kThreads), 0, s, g.table, g.chunks,
                                            g.partial, g.ticket, sumsq, (int)accumulate);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 cudaError_t grads_clip(const sn_grads &g, const double *sumsq, float max_norm, float *norm, cudaStream_t s)
 {
+    const int per_sm = g.chunks >= (int64_t)kMany * g.sms ? kPerSmMany : kPerSm;
     count_launch();
-    const cudaError_t e = launch_dependent(k_clip, dim3(grid_of(g)), dim3(kThreads), 0, s, g.table, g.chunks,
+    const cudaError_t e = launch_dependent(k_clip, dim3(grid_of(g, per_sm)), dim3(kThreads), 0, s, g.table, g.chunks,
                                            sumsq, max_norm, norm);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
