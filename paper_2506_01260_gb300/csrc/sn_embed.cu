@@ -447,7 +447,9 @@ __device__ __forceinline__ void write_part(float *dst, const float2 (&acc)[4])
     *(float4 *)(dst + 4) = make_float4(acc[2].x, acc[2].y, acc[3].x, acc[3].y);
 }
 
-// Blocks [0, windows * slices) sum; the others, 32 ids each, write the rows without tokens.
+// Blocks [0, windows * slices) sum; the others, 32 ids each, write the rows without tokens, a
+// warp a row.  A thread has 8 columns: narrow rows have smaller blocks, more of them an SM (27551
+// bf16 rows of 512 into 50257 ids: 28 us, 39 with 256 threads for either kind of block).
 // MODE 0 writes dE.  MODE 1 adds to it and loads the rows of dE that a batch of tokens ends in
 // with the batch's rows of G; MODE 2 loads them when it gets there, with more rows of G in
 // flight.
@@ -465,14 +467,14 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
         const uint32_t used = a.used[word];
         const int64_t v0 = word * 32;
         const int n = (int)min((int64_t)32, a.vocab - v0);
-        for (int i = 0; i < n; ++i)
+        for (int i = threadIdx.x / 32; i < n; i += blockDim.x / 32)
             if (!((used >> i) & 1u)) {
                 D *row = dE + (v0 + i) * a.d;
                 if (VEC)
-                    for (int j = threadIdx.x; j < a.d / Vec<D>::N; j += kThreads)
+                    for (int j = threadIdx.x % 32; j < a.d / Vec<D>::N; j += 32)
                         ((uint4 *)row)[j] = make_uint4(0, 0, 0, 0);
                 else
-                    for (int j = threadIdx.x; j < a.d; j += kThreads)
+                    for (int j = threadIdx.x % 32; j < a.d; j += 32)
                         row[j] = Vec<D>::round(0.f);
             }
         return;
@@ -486,7 +488,7 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
     // starts; a longer one leaves a part in every window.
     // ids from the place before the window to the one after the next, tokens of both
     __shared__ int all_ids[2 * kMaxWindow + 2], all_tokens[2 * kMaxWindow];
-    for (int k = threadIdx.x; k < 2 * a.window + 2; k += kThreads) {
+    for (int k = threadIdx.x; k < 2 * a.window + 2; k += blockDim.x) {
         const int p = p0 - 1 + k;
         all_ids[k] = p >= 0 && p < places ? a.sorted[p] : -1;
         if (k < 2 * a.window)
@@ -494,21 +496,25 @@ __global__ void __launch_bounds__(kThreads) k_sum_rows(const SumArgs a)
     }
     const int far_before = p0 > a.window ? a.sorted[p0 - a.window - 1] : -1;
     __syncthreads();
-    const int len = p1 - p0, i = threadIdx.x;
+    const int len = p1 - p0;
     const int head = all_ids[1], tail = all_ids[len], after = all_ids[len + 1];
     const bool going_on = all_ids[0] == head;
     // the head run, where the window before has it; the tail run's tokens of the next window
-    const int skip = __syncthreads_count(i < len && going_on && far_before != head && after != head &&
-                                         all_ids[1 + i] == head);
-    const int more = __syncthreads_count(i < a.window && after == tail && all_ids[len + 1 + a.window] != tail &&
-                                         !(going_on && tail == head) && all_ids[len + 1 + i] == tail);
+    int skip = 0, more = 0;
+    for (int i0 = 0; i0 < a.window; i0 += blockDim.x) {
+        const int i = i0 + threadIdx.x;
+        skip += __syncthreads_count(i < len && going_on && far_before != head && after != head &&
+                                    all_ids[1 + i] == head);
+        more += __syncthreads_count(i < a.window && after == tail && all_ids[len + 1 + a.window] != tail &&
+                                    !(going_on && tail == head) && all_ids[len + 1 + i] == tail);
+    }
     const int n = len + more - skip;
     if (n <= 0)
         return;
     const int *ids = all_ids + skip, *tokens = all_tokens + skip;
     const S *G = (const S *)a.G;
     constexpr int U = sizeof(S) == 2 && !ACC ? 8 : 4;         // rows in flight
-    for (int j = slice * kThreads + threadIdx.x; j < nv; j += a.slices * kThreads) {
+    for (int j = slice * blockDim.x + threadIdx.x; j < nv; j += a.slices * blockDim.x) {
         float2 acc[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -676,10 +682,11 @@ size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 Layout layout_of(int64_t T, int64_t vocab, int d)
 {
     Layout l;
-    // 8 to 128 places a window, so that small calls still fill the SMs
+    // 8 to 128 places a window, so that small calls still fill the SMs (with blocks of a warp for
+    // every 256 columns)
     const int64_t sms = device_sms();
     int64_t w = 8;
-    while (w < kMaxWindow && T / w * ((d + 2047) / 2048) > 8 * sms)
+    while (w < kMaxWindow && T / w * ((d + 255) / 256) > 64 * sms)
         w *= 2;
     l.window = (int)w;
     l.windows = (int)((T + w - 1) / w);
@@ -704,7 +711,8 @@ template <typename S, typename D, int MODE, bool VEC>
 cudaError_t sum_and_join(const SumArgs &a, cudaStream_t s)
 {
     const int64_t grid = (int64_t)a.windows * a.slices + (MODE == WRITE ? (a.vocab + 31) / 32 : 0);
-    cudaError_t e = grid > 0 ? launch(k_sum_rows<S, D, MODE, VEC>, grid, kThreads, 0, s, a) : cudaSuccess;
+    const int threads = std::min(kThreads, (a.dp / 8 + 31) / 32 * 32);      // 256: slices may be more than one
+    cudaError_t e = grid > 0 ? launch(k_sum_rows<S, D, MODE, VEC>, grid, threads, 0, s, a) : cudaSuccess;
     if (e == cudaSuccess && a.windows > 1)
         e = launch(k_join_rows<D, VEC>, (int64_t)(a.windows - 1 + kJoin - 1) / kJoin * ((a.d + 255) / 256), kThreads,
                    0, s, a);
