@@ -979,17 +979,56 @@ struct RowCoef {
     }
 };
 
+// 16 bytes from byte `from` (a multiple of 2, below 16) of lo and hi on
+__device__ __forceinline__ uint4 bytes_from(uint4 lo, uint4 hi, int from)
+{
+    uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i)
+        w[i] = from & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i)
+        w[i] = from & 4 ? w[i + 1] : w[i];
+    const int bits = (from & 2) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits),
+                      __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+
+// N elements from p on, in the row [begin, end): the two pieces that they lie in, or, where those
+// pass the row's ends, one by one
+template <typename T>
+__device__ __forceinline__ uint4 unaligned_piece(const T *p, const T *begin, const T *end)
+{
+    constexpr int N = Vec<T>::N;
+    const int from = (int)((uintptr_t)p & 15);
+    const T *lo = (const T *)((const char *)p - from);
+    if (from == 0)
+        return __ldcs((const uint4 *)p);
+    if (lo >= begin && lo + 2 * N <= end)
+        return bytes_from(__ldcs((const uint4 *)lo), __ldcs((const uint4 *)lo + 1), from);
+    float f[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        f[k] = Vec<T>::one(p[k]);
+    return Vec<T>::pack(f);
+}
+
 // LANES threads share a row's step: a block has one row's, or several narrow rows' (16384 rows of
-// 1024 bf16: 12 us, 33 with a block a row)
-template <typename T, int LANES>
-__global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArgs a)
+// 1024 bf16: 12 us, 33 with a block a row).  SHIFT: some rows of the logits lie otherwise to their
+// 16-byte boundaries than the gradient's.  Then the pieces are whole in the output for bf16 (8191
+// rows of 50257, 47 elements of padding: 386 us, 924 with elements written one by one), and in
+// the logits for fp32, with single writes (500 us, 700 the other way).
+template <typename T, int LANES, bool SHIFT>
+__global__ void __launch_bounds__(kBwdThreads, SHIFT && sizeof(T) == 2 ? 4 : 5) k_logprob_bwd(const LogpBwdArgs a)
 {
     griddep_start();
     constexpr int N = Vec<T>::N, U = kBwdPieces, kRows = kBwdThreads / LANES;
+    constexpr bool SINGLE = SHIFT && sizeof(T) == 4;
     const int seg = blockIdx.x, lane = threadIdx.x % LANES;
     for (int64_t t = (int64_t)blockIdx.y * kRows + threadIdx.x / LANES; t < a.T; t += (int64_t)gridDim.y * kRows) {
-        const RowView<T> row((const T *)a.x + t * a.ld, a.V);
+        const T *x = (const T *)a.x + t * a.ld;
         T *out = (T *)a.dx + t * a.ldd;
+        const RowView<T> row(SINGLE ? x : out, a.V);
         RowCoef q;
         const float2 lse = *(const float2 *)(a.lse + 2 * t);
         q.m = lse.x;
@@ -1002,7 +1041,6 @@ __global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArg
         const float b = a.dentropy ? a.dentropy[t] * a.scale : 0.f;
         q.k = -q.a - (a.dentropy ? b * a.entropy[t] : 0.f);
         q.b = b * kLn2;
-        const bool wide = (((uintptr_t)row.p ^ (uintptr_t)out) & 15) == 0;
         // marked to leave L2 first, coming and going: 8191 rows of 50257 took 275 us without, now
         // 253, 4096 of 128256 322, now 295; with either mark alone less was gained, or nothing
         uint4 v[U];
@@ -1010,7 +1048,8 @@ __global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArg
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (i0 + u * LANES < row.nv)
-                v[u] = __ldcs((const uint4 *)(row.p + row.head) + i0 + u * LANES);
+                v[u] = SHIFT && !SINGLE ? unaligned_piece(x + row.head + (i0 + u * LANES) * N, x, x + a.V)
+                             : __ldcs((const uint4 *)(x + row.head) + i0 + u * LANES);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u * LANES;
@@ -1019,11 +1058,11 @@ __global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArg
             const int c0 = row.head + i * N;
             float f[N];
             if (q.near_) {
-                float2 x[N / 2];
-                Words<T>::pairs(v[u], x);
+                float2 y[N / 2];
+                Words<T>::pairs(v[u], y);
 #pragma unroll
                 for (int k = 0; k < N / 2; ++k) {
-                    const float2 z = fma2(add2(x[k], both(-q.m)), both(q.c), both(-q.l2));
+                    const float2 z = fma2(add2(y[k], both(-q.m)), both(q.c), both(-q.l2));
                     const float2 g = mul2(make_float2(ex2(z.x), ex2(z.y)), fma2(both(-q.b), z, both(q.k)));
                     f[2 * k] = g.x;
                     f[2 * k + 1] = g.y;
@@ -1038,7 +1077,7 @@ __global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArg
 #pragma unroll
                 for (int k = 0; k < N; ++k)
                     f[k] += q.target - c0 == k ? q.a : 0.f;
-            if (wide) {
+            if (!SINGLE) {
                 __stcs((uint4 *)(out + c0), Vec<T>::pack(f));
             } else {
 #pragma unroll
@@ -1048,7 +1087,7 @@ __global__ void __launch_bounds__(kBwdThreads, 5) k_logprob_bwd(const LogpBwdArg
         }
         if (seg == 0 && lane < row.loose()) {
             const int c = row.loose_at(lane);
-            out[c] = Vec<T>::round(q.at(Vec<T>::one(row.p[c])) + (c == q.target ? q.a : 0.f));
+            out[c] = Vec<T>::round(q.at(Vec<T>::one(x[c])) + (c == q.target ? q.a : 0.f));
         }
     }
 }
@@ -1113,9 +1152,10 @@ cudaError_t fwd_type(const LogpArgs &a, cudaStream_t s)
 template <typename T, int LANES>
 cudaError_t bwd_launch(const LogpBwdArgs &a, cudaStream_t s)
 {
+    const bool same = (((uintptr_t)a.x ^ (uintptr_t)a.dx) & 15) == 0 && (a.ld - a.ldd) % Vec<T>::N == 0;
     constexpr int per = Vec<T>::N * kBwdPieces * LANES, kRows = kBwdThreads / LANES;
     count_launch();
-    const cudaError_t e = launch_dependent(k_logprob_bwd<T, LANES>,
+    const cudaError_t e = launch_dependent(same ? k_logprob_bwd<T, LANES, false> : k_logprob_bwd<T, LANES, true>,
                                            dim3((unsigned)((a.V + per - 1) / per),
                                                 (unsigned)std::min<int64_t>((a.T + kRows - 1) / kRows, 65535)),
                                            dim3(kBwdThreads), 0, s, a);

@@ -293,6 +293,14 @@ def test_gradient(sn, dt, T, V, pad, opad, scale, terms):
     assert torch.equal(sn.sn_logprob_bwd(place, lse, scale=scale, out=place, **lp, **en), out)
 
 
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("T,V,pad,opad", [(9, 5, 0, 1), (17, 40, 3, 0), (17, 300, 1, 8), (18, 1000, 5, 2), (9, 1030, 47, 0),
+                                          (10, 4099, 0, 3), (9, 50257, 47, 0)])
+def test_gradient_of_rows_that_lie_differently(sn, dt, T, V, pad, opad):
+    """Logits and gradient at every distance from their 16-byte boundaries, steps of 32 to 256 threads."""
+    test_gradient(sn, dt, T, V, pad, opad, 1.25, "both")
+
+
 def test_gradient_against_differences(sn):
     """Central differences of the forward in fp32, step 1/32 along a direction of unit elements: the
     third derivative's term (step^2 / 6) is below 1e-3 of the weights' sum, the forward's error
