@@ -184,16 +184,22 @@ __device__ __forceinline__ float max_of_lanes(const float (&v)[C], int lane, int
     return m;
 }
 
-// Threads of an SM that registers are kept low enough for.  Codes from bf16 rows want 110
-// registers at 4 pieces a lane: capped at 80 for 768 threads they spill (16384 rows of 4096: 95
-// us, 73 as it is).  Blocks of 512 are two an SM even where they spill (8192 rows of 16384
-// bf16: 163 us, 230 with one block).
-template <typename T, int S, int C, int FMT>
-constexpr int kResident = S > 512 ? S : S == 512 ? 1024 : C == 1 ? 1536 : C == 2 ? 1024
-                        : FMT < 0 || sizeof(T) == 4 ? 768 : 512;
+// Threads of an SM that registers are kept low enough for.  With a residual, codes from bf16 rows
+// want 110 registers at 4 pieces a lane: capped at 80 for 768 threads they spill (16384 rows of
+// 4096: 95 us, 73 as it is).  Blocks of 512 are two an SM even where they spill (8192 rows of
+// 16384 bf16: 163 us, 230 with one block).  Without a residual (RES) a thread has half the loads
+// in flight and fewer registers, so more threads pay: 16384 rows of 8192 bf16 take 85 us, 95 with
+// as many as with one, codes of 16384 rows of 4096 55 and 61.
+template <typename T, int S, int C, int FMT, bool RES>
+constexpr int kResident = S > 512    ? S
+                          : S == 512 ? 1024
+                          : C == 1   ? 1536
+                          : C == 2   ? (RES || FMT >= 0 ? 1024 : 1536)
+                          : RES      ? (FMT < 0 || sizeof(T) == 4 ? 768 : 512)
+                                     : (sizeof(T) == 4 ? 1280 : FMT < 0 ? 1024 : 768);
 
-template <typename T, int S, bool EXACT, int C, int FMT>
-__global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / Shape<S>::kThreads)
+template <typename T, int S, bool EXACT, int C, int FMT, bool RES>
+__global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT, RES> / Shape<S>::kThreads)
     k_rmsnorm(const NormArgs a)
 {
     griddep_start();
@@ -202,7 +208,7 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / 
     int turn = 0;
     const int G = Shape<S, EXACT>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
     const int nv = a.d / N;
-    const T *X = (const T *)a.X, *R = (const T *)a.R;
+    const T *X = (const T *)a.X, *R = RES ? (const T *)a.R : nullptr;
     T *H = (T *)a.H, *Y = (T *)a.Y;
     for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
         const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
@@ -213,10 +219,10 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / 
             const int j = lane + G * i;
             const bool in = live && j < nv;
             xv[i] = in ? *((const uint4 *)(X + t * a.ldx) + j) : make_uint4(0, 0, 0, 0);
-            rv[i] = in && R ? *((const uint4 *)(R + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+            rv[i] = RES && in ? *((const uint4 *)(R + t * a.d) + j) : make_uint4(0, 0, 0, 0);
         }
         if (FMT >= 0 && a.ahead > 0 && threadIdx.x < 2 && t0 + a.ahead + kRows <= a.T) {
-            const T *p = threadIdx.x == 0 ? X + (t0 + a.ahead) * a.ldx : R ? R + (t0 + a.ahead) * a.d : nullptr;
+            const T *p = threadIdx.x == 0 ? X + (t0 + a.ahead) * a.ldx : RES ? R + (t0 + a.ahead) * a.d : nullptr;
             if (p)
                 prefetch_l2(p, (uint32_t)(kRows * a.d * sizeof(T)));
         }
@@ -224,7 +230,7 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT> / 
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             unpack_pairs(xv[i], h[i]);
-            if (R) {
+            if (RES) {
                 float2 r[P];
                 unpack_pairs(rv[i], r);
 #pragma unroll
@@ -597,17 +603,23 @@ cudaError_t launch(K kernel, int64_t grid, int threads, const A &a, cudaStream_t
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <typename T, int S, bool EXACT, int C, int FMT>
-cudaError_t fwd_shape(NormArgs a, int lanes, cudaStream_t s)
+template <typename T, int S, bool EXACT, int C, int FMT, bool RES>
+cudaError_t fwd_rows(NormArgs a, int lanes, cudaStream_t s)
 {
     constexpr int kRows = Shape<S>::kRows;
     const int threads = S == 32 ? 256 : lanes;
     const int64_t blocks = (a.T + kRows - 1) / kRows;
     a.ahead = 0;
     if (FMT >= 0 && a.ldx == a.d && a.d * sizeof(T) >= 4096) {
-        a.ahead = resident<k_rmsnorm<T, S, EXACT, C, FMT>>(threads) * device_sms() * kRows;
+        a.ahead = resident<k_rmsnorm<T, S, EXACT, C, FMT, RES>>(threads) * device_sms() * kRows;
     }
-    return launch(k_rmsnorm<T, S, EXACT, C, FMT>, std::min<int64_t>(blocks, (int64_t)1 << 30), threads, a, s);
+    return launch(k_rmsnorm<T, S, EXACT, C, FMT, RES>, std::min<int64_t>(blocks, (int64_t)1 << 30), threads, a, s);
+}
+
+template <typename T, int S, bool EXACT, int C, int FMT>
+cudaError_t fwd_shape(const NormArgs &a, int lanes, cudaStream_t s)
+{
+    return a.R ? fwd_rows<T, S, EXACT, C, FMT, true>(a, lanes, s) : fwd_rows<T, S, EXACT, C, FMT, false>(a, lanes, s);
 }
 
 template <typename T, int FMT>
