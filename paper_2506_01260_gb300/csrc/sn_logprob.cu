@@ -1016,10 +1016,15 @@ __device__ __forceinline__ uint4 unaligned_piece(const T *p, const T *begin, con
 // LANES threads share a row's step: a block has one row's, or several narrow rows' (16384 rows of
 // 1024 bf16: 12 us, 33 with a block a row).  SHIFT: some rows of the logits lie otherwise to their
 // 16-byte boundaries than the gradient's.  Then the pieces are whole in the output for bf16 (8191
-// rows of 50257, 47 elements of padding: 386 us, 924 with elements written one by one), and in
-// the logits for fp32, with single writes (500 us, 700 the other way).
+// rows of 50257, 47 elements of padding: 309 us, 924 with elements written one by one), and in
+// the logits for fp32, with single writes (473 us, 700 the other way).
+//
+// A step is loads, a few instructions and stores, so what counts is how many are on an SM: at 32
+// registers, all 2048 threads (8191 rows of 50257 bf16: 234 us, 7.05 TB/s; 254 with 48 registers,
+// 366 with 72).  With several rows a block that spills (16384 rows of 1024: 20 us, 12 with 48).
 template <typename T, int LANES, bool SHIFT>
-__global__ void __launch_bounds__(kBwdThreads, SHIFT && sizeof(T) == 2 ? 4 : 5) k_logprob_bwd(const LogpBwdArgs a)
+__global__ void __launch_bounds__(kBwdThreads, LANES == kBwdThreads ? 8 : SHIFT && sizeof(T) == 2 ? 4 : 5)
+    k_logprob_bwd(const LogpBwdArgs a)
 {
     griddep_start();
     constexpr int N = Vec<T>::N, U = kBwdPieces, kRows = kBwdThreads / LANES;
@@ -1041,8 +1046,8 @@ __global__ void __launch_bounds__(kBwdThreads, SHIFT && sizeof(T) == 2 ? 4 : 5) 
         const float b = a.dentropy ? a.dentropy[t] * a.scale : 0.f;
         q.k = -q.a - (a.dentropy ? b * a.entropy[t] : 0.f);
         q.b = b * kLn2;
-        // marked to leave L2 first, coming and going: 8191 rows of 50257 took 275 us without, now
-        // 253, 4096 of 128256 322, now 295; with either mark alone less was gained, or nothing
+        // marked to leave L2 first, coming and going (with 48 registers: 8191 rows of 50257 took 275
+        // us without, 253 with, 4096 of 128256 322 and 295; either mark alone gained less, or nothing)
         uint4 v[U];
         const int i0 = seg * U * LANES + lane;
 #pragma unroll
