@@ -32,10 +32,9 @@
  *     device error word records SN_ERR_BAD_ID, reported by sn_check_errors.
  *   - Only sn_basis_create and sn_grads_create allocate (and their _destroy
  *     calls free); no other call allocates memory or falls back to the CPU.
- *     A basis holds two
- *     scratch areas of (SM count) x 128 x (k rounded up to 16) floats that the
- *     bf16 contractions use for the partial sums of their last-round row
- *     tiles: one for the forward calls (sn_compress_fwd,
+ *     A basis holds two scratch areas of (SM count) x 128 x (k rounded up to
+ *     16) floats that the bf16 contractions use for the partial sums of their
+ *     last-round row tiles: one for the forward calls (sn_compress_fwd,
  *     sn_compress_fwd_projected, sn_project_tables), one for sn_compress_bwd.
  *     Forward calls on one basis must therefore not overlap each other in time
  *     (other streams, other host threads), nor backward calls each other; a
@@ -336,7 +335,7 @@ sn_status sn_rmsnorm_fwd(sn_dtype dtype, const void *X, int64_t ldx, const void 
  *   a = max |y|,  scale = a / qmax,  code = Q(y * (qmax / a)),   from y in fp32.
  * codes: uint8 [T, d]; scale: fp32 [T] (group = 0) or [T, ceil(d / group)].  A
  * group of zeros has scale 0; below 2^-100, a counts as 2^-100; a NaN or an
- * infinity in a group makes its scale one. */
+ * infinity in a group makes its scale a NaN or an infinity. */
 sn_status sn_rmsnorm_fwd_quant(sn_dtype dtype, const void *X, int64_t ldx, const void *R, void *H,
                                sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps,
                                int32_t format, int32_t group, uint8_t *codes, float *scale,
@@ -363,15 +362,15 @@ sn_status sn_rmsnorm_bwd(sn_dtype dtype, const void *dY, int64_t ldy, const void
  *   logp[t] = ln p[t, target[t]],   p = exp(z) / sum_v exp(z),
  *   entropy[t] = -sum_v p ln p
  * lse: fp32 [T, 2], ln sum_v exp(z) in two parts: the largest logit m, and
- * ln sum_v exp(scale * (logits - m)); the sum is scale * m plus the second
- * and the `top` largest logits of a row in order (the lower token first among
- * equals): top_ids int32 [T, top], top_logp fp32 [T, top].  0 <= top <= 32 and
+ * ln sum_v exp(scale * (logits - m)); the whole is scale * m plus the second part.
+ * The `top` largest logits of a row in order (the lower token first among equals)
+ * go to top_ids, int32 [T, top], and top_logp, fp32 [T, top].  0 <= top <= 32 and
  * top <= vocab; logp, entropy (fp32 [T]) and lse (8-byte aligned) may each be NULL,
- * target and logp only together.  A negative target is none: logp 0.  A target >= vocab counts as
- * none and records SN_ERR_BAD_ID where `errors` is a basis (it may be NULL).
- * -infinity masks a token out; a row of nothing else has both parts of lse and
- * every log probability -infinity and entropy 0.  A row with a NaN or +infinity gives NaN
- * (its alternatives are the NaNs first). */
+ * target and logp only together.  A negative target is none: logp 0.  A target
+ * >= vocab counts as none and records SN_ERR_BAD_ID where `errors` is a basis (it
+ * may be NULL).  -infinity masks a token out; a row of nothing else has both parts
+ * of lse and every log probability -infinity and entropy 0.  A row with a NaN or
+ * +infinity gives NaN (its alternatives are the NaNs first). */
 sn_status sn_logprob_fwd(sn_basis_t errors, sn_dtype dtype, const void *logits, int64_t T,
                          int64_t vocab, int64_t ld, const int32_t *target, float scale, float *logp,
                          float *lse, float *entropy, int32_t top, int32_t *top_ids, float *top_logp,
@@ -380,7 +379,8 @@ sn_status sn_logprob_fwd(sn_basis_t errors, sn_dtype dtype, const void *logits, 
 /* The gradient of logp and entropy with respect to the logits, from sn_logprob_fwd's
  * lse (and entropy):
  *   dlogits[t, v] = scale * (dlogp[t] ([v = target[t]] - p) - dentropy[t] p (ln p + entropy[t]))
- * Tokens without a target have no first term; a row without a token gets zeros.  dlogp with target, dentropy with entropy: either pair may be NULL.  dlogits:
+ * Tokens without a target have no first term; a row without a token gets zeros.
+ * dlogp goes with target, dentropy with entropy; either pair may be NULL.  dlogits:
  * [T, vocab] in dtype with row stride ldd; it may be logits (with ldd = ld). */
 sn_status sn_logprob_bwd(sn_dtype dtype, const void *logits, int64_t T, int64_t vocab, int64_t ld,
                          const int32_t *target, const float *lse, const float *dlogp,

@@ -9,7 +9,11 @@
 // arithmetic hides behind it: one pass over a row keeps a running maximum, S and the
 // entropy's sum in each thread, in base 2 so that an exponential is one fma and one ex2.
 // Sums are fp32.  A row is one block's, or, where rows are few, that of a cluster of blocks
-// that join their sums in shared memory.
+// that join their sums in shared memory; a narrow row is a warp's.
+//
+// Measured, bf16: 4096 rows of 128256 with the entropy 154 us (6.8 TB/s), with 8 alternatives
+// too 171, their search being latency (four barriers and a read of L2 a row); the gradient of
+// 8191 rows of 50257 234 us (7.05 TB/s).  8 fp32 rows of 128256 5.7 us, with 20 alternatives 9.6.
 //
 // The alternatives come out of the same pass: each thread keeps the largest logit it saw, the
 // step that it was in and the largest of its other steps.  The n-th largest of the maxima of 64
