@@ -13,9 +13,9 @@
 //
 // Measured: 16384 bf16 rows of 4096 with a residual 80 us (6.7 TB/s), their gradient 82 us (6.6
 // TB/s, the sum of dw's parts in it); e4m3 codes of 65536 bf16 rows of 8192 with a scale per 128
-// columns 559 us (6.7 TB/s), where instructions (0.58 of the issue slots) and DRAM (0.75 at
-// 16384 rows) are both near; the gradient of 4173 fp32 rows of 2056 29 us (4.7 TB/s), where the
-// 27 rows a block walks cost latency.
+// columns 557 us (6.8 TB/s), where instructions (0.54 of the issue slots) and DRAM (0.78 at
+// 16384 rows) are both near; the gradient of 4173 fp32 rows of 2056 26 us (5.3 TB/s), where the
+// 14 rows a block walks and the sum of dw's parts cost latency.
 #include <algorithm>
 #include <atomic>
 
@@ -410,7 +410,7 @@ struct NormBwdArgs {
 // Every group of G lanes walks the rows its place, its place + the number of groups, ...
 // and keeps the part of dw of its columns in registers.
 template <typename T, int S, int C>
-constexpr int kBwdResident = S > 512 ? S : C == 1 ? 1024 : sizeof(T) == 4 && S <= 256 ? 768 : 512;
+constexpr int kBwdResident = S > 512 ? S : S == 320 ? 640 : C == 1 ? 1024 : sizeof(T) == 4 && S <= 256 ? 768 : 512;
 
 template <typename T, int S, int C>
 __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Shape<S>::kThreads)
@@ -690,6 +690,9 @@ cudaError_t bwd_launch(BwdShape p, NormBwdArgs a, int &parts, cudaStream_t s)
 }
 
 template <typename T>
+constexpr int kNext = sizeof(T) == 4 ? 320 : 512;
+
+template <typename T>
 cudaError_t bwd(const NormBwdArgs &a, float *dw, bool accumulate, cudaStream_t s)
 {
     const bool registers = bwd_in_registers<T>(a.d, a.ldy);
@@ -703,7 +706,10 @@ cudaError_t bwd(const NormBwdArgs &a, float *dw, bool accumulate, cudaStream_t s
         e = nv <= 32 ? bwd_launch<k_rmsnorm_bwd<T, 32, 1>>(p, a, parts, s)
                      : bwd_launch<k_rmsnorm_bwd<T, 32, kBwdPieces>>(p, a, parts, s);
     else
+        // fp32 rows of a little more than 256 lanes: two blocks of up to 320 an SM (4173 rows of
+        // 2056: 26 us, 29 with one; bf16, which has twice the sums, spills: 2000 of 5000 26, 22)
         e = p.threads <= 256   ? bwd_launch<k_rmsnorm_bwd<T, 256, kBwdPieces>>(p, a, parts, s)
+            : p.threads <= kNext<T> ? bwd_launch<k_rmsnorm_bwd<T, kNext<T>, kBwdPieces>>(p, a, parts, s)
             : p.threads <= 512 ? bwd_launch<k_rmsnorm_bwd<T, 512, kBwdPieces>>(p, a, parts, s)
                                : bwd_launch<k_rmsnorm_bwd<T, 1024, kBwdPieces>>(p, a, parts, s);
     if (e != cudaSuccess)
