@@ -11,10 +11,9 @@
 // piece until it is written (`Shape` below gives the lanes of a width).  Sums are
 // fp32 in every type; y is computed from the unrounded h and rounded once, the stored h once.
 //
-// Measured: 16384 bf16 rows of 4096 with a residual 80 us (6.7 TB/s), their gradient 82 us (6.6
+// Measured: 16384 bf16 rows of 4096 with a residual 79 us (6.8 TB/s), their gradient 82 us (6.6
 // TB/s, the sum of dw's parts in it); e4m3 codes of 65536 bf16 rows of 8192 with a scale per 128
-// columns 557 us (6.8 TB/s), where instructions (0.54 of the issue slots) and DRAM (0.78 at
-// 16384 rows) are both near; the gradient of 4173 fp32 rows of 2056 26 us (5.3 TB/s), where the
+// columns 519 us (7.2 TB/s); the gradient of 4173 fp32 rows of 2056 26 us (5.3 TB/s), where the
 // 14 rows a block walks and the sum of dw's parts cost latency.
 #include <algorithm>
 #include <atomic>
@@ -30,7 +29,9 @@ namespace {
 // l + G, ... (at most C).  Narrow rows are a warp's each (S = 32: a block of 256 threads takes
 // eight), wider ones a block's of G <= S threads, G a multiple of 32, so that no width leaves
 // more than a few lanes without work.
-// EXACT: G is S, and the indices are constants (codes of 16384 rows of 4096: 73 us, 80 without).
+// EXACT: G is S, and every lane has all its pieces: no bounds, and indices that are constants
+// (codes of 65536 rows of 8192: 521 us, 557 with bounds; without a residual 16384 rows of 4096 42
+// and 55).
 template <int S, bool EXACT = false>
 struct Shape {
     static constexpr int kThreads = S == 32 ? 256 : S;      // at most
@@ -191,11 +192,11 @@ __device__ __forceinline__ float max_of_lanes(const float (&v)[C], int lane, int
 }
 
 // Threads of an SM that registers are kept low enough for.  With a residual, codes from bf16 rows
-// want 110 registers at 4 pieces a lane: capped at 80 for 768 threads they spill (16384 rows of
-// 4096: 95 us, 73 as it is).  Blocks of 512 are two an SM even where they spill (8192 rows of
+// want 110 registers at 4 pieces a lane: capped at 80 for 768 threads they spilled (16384 rows of
+// 4096 with bounds: 95 us, 73 without the cap).  Blocks of 512 are two an SM even where they spill (8192 rows of
 // 16384 bf16: 163 us, 230 with one block).  Without a residual (RES) a thread has half the loads
 // in flight and fewer registers, so more threads pay: 16384 rows of 8192 bf16 take 85 us, 95 with
-// as many as with one, codes of 16384 rows of 4096 55 and 61.
+// as many as with one.
 template <typename T, int S, int C, int FMT, bool RES>
 constexpr int kResident = S > 512    ? S
                           : S == 512 ? 1024
@@ -213,12 +214,12 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT, RE
     __shared__ __align__(16) float red[2 * 32];
     int turn = 0;
     const int G = Shape<S, EXACT>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
-    const int nv = a.d / N;
+    const int nv = EXACT ? S * C : a.d / N;
     const T *X = (const T *)a.X, *R = RES ? (const T *)a.R : nullptr;
     T *H = (T *)a.H, *Y = (T *)a.Y;
     for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
         const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
-        const bool live = t < a.T;
+        const bool live = S != 32 || t < a.T;
         uint4 xv[C], rv[C];
 #pragma unroll
         for (int i = 0; i < C; ++i) {
@@ -635,16 +636,18 @@ cudaError_t fwd(const NormArgs &a, cudaStream_t s)
         return launch(k_rmsnorm_any<T, FMT>, std::min<int64_t>(a.T, (int64_t)1 << 30), kAnyThreads, a, s);
     const int nv = a.d / Vec<T>::N, g = lanes_of(nv, kPieces);
     if (g == 32)
-        return nv <= 32   ? fwd_shape<T, 32, true, 1, FMT>(a, g, s)
-               : nv <= 64 ? fwd_shape<T, 32, true, 2, FMT>(a, g, s)
-                          : fwd_shape<T, 32, true, kPieces, FMT>(a, g, s);
-    if (g == 64)
+        return nv == 32             ? fwd_shape<T, 32, true, 1, FMT>(a, g, s)
+               : nv == 64           ? fwd_shape<T, 32, true, 2, FMT>(a, g, s)
+               : nv == 32 * kPieces ? fwd_shape<T, 32, true, kPieces, FMT>(a, g, s)
+               : nv < 64            ? fwd_shape<T, 32, false, 2, FMT>(a, g, s)
+                                    : fwd_shape<T, 32, false, kPieces, FMT>(a, g, s);
+    if (g == 64 && nv == 64 * kPieces)
         return fwd_shape<T, 64, true, kPieces, FMT>(a, g, s);
-    if (g == 128)
+    if (g == 128 && nv == 128 * kPieces)
         return fwd_shape<T, 128, true, kPieces, FMT>(a, g, s);
-    if (g == 256)
+    if (g == 256 && nv == 256 * kPieces)
         return fwd_shape<T, 256, true, kPieces, FMT>(a, g, s);
-    return g < 256    ? fwd_shape<T, 256, false, kPieces, FMT>(a, g, s)
+    return g <= 256   ? fwd_shape<T, 256, false, kPieces, FMT>(a, g, s)
            : g <= 512 ? fwd_shape<T, 512, false, kPieces, FMT>(a, g, s)
                       : fwd_shape<T, 1024, false, kPieces, FMT>(a, g, s);
 }
