@@ -223,10 +223,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a)
         auto look = [&](const int4 &v, int64_t t) {          // 4 tokens; which are the range's
             const int id[4] = {v.x, v.y, v.z, v.w};
             uint32_t h = 0;
+            if (range == 0)                                  // one block reports ids that are none
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    bad |= (uint32_t)id[k] >= (uint64_t)a.vocab && t + k < a.T;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 below += (uint32_t)id[k] < (uint32_t)lo;
-                bad |= (uint32_t)id[k] >= (uint64_t)a.vocab && t + k < a.T;
                 h |= ((uint32_t)id[k] - (uint32_t)lo < n_ids ? 1u : 0u) << k;
             }
             return h;
