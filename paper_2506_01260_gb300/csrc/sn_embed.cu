@@ -91,13 +91,15 @@ struct LookupArgs {
 // 2^lx lanes walk a row's pieces of 8 elements, two at a time; a block takes 256 >> lx rows.
 // Loads and stores are marked to leave L2 first (16384 rows of 4096 from 128256: 42.5 us, 46.5
 // without; 65536 rows of 2048 from 1024: 107, 122).  Blocks on an SM hide the chain id -> row:
-// eight for bf16 (27551 rows of 512: 10.5 us, 11.7 with six), six of 32 bytes of loads a thread
-// from fp32 tables (65536 rows of 1024: 76 us, 81 with five of 64 bytes).
-template <typename S, typename D>
-__global__ void __launch_bounds__(kThreads, sizeof(S) + sizeof(D) == 4 ? 8 : 6) k_lookup(const LookupArgs a, int lx)
+// eight for bf16 (27551 rows of 512: 10.5 us, 11.7 with six), from fp32 tables six of 32 bytes
+// of loads a thread (U = 1) for rows of one step (65536 rows of 1024: 76 us, 81 with five of 64
+// bytes) and five of 64 bytes for longer ones (65536 rows of 8192: 513 us, 534 the other way).
+template <typename S, typename D, int U>
+__global__ void __launch_bounds__(kThreads, sizeof(S) + sizeof(D) == 4 ? 8 : U == 1 ? 6 : 5)
+    k_lookup(const LookupArgs a, int lx)
 {
     griddep_start();
-    constexpr int N = 8, U = sizeof(S) == 2 ? 2 : 1;
+    constexpr int N = 8;
     const int lane = threadIdx.x & ((1 << lx) - 1), per = kThreads >> lx;
     const int nv = a.d / N;
     for (int64_t t = (int64_t)blockIdx.x * per + (threadIdx.x >> lx); t < a.T; t += (int64_t)gridDim.x * per) {
@@ -678,7 +680,9 @@ cudaError_t lookup(const LookupArgs &a, cudaStream_t s)
     while (lx < 8 && (1 << lx) < a.d / 8)
         ++lx;
     const int per = kThreads >> lx;
-    return launch(k_lookup<S, D>, std::min((a.T + per - 1) / per, most), kThreads, 0, s, a, lx);
+    const int64_t blocks = std::min((a.T + per - 1) / per, most);
+    return sizeof(S) == 4 && a.d / 8 <= kThreads ? launch(k_lookup<S, D, 1>, blocks, kThreads, 0, s, a, lx)
+                                                 : launch(k_lookup<S, D, 2>, blocks, kThreads, 0, s, a, lx);
 }
 
 // Where the sort's and the sums' buffers lie in the workspace
