@@ -2,9 +2,11 @@
 
 Argument marshalling only: each function checks tensor shapes and dtypes,
 passes raw pointers, sizes and the current CUDA stream to the C entry point of
-the same name, and raises SNError on a non-OK status.  Every step of the
-boundary runs in the library's kernels; torch supplies device memory, pinned
-host memory and streams.  There is no fallback: importing this module fails
+the same name, and raises SNError on a non-OK status.  A call that is given a
+stream makes its workspace and its results as that stream's memory; ordering
+what the caller gives, and keeping it until then, is the caller's.  Every step
+of the boundary runs in the library's kernels; torch supplies device memory,
+pinned host memory and streams.  There is no fallback: importing this module fails
 loudly when the library has not been built.
 """
 import ctypes
@@ -127,6 +129,41 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
+def _made(stream, device, make):
+    """make(): a tensor for a call on `stream`, its workspace or a result.  On another stream than
+    the current one it is made as that stream's memory: memory that the current stream's
+    allocations get may still be in use there, and a workspace dropped on return would be given
+    away while the call's kernels use it.  It is recorded as used on the current stream too, so
+    that a result dropped while that stream reads it is not given to the next call on `stream`."""
+    if stream is None or _stream(stream) == _raw_stream(device.index):
+        return make()
+    raw = _stream(stream)
+    raw = (raw.value or 0) if isinstance(raw, _P) else raw
+    if raw in (0, 1):                                    # the legacy default stream's handles
+        on = torch.cuda.default_stream(device)
+    else:
+        on = torch.cuda.ExternalStream(raw, device=device)
+    with torch.cuda.stream(on):
+        t = make()
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _empty(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return _made(stream, device, lambda: torch.empty(shape, dtype=dtype, device=device))
+
+
+def _empty_like(t, stream):
+    return _made(stream, t.device, lambda: torch.empty_like(t))
+
+
+def _bytes(n, device, stream):
+    """A workspace of n bytes."""
+    return _empty(n, torch.uint8, device, stream)
+
+
 def _dtype(t):
     if t.dtype == torch.bfloat16:
         return SN_BF16
@@ -227,7 +264,7 @@ def sn_compress_fwd(basis, X, ids, tok_emb, seq_len, pos_emb=None, pos=None, out
         raise ValueError("shape mismatch")
     _check_rows(T, seq_len, basis.d, pos_emb, pos)
     if out is None:
-        out = torch.empty(T, basis.k, dtype=X.dtype, device=X.device)
+        out = _empty((T, basis.k), X.dtype, X.device, stream)
     _need(out, "out", X.dtype)
     _check_out(out, (T, basis.k))
     _check(_lib.sn_compress_fwd(basis.handle, _dtype(X), _ptr(X), _ptr(ids), _ptr(pos), T,
@@ -243,7 +280,7 @@ def sn_project_tables(basis, tok_emb, pos_emb=None, TU=None, PU=None, stream=Non
     if tok_emb.shape != (V, basis.d):
         raise ValueError("shape mismatch")
     if TU is None:
-        TU = torch.empty(V, basis.k, dtype=torch.float32, device=tok_emb.device)
+        TU = _empty((V, basis.k), torch.float32, tok_emb.device, stream)
     _need(TU, "TU", torch.float32)
     _check_out(TU, (V, basis.k))
     n = 0
@@ -253,7 +290,7 @@ def sn_project_tables(basis, tok_emb, pos_emb=None, TU=None, PU=None, stream=Non
         if pos_emb.shape != (n, basis.d):
             raise ValueError("shape mismatch")
         if PU is None:
-            PU = torch.empty(n, basis.k, dtype=torch.float32, device=tok_emb.device)
+            PU = _empty((n, basis.k), torch.float32, tok_emb.device, stream)
         _need(PU, "PU", torch.float32)
         _check_out(PU, (n, basis.k))
     else:
@@ -278,7 +315,7 @@ def sn_compress_fwd_projected(basis, X, ids, TU, seq_len, PU=None, pos=None, out
         raise ValueError("shape mismatch")
     _check_rows(T, seq_len, basis.d, PU, pos, width=basis.k)
     if out is None:
-        out = torch.empty(T, basis.k, dtype=X.dtype, device=X.device)
+        out = _empty((T, basis.k), X.dtype, X.device, stream)
     _need(out, "out", X.dtype)
     _check_out(out, (T, basis.k))
     _check(_lib.sn_compress_fwd_projected(basis.handle, _dtype(X), _ptr(X), _ptr(ids), _ptr(pos),
@@ -294,12 +331,12 @@ def sn_build_ts(basis, tok_emb, out=None, workspace=None, stream=None):
     if tok_emb.shape != (V, basis.d):
         raise ValueError("shape mismatch")
     if out is None:
-        out = torch.empty_like(tok_emb)
+        out = _empty_like(tok_emb, stream)
     _need(out, "out", tok_emb.dtype)
     _check_out(out, (V, basis.d))
     nbytes = sn_wire_bytes(basis, tok_emb.dtype, V)
     if workspace is None:
-        workspace = torch.empty(max(16, nbytes), dtype=torch.uint8, device=tok_emb.device)
+        workspace = _bytes(max(16, nbytes), tok_emb.device, stream)
     _need(workspace, "workspace")
     _check(_lib.sn_build_ts(basis.handle, _dtype(tok_emb), _ptr(tok_emb), V, _ptr(out),
                             _ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -324,8 +361,7 @@ def sn_grassmann_accumulate(basis, G, Cg, M, workspace=None, stream=None):
     if G.shape != (T, basis.d) or Cg.shape != (T, basis.k) or M.shape != (basis.d, basis.k):
         raise ValueError("shape mismatch")
     if workspace is None:
-        workspace = torch.empty(max(256, sn_grassmann_workspace(basis, T)[0]), dtype=torch.uint8,
-                                device=G.device)
+        workspace = _bytes(max(256, sn_grassmann_workspace(basis, T)[0]), G.device, stream)
     _need(workspace, "workspace")
     _check(_lib.sn_grassmann_accumulate(basis.handle, SN_BF16, _ptr(G), _ptr(Cg), T, _ptr(M),
                                         _ptr(workspace),
@@ -354,12 +390,11 @@ def sn_grassmann_step(basis, M, K, eta, out=None, workspace=None, stream=None):
     if M.shape != (basis.d, basis.k):
         raise ValueError("shape mismatch")
     if out is None:
-        out = torch.empty_like(M)
+        out = _empty_like(M, stream)
     _need(out, "out", torch.float32)
     _check_out(out, (basis.d, basis.k))
     if workspace is None:
-        workspace = torch.empty(max(256, sn_grassmann_workspace(basis, 1)[1]), dtype=torch.uint8,
-                                device=M.device)
+        workspace = _bytes(max(256, sn_grassmann_workspace(basis, 1)[1]), M.device, stream)
     _need(workspace, "workspace")
     _check(_lib.sn_grassmann_step(basis.handle, _ptr(M), int(K), float(eta), _ptr(out),
                                   _ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -379,7 +414,7 @@ def sn_adamw_rowconst(W, grad, M, V, step, lr, beta1=0.9, beta2=0.999, eps=1e-8,
         raise ValueError("shape mismatch")
     rows, cols = W.shape
     if workspace is None:
-        workspace = torch.empty(cols, dtype=torch.float32, device=W.device)
+        workspace = _empty(cols, torch.float32, W.device, stream)
     _need(workspace, "workspace")
     _check(_lib.sn_adamw_rowconst(_dtype(grad), _ptr(W), _ptr(grad), _ptr(M), _ptr(V), rows, cols,
                                   int(step), float(lr), float(beta1), float(beta2), float(eps),
@@ -393,10 +428,9 @@ def sn_topk_compress(X, kk, values=None, cols=None, stream=None):
     """Per-row top-kk by magnitude of a bf16 batch: (values bf16 [T, kk], cols uint16-as-int16 [T, kk])."""
     _need(X, "X", torch.bfloat16)
     T, d = X.shape
-    vals = values if values is not None else torch.empty(T, kk, dtype=torch.bfloat16,
-                                                         device=X.device)
+    vals = values if values is not None else _empty((T, kk), torch.bfloat16, X.device, stream)
     if cols is None:
-        cols = torch.empty(T, kk, dtype=torch.int16, device=X.device)
+        cols = _empty((T, kk), torch.int16, X.device, stream)
     _need(vals, "values", torch.bfloat16)
     _need(cols, "cols", torch.int16)
     if vals.shape != (T, kk) or cols.shape != (T, kk):
@@ -413,7 +447,7 @@ def sn_topk_restore(vals, cols, d, out=None, stream=None):
     if cols.shape != vals.shape:
         raise ValueError("values and cols must have the same shape [T, kk]")
     if out is None:
-        out = torch.empty(T, d, dtype=torch.bfloat16, device=vals.device)
+        out = _empty((T, d), torch.bfloat16, vals.device, stream)
     _need(out, "out", torch.bfloat16)
     _check_out(out, (T, d))
     _check(_lib.sn_topk_restore(_ptr(vals), _ptr(cols), T, d, kk, _ptr(out), _stream(stream)),
@@ -426,9 +460,9 @@ def sn_sign_compress(X, bits=None, scale=None, stream=None):
     _need(X, "X", torch.bfloat16)
     T, d = X.shape
     if bits is None:
-        bits = torch.empty(T, (d + 31) // 32, dtype=torch.int32, device=X.device)
+        bits = _empty((T, (d + 31) // 32), torch.int32, X.device, stream)
     if scale is None:
-        scale = torch.empty(T, dtype=torch.float32, device=X.device)
+        scale = _empty(T, torch.float32, X.device, stream)
     _need(bits, "bits", torch.int32)
     _need(scale, "scale", torch.float32)
     if bits.shape != (T, (d + 31) // 32) or scale.shape != (T,):
@@ -445,7 +479,7 @@ def sn_sign_restore(bits, scale, d, out=None, stream=None):
     if scale.dim() != 1 or bits.shape != (T, (d + 31) // 32):
         raise ValueError("bits must be [T, ceil(d/32)] and scale [T]")
     if out is None:
-        out = torch.empty(T, d, dtype=torch.bfloat16, device=scale.device)
+        out = _empty((T, d), torch.bfloat16, scale.device, stream)
     _need(out, "out", torch.bfloat16)
     _check_out(out, (T, d))
     _check(_lib.sn_sign_restore(_ptr(bits), _ptr(scale), T, d, _ptr(out), _stream(stream)),
@@ -463,9 +497,9 @@ def sn_quant_compress(X, fmt, codes=None, scale=None, stream=None):
     _need(X, "X", torch.bfloat16)
     T, d = X.shape
     if codes is None:
-        codes = torch.empty(T, d, dtype=torch.uint8, device=X.device)
+        codes = _empty((T, d), torch.uint8, X.device, stream)
     if scale is None:
-        scale = torch.empty(T, dtype=torch.float32, device=X.device)
+        scale = _empty(T, torch.float32, X.device, stream)
     _need(codes, "codes", torch.uint8)
     _need(scale, "scale", torch.float32)
     if codes.shape != (T, d) or scale.shape != (T,):
@@ -482,7 +516,7 @@ def sn_quant_restore(codes, scale, fmt, out=None, stream=None):
     if scale.shape != (T,):
         raise ValueError("scale must be [T]")
     if out is None:
-        out = torch.empty(T, d, dtype=torch.bfloat16, device=codes.device)
+        out = _empty((T, d), torch.bfloat16, codes.device, stream)
     _need(out, "out", torch.bfloat16)
     _check_out(out, (T, d))
     _check(_lib.sn_quant_restore(_ptr(codes), _ptr(scale), T, d, QUANT_FORMATS[fmt], _ptr(out),
@@ -527,7 +561,7 @@ def sn_embed_fwd(table, ids, scale=1.0, out=None, out_dtype=None, basis=None, st
     V, d = table.shape
     T = ids.shape[0]
     if out is None:
-        out = torch.empty((T, d), dtype=out_dtype or table.dtype, device=table.device)
+        out = _empty((T, d), out_dtype or table.dtype, table.device, stream)
     else:
         _given(out, "out", (T, d), out_dtype)
     _check(_lib.sn_embed_fwd(_error_basis(basis), _dtype(table), table.data_ptr(), V, d,
@@ -553,12 +587,12 @@ def sn_embed_bwd(G, ids, vocab, scale=1.0, out=None, out_dtype=None, accumulate=
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
-        out = torch.empty((vocab, d), dtype=out_dtype or G.dtype, device=G.device)
+        out = _empty((vocab, d), out_dtype or G.dtype, G.device, stream)
     else:
         _given(out, "out", (vocab, d), out_dtype)
     if workspace is None:
         nbytes = sn_embed_bwd_workspace(T, vocab, d)
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=G.device)
+        workspace = _bytes(nbytes, G.device, stream)
     else:
         _need(workspace, "workspace")
         nbytes = workspace.numel() * workspace.element_size()
@@ -569,14 +603,14 @@ def sn_embed_bwd(G, ids, vocab, scale=1.0, out=None, out_dtype=None, accumulate=
     return out
 
 
-def _norm_inputs(X, w, R, H):
+def _norm_inputs(X, w, R, H, stream):
     """Row stride of X and the tensor that h is stored in (None without a residual)."""
     ldx = _rows(X, "X")
     _given(w, "w", X.shape[1:], None)
     if R is not None:
         _given(R, "R", X.shape, X.dtype)
         if H is None:
-            return ldx, torch.empty_like(R)
+            return ldx, _empty_like(R, stream)
     if H is not None:
         _given(H, "H", X.shape, X.dtype)
     return ldx, H
@@ -585,10 +619,10 @@ def _norm_inputs(X, w, R, H):
 def sn_rmsnorm_fwd(X, w, eps, R=None, H=None, out=None, stream=None):
     """h = X + R, Y = h / sqrt(mean(h^2) + eps) * w; returns (Y, h), h = X without a residual.
     H may be R (the residual stream updated in place).  X may be a row-strided view."""
-    ldx, H = _norm_inputs(X, w, R, H)
+    ldx, H = _norm_inputs(X, w, R, H, stream)
     T, d = X.shape
     if out is None:
-        out = torch.empty((T, d), dtype=X.dtype, device=X.device)
+        out = _empty((T, d), X.dtype, X.device, stream)
     else:
         _given(out, "out", (T, d), X.dtype)
     _check(_lib.sn_rmsnorm_fwd(_dtype(X), X.data_ptr(), ldx, _ptr(R), _ptr(H), _dtype(w),
@@ -601,15 +635,15 @@ def sn_rmsnorm_fwd_quant(X, w, eps, fmt, R=None, H=None, group=0, codes=None, sc
                          stream=None):
     """The norm's output as 8-bit codes (uint8 [T, d]; fmt "int8" or "e4m3") and fp32 scales, one
     a row or one for every `group` (32, 64, 128) columns; returns (codes, scale, h)."""
-    ldx, H = _norm_inputs(X, w, R, H)
+    ldx, H = _norm_inputs(X, w, R, H, stream)
     T, d = X.shape
     shape = (T, -(-d // group)) if group else (T,)
     if codes is None:
-        codes = torch.empty((T, d), dtype=torch.uint8, device=X.device)
+        codes = _empty((T, d), torch.uint8, X.device, stream)
     else:
         _given(codes, "codes", (T, d), torch.uint8)
     if scale is None:
-        scale = torch.empty(shape, dtype=torch.float32, device=X.device)
+        scale = _empty(shape, torch.float32, X.device, stream)
     else:
         _given(scale, "scale", shape, torch.float32)
     _check(_lib.sn_rmsnorm_fwd_quant(_dtype(X), X.data_ptr(), ldx, _ptr(R), _ptr(H), _dtype(w),
@@ -637,18 +671,18 @@ def sn_rmsnorm_bwd(dY, H, w, eps, dH=None, out=None, dw=None, accumulate=False, 
     if dH is not None:
         _given(dH, "dH", (T, d), dY.dtype)
     if out is None:
-        out = torch.empty((T, d), dtype=dY.dtype, device=dY.device)
+        out = _empty((T, d), dY.dtype, dY.device, stream)
     else:
         _given(out, "out", (T, d), dY.dtype)
     if dw is None:
         if accumulate:
             raise ValueError("accumulate=True needs dw")
-        dw = torch.empty((d,), dtype=torch.float32, device=dY.device)
+        dw = _empty((d,), torch.float32, dY.device, stream)
     else:
         _given(dw, "dw", (d,), torch.float32)
     if workspace is None:
         nbytes = max(16, sn_rmsnorm_bwd_workspace(T, d))
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dY.device)
+        workspace = _bytes(nbytes, dY.device, stream)
     else:
         _need(workspace, "workspace")
         nbytes = workspace.numel() * workspace.element_size()
@@ -668,16 +702,16 @@ def sn_logprob_fwd(logits, target=None, scale=1.0, top=0, entropy=True, basis=No
     ld = _rows(logits, "logits")
     T, V = logits.shape
     dev = logits.device
-    lse = torch.empty((T, 2), dtype=torch.float32, device=dev)
+    lse = _empty((T, 2), torch.float32, dev, stream)
     logp = H = ids = alt = None
     if target is not None:
         _given(target, "target", (T,), torch.int32)
-        logp = torch.empty((T,), dtype=torch.float32, device=dev)
+        logp = _empty((T,), torch.float32, dev, stream)
     if entropy:
-        H = torch.empty((T,), dtype=torch.float32, device=dev)
+        H = _empty((T,), torch.float32, dev, stream)
     if top:
-        ids = torch.empty((T, top), dtype=torch.int32, device=dev)
-        alt = torch.empty((T, top), dtype=torch.float32, device=dev)
+        ids = _empty((T, top), torch.int32, dev, stream)
+        alt = _empty((T, top), torch.float32, dev, stream)
     _check(_lib.sn_logprob_fwd(_error_basis(basis), _dtype(logits), logits.data_ptr(), T, V, ld,
                                _ptr(target), scale, _ptr(logp), lse.data_ptr(), _ptr(H), top,
                                _ptr(ids), _ptr(alt), _stream_of(logits, stream)),
@@ -698,7 +732,7 @@ def sn_logprob_bwd(logits, lse, target=None, dlogp=None, scale=1.0, entropy=None
     if target is not None:
         _given(target, "target", (T,), torch.int32)
     if out is None:
-        out = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        out = _empty((T, V), logits.dtype, logits.device, stream)
         ldd = V
     else:
         ldd = _rows(out, "out", logits.dtype)
@@ -768,7 +802,7 @@ def sn_grads_sumsq(grads, out=None, accumulate=False, stream=None):
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
-        out = torch.empty((1,), dtype=torch.float64, device=grads.device)
+        out = _empty((1,), torch.float64, grads.device, stream)
     else:
         _need(out, "out", torch.float64)
         if out.numel() < 1:
@@ -783,7 +817,7 @@ def sn_grads_clip(grads, sumsq, max_norm, norm=None, stream=None):
     (device fp32 [1])."""
     _need(sumsq, "sumsq", torch.float64)
     if norm is None:
-        norm = torch.empty((1,), dtype=torch.float32, device=grads.device)
+        norm = _empty((1,), torch.float32, grads.device, stream)
     else:
         _need(norm, "norm", torch.float32)
     if sumsq.numel() < 1 or norm.numel() < 1:
@@ -808,7 +842,7 @@ def sn_decompress_fwd(basis, C, ids, tok_emb, seq_len, pos_emb=None, pos=None, o
         raise ValueError("shape mismatch")
     _check_rows(T, seq_len, basis.d, pos_emb, pos)
     if out is None:
-        out = torch.empty(T, basis.d, dtype=C.dtype, device=C.device)
+        out = _empty((T, basis.d), C.dtype, C.device, stream)
     _need(out, "out", C.dtype)
     _check_out(out, (T, basis.d))
     _check(_lib.sn_decompress_fwd(basis.handle, _dtype(C), _ptr(C), _ptr(ids), _ptr(pos), T,
@@ -824,7 +858,7 @@ def sn_compress_bwd(basis, G, out=None, stream=None):
     if G.shape != (T, basis.d):
         raise ValueError("shape mismatch")
     if out is None:
-        out = torch.empty(T, basis.k, dtype=G.dtype, device=G.device)
+        out = _empty((T, basis.k), G.dtype, G.device, stream)
     _need(out, "out", G.dtype)
     _check_out(out, (T, basis.k))
     _check(_lib.sn_compress_bwd(basis.handle, _dtype(G), _ptr(G), T, _ptr(out), _stream(stream)),
@@ -839,7 +873,7 @@ def sn_decompress_bwd(basis, C, out=None, stream=None):
     if C.shape != (T, basis.k):
         raise ValueError("shape mismatch")
     if out is None:
-        out = torch.empty(T, basis.d, dtype=C.dtype, device=C.device)
+        out = _empty((T, basis.d), C.dtype, C.device, stream)
     _need(out, "out", C.dtype)
     _check_out(out, (T, basis.d))
     _check(_lib.sn_decompress_bwd(basis.handle, _dtype(C), _ptr(C), T, _ptr(out),
@@ -864,13 +898,13 @@ def sn_project_weight(basis, W, out=None, workspace=None, stream=None):
     rows, cols = W.shape
     ld = W.stride(0)
     if out is None:
-        out = torch.empty_like(W)
+        out = _empty_like(W, stream)
     _need(out, "out", W.dtype, contiguous=False)
     if out.stride() != W.stride() or out.shape != W.shape:
         raise ValueError("out must have W's shape and strides")
     need = sn_project_weight_workspace(basis, W.dtype, cols)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=W.device)
+        workspace = _bytes(max(need, 16), W.device, stream)
     _need(workspace, "workspace")
     _check(_lib.sn_project_weight(basis.handle, _dtype(W), _ptr(W), rows, cols, ld, _ptr(out),
                                   _ptr(workspace), workspace.numel() * workspace.element_size(),
