@@ -358,7 +358,8 @@ sn_status sn_rmsnorm_bwd(sn_dtype dtype, const void *dY, int64_t ldy, const void
 
 /* ---- Log probabilities of given tokens ----------------------------------------------
  * The last stage's loss and a server's scores.  logits: [T, vocab] in dtype with
- * row stride ld (elements); z = scale * logits, scale > 0 (the inverse temperature).
+ * row stride ld (elements); z = scale * logits, 0 < scale < 2.35e38 (the inverse
+ * temperature).
  *   logp[t] = ln p[t, target[t]],   p = exp(z) / sum_v exp(z),
  *   entropy[t] = -sum_v p ln p
  * lse: fp32 [T, 2], ln sum_v exp(z) in two parts: the largest logit m, and

@@ -817,8 +817,9 @@ sn_status sn_rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H
 namespace {
 sn_status check_logits(sn_dtype dt, int64_t T, int64_t V, int64_t ld, float scale)
 {
+    // (the kernels' exponents are scale * log2(e) times a difference of logits)
     if (!is_dtype(dt) || T < 0 || T >= kMaxRows || V < 1 || V >= kMaxTokens || ld < V || ld >= kMaxRows ||
-        !(scale > 0.f) || !std::isfinite(scale))
+        !(scale > 0.f) || !std::isfinite(scale * 1.4426950408889634f))
         return SN_ERR_INVALID_ARG;
     return SN_OK;
 }

@@ -467,9 +467,10 @@ constexpr int kAhead = 64 * 1024;
 constexpr float kLow = -1e20f;
 constexpr uint32_t kLowPair = 0xE0AEE0AEu;       // bf16, twice
 
+__host__ __device__ __forceinline__ bool near_scale(float c) { return c > 1e-17f && c < 1e17f; }
 __device__ __forceinline__ bool near(float m, float c)
 {
-    return fabsf(m) < 1e19f && c > 1e-17f && rounded(m * c);
+    return fabsf(m) < 1e19f && near_scale(c) && rounded(m * c);
 }
 
 __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
@@ -966,6 +967,7 @@ struct LogpBwdArgs {
     const int32_t *target;
     const float *lse, *entropy, *dlogp, *dentropy;   // target with dlogp, entropy with dentropy
     float scale;
+    float most;                // |scale * dentropy| on the short path, at most; below 0: no short path
 };
 
 constexpr int kBwdThreads = 256, kBwdPieces = 4;
@@ -1045,11 +1047,12 @@ __global__ void __launch_bounds__(kBwdThreads, LANES == kBwdThreads ? 8 : SHIFT 
         q.l2 = lse.y * kLog2e;
         q.empty = lse.y == -INFINITY;
         q.target = a.dlogp ? a.target[t] : -1;
-        q.near_ = !q.empty && near(q.m, q.c);
         q.a = !q.empty && a.dlogp && q.target >= 0 && q.target < a.V ? a.dlogp[t] * a.scale : 0.f;
         const float b = a.dentropy ? a.dentropy[t] * a.scale : 0.f;
         q.k = -q.a - (a.dentropy ? b * a.entropy[t] : 0.f);
         q.b = b * kLn2;
+        // near() of m and c, and b t finite too (t is above -2 * 10^20 c)
+        q.near_ = !q.empty && fabsf(q.m) < 1e19f && rounded(q.m * q.c) && fabsf(b) <= a.most;
         // marked to leave L2 first, coming and going (with 48 registers: 8191 rows of 50257 took 275
         // us without, 253 with, 4096 of 128256 322 and 295; either mark alone gained less, or nothing)
         uint4 v[U];
@@ -1195,7 +1198,9 @@ cudaError_t logprob_bwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld
                         const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
                         float scale, void *dx, int64_t ldd, cudaStream_t s)
 {
-    const LogpBwdArgs a{x, dx, T, ld, ldd, V, target, lse, entropy, dlogp, dentropy, scale};
+    const float c = scale * kLog2e;
+    const LogpBwdArgs a{x, dx, T, ld, ldd, V, target, lse, entropy, dlogp, dentropy, scale,
+                        near_scale(c) ? 1e17f / c : -1.f};
     return dt == SN_BF16 ? bwd_type<__nv_bfloat16>(a, s) : bwd_type<float>(a, s);
 }
 
