@@ -129,34 +129,34 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
-def _made(stream, device, make):
-    """make(): a tensor for a call on `stream`, its workspace or a result.  On another stream than
-    the current one it is made as that stream's memory: memory that the current stream's
-    allocations get may still be in use there, and a workspace dropped on return would be given
-    away while the call's kernels use it.  It is recorded as used on the current stream too, so
-    that a result dropped while that stream reads it is not given to the next call on `stream`."""
+def _maker(stream, device):
+    """torch.empty for the tensors that a call on `stream` needs, its workspace and its results.
+    On another stream than the current one they are made as that stream's memory: memory that the
+    current stream's allocations get may still be in use there, and a workspace dropped on return
+    would be given away while the call's kernels use it.  They are recorded as used on the current
+    stream too, so that a result dropped while that stream reads it is not given to the next call
+    on `stream`."""
     if stream is None or _stream(stream) == _raw_stream(device.index):
-        return make()
+        return torch.empty
     raw = _stream(stream)
     raw = (raw.value or 0) if isinstance(raw, _P) else raw
     if raw in (0, 1):                                    # the legacy default stream's handles
         on = torch.cuda.default_stream(device)
     else:
         on = torch.cuda.ExternalStream(raw, device=device)
-    with torch.cuda.stream(on):
-        t = make()
-    t.record_stream(torch.cuda.current_stream(device))
-    return t
+
+    def made(*args, **kwargs):
+        with torch.cuda.stream(on):
+            t = torch.empty(*args, **kwargs)
+        t.record_stream(torch.cuda.current_stream(device))
+        return t
+    return made
 
 
 def _empty(shape, dtype, device, stream):
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    return _made(stream, device, lambda: torch.empty(shape, dtype=dtype, device=device))
-
-
-def _empty_like(t, stream):
-    return _made(stream, t.device, lambda: torch.empty_like(t))
+    return _maker(stream, device)(shape, dtype=dtype, device=device)
 
 
 def _bytes(n, device, stream):
@@ -331,7 +331,7 @@ def sn_build_ts(basis, tok_emb, out=None, workspace=None, stream=None):
     if tok_emb.shape != (V, basis.d):
         raise ValueError("shape mismatch")
     if out is None:
-        out = _empty_like(tok_emb, stream)
+        out = _empty((V, basis.d), tok_emb.dtype, tok_emb.device, stream)
     _need(out, "out", tok_emb.dtype)
     _check_out(out, (V, basis.d))
     nbytes = sn_wire_bytes(basis, tok_emb.dtype, V)
@@ -390,7 +390,7 @@ def sn_grassmann_step(basis, M, K, eta, out=None, workspace=None, stream=None):
     if M.shape != (basis.d, basis.k):
         raise ValueError("shape mismatch")
     if out is None:
-        out = _empty_like(M, stream)
+        out = _empty((basis.d, basis.k), torch.float32, M.device, stream)
     _need(out, "out", torch.float32)
     _check_out(out, (basis.d, basis.k))
     if workspace is None:
@@ -584,15 +584,16 @@ def sn_embed_bwd(G, ids, vocab, scale=1.0, out=None, out_dtype=None, accumulate=
     ldg = _rows(G, "G")
     T, d = G.shape
     _given(ids, "ids", (T,), torch.int32)
+    empty = torch.empty if stream is None else _maker(stream, G.device)
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
-        out = _empty((vocab, d), out_dtype or G.dtype, G.device, stream)
+        out = empty((vocab, d), dtype=out_dtype or G.dtype, device=G.device)
     else:
         _given(out, "out", (vocab, d), out_dtype)
     if workspace is None:
         nbytes = sn_embed_bwd_workspace(T, vocab, d)
-        workspace = _bytes(nbytes, G.device, stream)
+        workspace = empty(nbytes, dtype=torch.uint8, device=G.device)
     else:
         _need(workspace, "workspace")
         nbytes = workspace.numel() * workspace.element_size()
@@ -610,7 +611,7 @@ def _norm_inputs(X, w, R, H, stream):
     if R is not None:
         _given(R, "R", X.shape, X.dtype)
         if H is None:
-            return ldx, _empty_like(R, stream)
+            return ldx, _empty(R.shape, R.dtype, R.device, stream)
     if H is not None:
         _given(H, "H", X.shape, X.dtype)
     return ldx, H
@@ -638,12 +639,13 @@ def sn_rmsnorm_fwd_quant(X, w, eps, fmt, R=None, H=None, group=0, codes=None, sc
     ldx, H = _norm_inputs(X, w, R, H, stream)
     T, d = X.shape
     shape = (T, -(-d // group)) if group else (T,)
+    empty = torch.empty if stream is None else _maker(stream, X.device)
     if codes is None:
-        codes = _empty((T, d), torch.uint8, X.device, stream)
+        codes = empty((T, d), dtype=torch.uint8, device=X.device)
     else:
         _given(codes, "codes", (T, d), torch.uint8)
     if scale is None:
-        scale = _empty(shape, torch.float32, X.device, stream)
+        scale = empty(shape, dtype=torch.float32, device=X.device)
     else:
         _given(scale, "scale", shape, torch.float32)
     _check(_lib.sn_rmsnorm_fwd_quant(_dtype(X), X.data_ptr(), ldx, _ptr(R), _ptr(H), _dtype(w),
@@ -666,23 +668,24 @@ def sn_rmsnorm_bwd(dY, H, w, eps, dH=None, out=None, dw=None, accumulate=False, 
     reaches h along the residual stream; dw fp32 [d], added to with accumulate=True."""
     ldy = _rows(dY, "dY")
     T, d = dY.shape
+    empty = torch.empty if stream is None else _maker(stream, dY.device)
     _given(H, "H", (T, d), dY.dtype)
     _given(w, "w", (d,), None)
     if dH is not None:
         _given(dH, "dH", (T, d), dY.dtype)
     if out is None:
-        out = _empty((T, d), dY.dtype, dY.device, stream)
+        out = empty((T, d), dtype=dY.dtype, device=dY.device)
     else:
         _given(out, "out", (T, d), dY.dtype)
     if dw is None:
         if accumulate:
             raise ValueError("accumulate=True needs dw")
-        dw = _empty((d,), torch.float32, dY.device, stream)
+        dw = empty((d,), dtype=torch.float32, device=dY.device)
     else:
         _given(dw, "dw", (d,), torch.float32)
     if workspace is None:
         nbytes = max(16, sn_rmsnorm_bwd_workspace(T, d))
-        workspace = _bytes(nbytes, dY.device, stream)
+        workspace = empty(nbytes, dtype=torch.uint8, device=dY.device)
     else:
         _need(workspace, "workspace")
         nbytes = workspace.numel() * workspace.element_size()
@@ -702,16 +705,17 @@ def sn_logprob_fwd(logits, target=None, scale=1.0, top=0, entropy=True, basis=No
     ld = _rows(logits, "logits")
     T, V = logits.shape
     dev = logits.device
-    lse = _empty((T, 2), torch.float32, dev, stream)
+    empty = torch.empty if stream is None else _maker(stream, dev)
+    lse = empty((T, 2), dtype=torch.float32, device=dev)
     logp = H = ids = alt = None
     if target is not None:
         _given(target, "target", (T,), torch.int32)
-        logp = _empty((T,), torch.float32, dev, stream)
+        logp = empty((T,), dtype=torch.float32, device=dev)
     if entropy:
-        H = _empty((T,), torch.float32, dev, stream)
+        H = empty((T,), dtype=torch.float32, device=dev)
     if top:
-        ids = _empty((T, top), torch.int32, dev, stream)
-        alt = _empty((T, top), torch.float32, dev, stream)
+        ids = empty((T, top), dtype=torch.int32, device=dev)
+        alt = empty((T, top), dtype=torch.float32, device=dev)
     _check(_lib.sn_logprob_fwd(_error_basis(basis), _dtype(logits), logits.data_ptr(), T, V, ld,
                                _ptr(target), scale, _ptr(logp), lse.data_ptr(), _ptr(H), top,
                                _ptr(ids), _ptr(alt), _stream_of(logits, stream)),
@@ -898,7 +902,9 @@ def sn_project_weight(basis, W, out=None, workspace=None, stream=None):
     rows, cols = W.shape
     ld = W.stride(0)
     if out is None:
-        out = _empty_like(W, stream)
+        out = _empty((rows, cols), W.dtype, W.device, stream)
+        if rows == 1:                                    # a lone row's stride may be any
+            out = out.as_strided(W.shape, W.stride())
     _need(out, "out", W.dtype, contiguous=False)
     if out.stride() != W.stride() or out.shape != W.shape:
         raise ValueError("out must have W's shape and strides")
