@@ -324,8 +324,9 @@ sn_status sn_embed_bwd(sn_basis_t errors, sn_dtype dtype, const void *G, int64_t
  * may be NULL (h is not stored).  h is summed in fp32 and rounded once when it is
  * stored; y comes from the unrounded h and is rounded once.  H may be R, and where
  * ldx = d also X; Y may be X or R (where ldx = d).  Other overlaps are
- * SN_ERR_INVALID_ARG.  eps >= 0 and finite; 1 <= d <= 2^20.  A row with an
- * infinity or a NaN gives NaN. */
+ * SN_ERR_INVALID_ARG.  eps >= 0 and finite; 1 <= d <= 2^20.  Finite rows of any
+ * size are right, also where their squares pass fp32's range; a row whose h has an
+ * infinity or a NaN is NaN whole. */
 sn_status sn_rmsnorm_fwd(sn_dtype dtype, const void *X, int64_t ldx, const void *R, void *H,
                          sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps, void *Y,
                          sn_stream_t stream);
@@ -334,8 +335,8 @@ sn_status sn_rmsnorm_fwd(sn_dtype dtype, const void *X, int64_t ldx, const void 
  * group = 32, 64 or 128 for every `group` columns of it (the last may be fewer),
  *   a = max |y|,  scale = a / qmax,  code = Q(y * (qmax / a)),   from y in fp32.
  * codes: uint8 [T, d]; scale: fp32 [T] (group = 0) or [T, ceil(d / group)].  A
- * group of zeros has scale 0; below 2^-100, a counts as 2^-100; a NaN or an
- * infinity in a group makes its scale a NaN or an infinity. */
+ * group of zeros has scale 0; below 2^-100, a counts as 2^-100; where y has a NaN
+ * or an infinity the group's scale is a NaN or an infinity. */
 sn_status sn_rmsnorm_fwd_quant(sn_dtype dtype, const void *X, int64_t ldx, const void *R, void *H,
                                sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps,
                                int32_t format, int32_t group, uint8_t *codes, float *scale,
@@ -349,7 +350,8 @@ sn_status sn_rmsnorm_bwd_workspace(int64_t T, int32_t d, size_t *bytes);
  *   dx = (g - n mean(g n)) / sqrt(mean(h^2) + eps) + dH,   dw = sum_t dy n
  * dX is the gradient of x and of r alike.  dY: [T, d] with row stride ldy; dH:
  * the gradient that reaches h along the residual stream, or NULL; dw: fp32 [d],
- * added to with accumulate != 0.  dX may be dH, H, or (where ldy = d) dY.
+ * added to with accumulate != 0.  h of any size as above; the products g h and
+ * dy n and their sums have to fit fp32.  dX may be dH, H, or (where ldy = d) dY.
  * workspace: 16-byte aligned, at least sn_rmsnorm_bwd_workspace bytes. */
 sn_status sn_rmsnorm_bwd(sn_dtype dtype, const void *dY, int64_t ldy, const void *H, const void *dH,
                          sn_dtype w_dtype, const void *w, int64_t T, int32_t d, float eps, void *dX,

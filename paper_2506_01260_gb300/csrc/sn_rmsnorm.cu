@@ -13,10 +13,11 @@
 //
 // Measured: 16384 bf16 rows of 4096 with a residual 79 us (6.8 TB/s), their gradient 82 us (6.6
 // TB/s, the sum of dw's parts in it); e4m3 codes of 65536 bf16 rows of 8192 with a scale per 128
-// columns 519 us (7.2 TB/s); the gradient of 4173 fp32 rows of 2056 26 us (5.3 TB/s), where the
+// columns 522 us (7.2 TB/s); the gradient of 4173 fp32 rows of 2056 26 us (5.3 TB/s), where the
 // 14 rows a block walks and the sum of dw's parts cost latency.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include <cuda_fp8.h>
 
@@ -30,8 +31,8 @@ namespace {
 // eight), wider ones a block's of G <= S threads, G a multiple of 32, so that no width leaves
 // more than a few lanes without work.
 // EXACT: G is S, and every lane has all its pieces: no bounds, and indices that are constants
-// (codes of 65536 rows of 8192: 521 us, 557 with bounds; without a residual 16384 rows of 4096 42
-// and 55).
+// (codes of 65536 rows of 8192: 522 us, 569 with bounds; without a residual 16384 rows of 4096 41
+// and 44).
 template <int S, bool EXACT = false>
 struct Shape {
     static constexpr int kThreads = S == 32 ? 256 : S;      // at most
@@ -105,6 +106,7 @@ struct NormArgs {
     uint8_t *codes;
     float *scale;
     int group_log2;         // columns that share a scale: 2^group_log2; 0: the row
+    float least, most;      // of a row's sum of squares that is taken as it is
     int ahead;              // rows that are in flight on the GPU at once; 0: no prefetch
 };
 
@@ -147,6 +149,27 @@ __device__ __forceinline__ uint8_t code_of(float y, float rec)
 {
     return (uint8_t)codes_of<FMT>(make_float2(y, 0.f), both(0.f), rec);
 }
+
+// ---- rows whose squares leave fp32's range -----------------------------------------------
+// A sum of squares is taken as it is where its mean (with eps) is from kLeast on, so that what
+// squares below fp32's numbers lose is below 2^-49 of it, and where it did not overflow.  Other
+// rows are taken again as h f, f = 2^-80 or 2^100: a finite row's mean of squares, with eps f^2
+// beside it, is then a number, n is the same, and the reciprocal root is 1 / f of the row's.  A
+// mean that still is none comes from an infinity or a NaN, and the row is NaN.
+//
+// The kernels below keep that off the other rows' way, each as its registers allow: the test is two
+// comparisons with bounds that the host made, and what a scaled row takes is not kept beside what
+// the others do (kept, it spilled: the gradient of 65536 rows of 8192 bf16 took 837 us, 605 now).
+constexpr float kLeast = 0x1p-100f, kMost = 3.402823466e38f;
+
+float least_sum(int d, float eps) { return std::max(0.f, (kLeast - eps) * (float)d); }
+float most_sum(float eps) { return eps < 1e37f ? kMost / 2.f : 0.f; }
+
+template <typename A>
+__device__ __forceinline__ bool in_range(const A &a, float sum) { return sum >= a.least && sum <= a.most; }
+template <typename A>
+__device__ __forceinline__ float factor_of(const A &a, float sum) { return sum < a.least ? 0x1p100f : 0x1p-80f; }
+__device__ __forceinline__ float root_of(float mean) { return mean <= kMost ? rsqrtf(mean) : NAN; }
 
 // ---- forward, rows in registers ------------------------------------------------------------
 
@@ -191,16 +214,92 @@ __device__ __forceinline__ float max_of_lanes(const float (&v)[C], int lane, int
     return m;
 }
 
+// A row by single elements, from memory.  SCALED: as h f; otherwise f is 1, and where the sum of
+// squares is not in range nothing is written.  Returns that sum.
+template <typename T, int S, bool EXACT, int FMT, bool SCALED>
+__device__ float norm_singly(const NormArgs &a, int64_t t, float f, float *red, int &turn)
+{
+    const int d = a.d, G = Shape<S, EXACT>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
+    const T *x = (const T *)a.X + t * a.ldx;
+    const T *r = a.R ? (const T *)a.R + t * d : nullptr;
+    T *H = a.H ? (T *)a.H + t * d : nullptr;
+    auto h_at = [&](int j) { return Vec<T>::one(x[j]) + (r ? Vec<T>::one(r[j]) : 0.f); };
+    float s[1] = {0.f};
+#pragma unroll SCALED ? 1 : 4
+    for (int j = lane; j < d; j += G) {
+        const float h = SCALED ? h_at(j) * f : h_at(j);
+        s[0] = fmaf(h, h, s[0]);
+    }
+    row_reduce<S, 1, false, EXACT>(s, red, turn);
+    if (!SCALED && !in_range(a, s[0]))
+        return s[0];
+    const float mean = s[0] / (float)d + (SCALED ? a.eps * f * f : a.eps);
+    const float rs = SCALED ? root_of(mean) : rsqrtf(mean);
+    auto y_of = [&](float h, int j) { return (SCALED ? h * f : h) * rs * weight_at(a, j); };
+    constexpr int F = FMT < 0 ? 0 : FMT;
+    if (FMT < 0) {
+#pragma unroll SCALED ? 1 : 4
+        for (int j = lane; j < d; j += G) {
+            const float h = h_at(j);
+            if (H)
+                H[j] = Vec<T>::round(h);
+            ((T *)a.Y)[t * d + j] = Vec<T>::round(y_of(h, j));
+        }
+    } else if (a.group_log2 == 0) {
+        float m[1] = {0.f};
+#pragma unroll SCALED ? 1 : 4
+        for (int j = lane; j < d; j += G)
+            m[0] = max_nan(m[0], fabsf(y_of(h_at(j), j)));
+        row_reduce<S, 1, true, EXACT>(m, red, turn);
+        const float rec = reciprocal_of<F>(m[0]);
+        if (lane == 0)
+            a.scale[t] = scale_of<F>(m[0]);
+#pragma unroll SCALED ? 1 : 4
+        for (int j = lane; j < d; j += G) {
+            const float h = h_at(j);
+            a.codes[t * d + j] = code_of<F>(y_of(h, j), rec);
+            if (H)
+                H[j] = Vec<T>::round(h);
+        }
+    } else {
+        // a warp takes whole groups
+        const int group = 1 << a.group_log2, groups = (d + group - 1) / group;
+#pragma unroll SCALED ? 1 : 4
+        for (int g = lane / 32; g < groups; g += G / 32) {
+            const int j0 = g * group, j1 = min(d, j0 + group);
+            float m = 0.f;
+#pragma unroll SCALED ? 1 : 4
+            for (int j = j0 + lane % 32; j < j1; j += 32)
+                m = max_nan(m, fabsf(y_of(h_at(j), j)));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+                m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float rec = reciprocal_of<F>(m);
+            if (lane % 32 == 0)
+                a.scale[t * groups + g] = scale_of<F>(m);
+#pragma unroll SCALED ? 1 : 4
+            for (int j = j0 + lane % 32; j < j1; j += 32) {
+                const float h = h_at(j);
+                a.codes[t * d + j] = code_of<F>(y_of(h, j), rec);
+                if (H)
+                    H[j] = Vec<T>::round(h);
+            }
+        }
+    }
+    return s[0];
+}
+
 // Threads of an SM that registers are kept low enough for.  With a residual, codes from bf16 rows
-// want 110 registers at 4 pieces a lane: capped at 80 for 768 threads they spilled (16384 rows of
-// 4096 with bounds: 95 us, 73 without the cap).  Blocks of 512 are two an SM even where they spill (8192 rows of
-// 16384 bf16: 163 us, 230 with one block).  Without a residual (RES) a thread has half the loads
-// in flight and fewer registers, so more threads pay: 16384 rows of 8192 bf16 take 85 us, 95 with
-// as many as with one.
+// take up to 115 registers at 4 pieces a lane and are left them (at most 80, for 768 threads:
+// 16384 rows of 4096 with bounds 95 us, 73 without that cap).  Blocks of 512 are two an SM (8192
+// rows of 16384 bf16: 143 us, 230 with one block).  Without a residual (RES) a thread has half the
+// loads in flight and fewer registers, so more threads pay: 16384 rows of 8192 bf16 take 85 us, 95
+// with as many as with one.  Rows of one piece fit 32 registers, all of an SM's threads (65536 rows
+// of 256 bf16 with a residual: 21.2 us, 22.5 with 1536).
 template <typename T, int S, int C, int FMT, bool RES>
 constexpr int kResident = S > 512    ? S
                           : S == 512 ? 1024
-                          : C == 1   ? 1536
+                          : C == 1   ? (FMT < 0 ? 2048 : 1536)
                           : C == 2   ? (RES || FMT >= 0 ? 1024 : 1536)
                           : RES      ? (FMT < 0 || sizeof(T) == 4 ? 768 : 512)
                                      : (sizeof(T) == 4 ? 1280 : FMT < 0 ? 1024 : 768);
@@ -251,19 +350,60 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<T, S, C, FMT, RE
             if (H && live && j < nv)
                 *((uint4 *)(H + t * a.d) + j) = pack_pairs(h[i]);
         }
-        float s[1] = {sq.x + sq.y};
-        row_reduce<S, 1, false, EXACT>(s, red, turn);
-        const float rs = rsqrtf(s[0] / (float)a.d + a.eps);
+        // The weights are asked for before the row's sums meet where they fit beside h: codes
+        // without a residual (16384 rows of 4096, 128 columns a scale: 41.0 us, 44.4 behind the
+        // sums) and norms with one (65536 rows of 512: 40.4, 41.1).  Elsewhere they cost more than
+        // they hide: codes of 65536 rows of 8192 with a residual 545 us, 522 behind the sums,
+        // norms of 16384 rows of 8192 without one 107 and 85.
+        constexpr bool kWeights = EXACT && (FMT < 0 ? RES && C > 1 : !RES && S > 32);
+        float wv[kWeights ? C : 1][N];
+        if (kWeights)
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                load_weight(a, (lane + G * i) * N, wv[kWeights ? i : 0]);
+        float s[1] = {sq.x + sq.y}, eps = a.eps;
+        const auto scale_row = [&] {
+            const float f = factor_of(a, s[0]);
+            sq = both(0.f);
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    h[i][k] = mul2(h[i][k], both(f));
+                    sq = fma2(h[i][k], h[i][k], sq);
+                }
+            s[0] = sq.x + sq.y;
+            eps = eps * f * f;
+        };
+        // A loop of two turns at most, the second for a row out of range; written out for one piece
+        // a lane (65536 rows of 256 bf16: 21.2 us, 22.7 as a loop), more pieces spill so.
+        if (FMT < 0 && C == 1) {
+            row_reduce<S, 1, false, EXACT>(s, red, turn);
+            if (!in_range(a, s[0])) {                // (every lane of the row)
+                scale_row();
+                row_reduce<S, 1, false, EXACT>(s, red, turn);
+            }
+        } else {
+#pragma unroll 1
+            for (bool scaled = false;; scaled = true) {
+                row_reduce<S, 1, false, EXACT>(s, red, turn);
+                if (scaled || in_range(a, s[0]))
+                    break;
+                scale_row();
+            }
+        }
+        const float rs = root_of(s[0] / (float)a.d + eps);
         float m[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
             if (j < nv) {
-                float wv[N];
-                load_weight(a, j * N, wv);
+                float (&w)[N] = wv[kWeights ? i : 0];
+                if (!kWeights)
+                    load_weight(a, j * N, w);
 #pragma unroll
                 for (int k = 0; k < P; ++k)
-                    h[i][k] = mul2(mul2(h[i][k], both(rs)), make_float2(wv[2 * k], wv[2 * k + 1]));
+                    h[i][k] = mul2(mul2(h[i][k], both(rs)), make_float2(w[2 * k], w[2 * k + 1]));
                 if (FMT < 0) {
                     if (live)
                         *((uint4 *)(Y + t * a.d) + j) = pack_pairs(h[i]);
@@ -332,65 +472,10 @@ __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_any(const NormArgs a)
     griddep_start();
     __shared__ __align__(16) float red[2 * 32];
     int turn = 0;
-    const T *X = (const T *)a.X, *R = (const T *)a.R;
-    T *H = (T *)a.H, *Y = (T *)a.Y;
-    const int d = a.d;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const T *x = X + t * a.ldx;
-        const T *r = R ? R + t * d : nullptr;
-        auto h_at = [&](int j) { return Vec<T>::one(x[j]) + (r ? Vec<T>::one(r[j]) : 0.f); };
-        float s[1] = {0.f};
-        for (int j = threadIdx.x; j < d; j += kAnyThreads) {
-            const float h = h_at(j);
-            s[0] = fmaf(h, h, s[0]);
-        }
-        row_reduce<kAnyThreads, 1, false>(s, red, turn);
-        const float rs = rsqrtf(s[0] / (float)d + a.eps);
-        auto y_at = [&](int j) { return h_at(j) * rs * weight_at(a, j); };
-        constexpr int F = FMT < 0 ? 0 : FMT;
-        if (FMT < 0) {
-            for (int j = threadIdx.x; j < d; j += kAnyThreads) {
-                const float h = h_at(j);
-                if (H)
-                    H[t * d + j] = Vec<T>::round(h);
-                Y[t * d + j] = Vec<T>::round(h * rs * weight_at(a, j));
-            }
-        } else if (a.group_log2 == 0) {
-            float m[1] = {0.f};
-            for (int j = threadIdx.x; j < d; j += kAnyThreads)
-                m[0] = max_nan(m[0], fabsf(y_at(j)));
-            row_reduce<kAnyThreads, 1, true>(m, red, turn);
-            const float rec = reciprocal_of<F>(m[0]);
-            if (threadIdx.x == 0)
-                a.scale[t] = scale_of<F>(m[0]);
-            for (int j = threadIdx.x; j < d; j += kAnyThreads) {
-                const float h = h_at(j);
-                a.codes[t * d + j] = code_of<F>(h * rs * weight_at(a, j), rec);
-                if (H)
-                    H[t * d + j] = Vec<T>::round(h);
-            }
-        } else {
-            // a warp takes whole groups
-            const int group = 1 << a.group_log2, groups = (d + group - 1) / group;
-            for (int g = threadIdx.x / 32; g < groups; g += kAnyThreads / 32) {
-                const int j0 = g * group, j1 = min(d, j0 + group);
-                float m = 0.f;
-                for (int j = j0 + threadIdx.x % 32; j < j1; j += 32)
-                    m = max_nan(m, fabsf(y_at(j)));
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1)
-                    m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-                const float rec = reciprocal_of<F>(m);
-                if (threadIdx.x % 32 == 0)
-                    a.scale[t * groups + g] = scale_of<F>(m);
-                for (int j = j0 + threadIdx.x % 32; j < j1; j += 32) {
-                    const float h = h_at(j);
-                    a.codes[t * d + j] = code_of<F>(h * rs * weight_at(a, j), rec);
-                    if (H)
-                        H[t * d + j] = Vec<T>::round(h);
-                }
-            }
-        }
+        const float sum = norm_singly<T, kAnyThreads, true, FMT, false>(a, t, 1.f, red, turn);
+        if (!in_range(a, sum))
+            norm_singly<T, kAnyThreads, true, FMT, true>(a, t, factor_of(a, sum), red, turn);
     }
 }
 
@@ -404,14 +489,52 @@ struct NormBwdArgs {
     int d;
     float eps;
     void *dX;
+    float least, most;          // of a row's sum of squares that is taken as it is
     float *part;                // [lanes of rows, d] partial sums of dw
     bool prefetch;
 };
 
+// A row of the gradient by single elements, from memory, M neighbouring ones a thread; its part of
+// dw is added to what `part` has.  SCALED and the result as in norm_singly.
+template <typename T, int S, int M, bool SCALED>
+__device__ float norm_bwd_singly(const NormBwdArgs &a, int64_t t, float f, float *part, float *red, int &turn)
+{
+    const int d = a.d, G = Shape<S>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
+    const T *H = (const T *)a.H + t * d, *dY = (const T *)a.dY + t * a.ldy;
+    const T *dH = a.dH ? (const T *)a.dH + t * d : nullptr;
+    T *dX = (T *)a.dX + t * d;
+    auto h_at = [&](int j) { return SCALED ? Vec<T>::one(H[j]) * f : Vec<T>::one(H[j]); };
+    float s[2] = {0.f, 0.f};
+    for (int i = lane * M; i < d; i += G * M)
+        for (int j = i; j < i + M; ++j) {
+            const float h = h_at(j), y = Vec<T>::one(dY[j]);
+            s[0] = fmaf(h, h, s[0]);
+            s[1] = fmaf(y * weight_at(a, j), h, s[1]);
+        }
+    row_reduce<S, 2, false>(s, red, turn);
+    if (!SCALED && !in_range(a, s[0]))
+        return s[0];
+    const float mean = s[0] / (float)d + (SCALED ? a.eps * f * f : a.eps);
+    const float rs = SCALED ? root_of(mean) : rsqrtf(mean);
+    const float c = s[1] / (float)d * rs * rs;
+    for (int i = lane * M; i < d; i += G * M)
+        for (int j = i; j < i + M; ++j) {
+            const float h = h_at(j), y = Vec<T>::one(dY[j]);
+            const float r = dH ? Vec<T>::one(dH[j]) : 0.f, g = fmaf(-h, c, y * weight_at(a, j));
+            dX[j] = Vec<T>::round(SCALED ? fmaf(rs * g, f, r) : fmaf(rs, g, r));
+            part[j] = fmaf(y * h, rs, part[j]);
+        }
+    return s[0];
+}
+
 // Every group of G lanes walks the rows its place, its place + the number of groups, ...
-// and keeps the part of dw of its columns in registers.
+// and keeps the part of dw of its columns in registers.  Threads of an SM:
 template <typename T, int S, int C>
-constexpr int kBwdResident = S > 512 ? S : S == 320 ? 640 : C == 1 ? 1024 : sizeof(T) == 4 && S <= 256 ? 768 : 512;
+constexpr int kBwdResident = S > 512                        ? S
+                             : S == 320                     ? 640
+                             : C == 1                       ? (sizeof(T) == 4 ? 1024 : 768)
+                             : sizeof(T) == 4 && S <= 256 ? 768
+                                                            : 512;
 
 template <typename T, int S, int C>
 __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Shape<S>::kThreads)
@@ -425,16 +548,6 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
     const int nv = a.d / N;
     const T *dY = (const T *)a.dY, *H = (const T *)a.H, *dH = (const T *)a.dH;
     T *dX = (T *)a.dX;
-    float dw[C][N], wv[C][N];
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int j = lane + G * i;
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            dw[i][k] = wv[i][k] = 0.f;
-        if (j < nv)
-            load_weight(a, j * N, wv[i]);
-    }
     const int64_t stride = (int64_t)gridDim.x * kRows;
     auto load = [&](int64_t t, uint4 (&hv)[C], uint4 (&yv)[C], uint4 (&rv)[C]) {
 #pragma unroll
@@ -447,72 +560,130 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
         }
     };
     // The next row's loads run before this row's sums meet, where registers allow (65536 rows of
-    // 8192: 604 us, 632 without; 4173 rows of 2056 in fp32: 29.6, 35.1); rows of 4 KB and more
-    // are asked for into L2 before that.
-    constexpr bool kEarly = S <= 512 && C > 1;
-    uint4 hv[C], yv[C], rv[C], hn[C], yn[C], rn[C];
-    if (kEarly)
-        load((int64_t)blockIdx.x * kRows + (S == 32 ? threadIdx.x / 32 : 0), hn, yn, rn);
-    for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += stride) {
-        const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
-        const bool live = t < a.T;
-        if (kEarly) {
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                hv[i] = hn[i];
-                yv[i] = yn[i];
-                rv[i] = rn[i];
-            }
-            load(t + stride, hn, yn, rn);
-        } else {
-            load(t, hv, yv, rv);
-        }
-        const int64_t later = t0 + (kEarly ? 2 : 1) * stride;
-        if (a.prefetch && threadIdx.x < 3 && later + kRows <= a.T) {
-            const T *p = threadIdx.x == 0 ? H : threadIdx.x == 1 ? dY : dH;
-            if (p)
-                prefetch_l2(p + later * a.d, (uint32_t)(kRows * a.d * sizeof(T)));
-        }
-        float s[2] = {0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            float h[N], y[N];
-            Vec<T>::unpack(hv[i], h);
-            Vec<T>::unpack(yv[i], y);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                s[0] = fmaf(h[k], h[k], s[0]);
-                s[1] = fmaf(y[k] * wv[i][k], h[k], s[1]);
-            }
-        }
-        row_reduce<S, 2, false>(s, red, turn);
-        const float rs = rsqrtf(s[0] / (float)a.d + a.eps);
-        const float c = s[1] / (float)a.d * rs * rs;
+    // 8192: 604 us, 632 without; 4173 rows of 2056 in fp32: 29.6, 35.1; 65536 of 256 34.0, 36.2);
+    // rows of 4 KB and more are asked for into L2 before that.
+    constexpr bool kEarly = S <= 512;
+    // A row out of range: from the registers that hold it (a warp's rows of two pieces a lane: 65536
+    // rows of 256 fp32 49.3 us, 55.0 the other way), or behind the loop, which is then entered
+    // again, by single elements (65536 rows of 8192 bf16: 605 us, 744 from the registers).
+    constexpr bool kInside = S == 32 && C > 1;
+    const int warp = S == 32 ? threadIdx.x / 32 : 0;
+    float *part = a.part + ((int64_t)blockIdx.x * kRows + warp) * a.d;
+    int64_t t0 = (int64_t)blockIdx.x * kRows;
+    // (a warp's rows: each warp for itself)
+    for (bool first = true;; first = false) {
+        float dw[C][N], wv[C][N];
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
-            if (!(live && j < nv))
-                continue;
-            float h[N], y[N], x[N];
-            Vec<T>::unpack(hv[i], h);
-            Vec<T>::unpack(yv[i], y);
-            Vec<T>::unpack(rv[i], x);
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                x[k] = fmaf(rs, fmaf(-h[k], c, y[k] * wv[i][k]), x[k]);
-                dw[i][k] = fmaf(y[k] * h[k], rs, dw[i][k]);
-            }
-            *((uint4 *)(dX + t * a.d) + j) = Vec<T>::pack(x);
+            for (int k = 0; k < N; ++k)
+                dw[i][k] = wv[i][k] = 0.f;
+            if (j < nv)
+                load_weight(a, j * N, wv[i]);
         }
-    }
-    float *part = a.part + ((int64_t)blockIdx.x * kRows + (S == 32 ? threadIdx.x / 32 : 0)) * a.d;
+        uint4 hv[C], yv[C], rv[C], hn[C], yn[C], rn[C];
+        if (kEarly)
+            load(t0 + warp, hn, yn, rn);
+        float sum = 0.f;
+        for (; t0 < a.T; t0 += stride) {
+            const int64_t t = t0 + warp;
+            const bool live = t < a.T;
+            if (kEarly) {
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int j = lane + G * i;
-        if (j < nv)
+                for (int i = 0; i < C; ++i) {
+                    hv[i] = hn[i];
+                    yv[i] = yn[i];
+                    rv[i] = rn[i];
+                }
+                load(t + stride, hn, yn, rn);
+            } else {
+                load(t, hv, yv, rv);
+            }
+            const int64_t later = t0 + (kEarly ? 2 : 1) * stride;
+            if (a.prefetch && threadIdx.x < 3 && later + kRows <= a.T) {
+                const T *p = threadIdx.x == 0 ? H : threadIdx.x == 1 ? dY : dH;
+                if (p)
+                    prefetch_l2(p + later * a.d, (uint32_t)(kRows * a.d * sizeof(T)));
+            }
+            const auto forget = [&] {                // the compiler keeps nothing made from hv and yv
 #pragma unroll
-            for (int k = 0; k < N; k += 4)
-                *(float4 *)(part + j * N + k) = make_float4(dw[i][k], dw[i][k + 1], dw[i][k + 2], dw[i][k + 3]);
+                for (int i = 0; i < C; ++i) {
+                    asm volatile("" : "+r"(yv[i].x), "+r"(yv[i].y), "+r"(yv[i].z), "+r"(yv[i].w));
+                    asm volatile("" : "+r"(hv[i].x), "+r"(hv[i].y), "+r"(hv[i].z), "+r"(hv[i].w));
+                }
+            };
+            float s[2];
+            const auto sums = [&](auto scaled, float f) {
+                s[0] = s[1] = 0.f;
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    float h[N], y[N];
+                    Vec<T>::unpack(hv[i], h);
+                    Vec<T>::unpack(yv[i], y);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const float x = scaled ? h[k] * f : h[k];
+                        s[0] = fmaf(x, x, s[0]);
+                        s[1] = fmaf(y[k] * wv[i][k], x, s[1]);
+                    }
+                }
+                row_reduce<S, 2, false>(s, red, turn);
+            };
+            const auto finish = [&](auto scaled, float rs, float f) {
+                const float c = s[1] / (float)a.d * rs * rs;
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    const int j = lane + G * i;
+                    if (!(live && j < nv))
+                        continue;
+                    float h[N], y[N], x[N];
+                    Vec<T>::unpack(hv[i], h);
+                    Vec<T>::unpack(yv[i], y);
+                    Vec<T>::unpack(rv[i], x);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        const float hk = scaled ? h[k] * f : h[k], g = fmaf(-hk, c, y[k] * wv[i][k]);
+                        x[k] = scaled ? fmaf(rs * g, f, x[k]) : fmaf(rs, g, x[k]);
+                        dw[i][k] = fmaf(y[k] * hk, rs, dw[i][k]);
+                    }
+                    *((uint4 *)(dX + t * a.d) + j) = Vec<T>::pack(x);
+                }
+            };
+            sums(std::false_type(), 1.f);
+            sum = s[0];
+            if (kInside) {
+                if (in_range(a, sum) || !live) {
+                    finish(std::false_type(), rsqrtf(sum / (float)a.d + a.eps), 1.f);
+                } else {
+                    const float f = factor_of(a, sum);
+                    forget();
+                    sums(std::true_type(), f);
+                    forget();
+                    finish(std::true_type(), root_of(s[0] / (float)a.d + a.eps * f * f), f);
+                }
+            } else {
+                if (live && !in_range(a, sum))       // (every lane of the row)
+                    break;
+                finish(std::false_type(), rsqrtf(sum / (float)a.d + a.eps), 1.f);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int j = lane + G * i;
+            if (j < nv)
+#pragma unroll
+                for (int k = 0; k < N; k += 4) {
+                    float4 *to = (float4 *)(part + j * N + k);
+                    const float4 was = kInside || first ? make_float4(0.f, 0.f, 0.f, 0.f) : *to;
+                    *to = make_float4(was.x + dw[i][k], was.y + dw[i][k + 1], was.z + dw[i][k + 2],
+                                      was.w + dw[i][k + 3]);
+                }
+        }
+        if (kInside || t0 >= a.T)
+            break;
+        norm_bwd_singly<T, S, N, true>(a, t0 + warp, factor_of(a, sum), part, red, turn);
+        t0 += stride;
     }
 }
 
@@ -524,28 +695,13 @@ __global__ void __launch_bounds__(kAnyThreads) k_rmsnorm_bwd_any(const NormBwdAr
     griddep_start();
     __shared__ __align__(16) float red[2 * 2 * 32];
     int turn = 0;
-    const T *dY = (const T *)a.dY, *H = (const T *)a.H, *dH = (const T *)a.dH;
-    T *dX = (T *)a.dX;
-    const int d = a.d;
-    float *part = a.part + (int64_t)blockIdx.x * d;
-    for (int j = threadIdx.x; j < d; j += kAnyThreads)
+    float *part = a.part + (int64_t)blockIdx.x * a.d;
+    for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
         part[j] = 0.f;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        float s[2] = {0.f, 0.f};
-        for (int j = threadIdx.x; j < d; j += kAnyThreads) {
-            const float h = Vec<T>::one(H[t * d + j]), y = Vec<T>::one(dY[t * a.ldy + j]);
-            s[0] = fmaf(h, h, s[0]);
-            s[1] = fmaf(y * weight_at(a, j), h, s[1]);
-        }
-        row_reduce<kAnyThreads, 2, false>(s, red, turn);
-        const float rs = rsqrtf(s[0] / (float)d + a.eps);
-        const float c = s[1] / (float)d * rs * rs;
-        for (int j = threadIdx.x; j < d; j += kAnyThreads) {
-            const float h = Vec<T>::one(H[t * d + j]), y = Vec<T>::one(dY[t * a.ldy + j]);
-            const float r = dH ? Vec<T>::one(dH[t * d + j]) : 0.f;
-            dX[t * d + j] = Vec<T>::round(fmaf(rs, fmaf(-h, c, y * weight_at(a, j)), r));
-            part[j] = fmaf(y * h, rs, part[j]);
-        }
+        const float sum = norm_bwd_singly<T, kAnyThreads, 1, false>(a, t, 1.f, part, red, turn);
+        if (!in_range(a, sum))
+            norm_bwd_singly<T, kAnyThreads, 1, true>(a, t, factor_of(a, sum), part, red, turn);
     }
 }
 
@@ -732,7 +888,8 @@ cudaError_t rmsnorm_fwd(sn_dtype dt, const void *X, int64_t ldx, const void *R, 
     int log2 = 0;
     while (1 << log2 < group)
         ++log2;
-    const NormArgs a{X, R, H, w, wdt == SN_BF16, T, ldx, d, eps, Y, codes, scale, log2, 0};
+    const NormArgs a{X, R, H, w, wdt == SN_BF16, T, ldx, d, eps, Y, codes, scale, log2,
+                     least_sum(d, eps), most_sum(eps), 0};
     return dt == SN_BF16 ? fwd_format<__nv_bfloat16>(a, format, s) : fwd_format<float>(a, format, s);
 }
 
@@ -757,8 +914,8 @@ cudaError_t rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H,
                         float *part, cudaStream_t s)
 {
     const size_t esize = dt == SN_BF16 ? 2 : 4;
-    const NormBwdArgs a{dY, H, dH, w, wdt == SN_BF16, T, ldy, d, eps, dX, part,
-                        ldy == d && d * esize >= 4096};
+    const NormBwdArgs a{dY, H, dH, w, wdt == SN_BF16, T, ldy, d, eps, dX, least_sum(d, eps), most_sum(eps),
+                        part, ldy == d && d * esize >= 4096};
     return dt == SN_BF16 ? bwd<__nv_bfloat16>(a, dw, accumulate, s) : bwd<float>(a, dw, accumulate, s);
 }
 
