@@ -359,7 +359,7 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t (&k)[K], int top, bo
     nan = hi == 0xffffffffu;
     const int first = 31 - __clz(hi ^ lo);                // -1: all the same
     uint32_t b = first < 0 ? hi : hi & ~((2u << first) - 1u);
-    for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {         // bf16 keys end there
+    for (int bit = first; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {         // bf16 keys differ above
         const uint32_t trial = b | 1u << bit;
         int n = 0;
 #pragma unroll
@@ -371,6 +371,10 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t (&k)[K], int top, bo
                 break;
         }
     }
+    // the low half of a bf16 key is ones below zero: with it the bound is the key itself, so that
+    // one more leaves out the elements that tie there
+    if (sizeof(T) == 2 && b >> 31 == 0)
+        b |= 0xffffu;
     return max(b, kLowestKey);
 }
 
