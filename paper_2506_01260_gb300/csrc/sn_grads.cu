@@ -165,13 +165,15 @@ __global__ void __launch_bounds__(kThreads) k_sumsq(const sn_grad_chunk *__restr
     }
 }
 
+// dst = src * pre * f; pre is 1, or 2^-126 for a factor below fp32's normal numbers, which would
+// lose bits in one: such a list goes by single elements.
 template <typename S, typename D>
-__device__ __forceinline__ void scale_chunk(const sn_grad_chunk &c, float f)
+__device__ __forceinline__ void scale_chunk(const sn_grad_chunk &c, float f, float pre)
 {
     const S *src = (const S *)c.src;
     D *dst = (D *)c.dst;
     int done = 0;
-    if (c.flags & ALIGNED) {
+    if ((c.flags & ALIGNED) && pre == 1.f) {
         constexpr int N = 8, U = sizeof(S) == 2 ? 4 : 2;  // 8 elements, 64 bytes of loads in flight
         const int nv = c.n / N;
         for (int i = threadIdx.x; i < nv; i += U * kThreads) {
@@ -201,7 +203,7 @@ __device__ __forceinline__ void scale_chunk(const sn_grad_chunk &c, float f)
         done = nv * N;
     }
     for (int i = done + threadIdx.x; i < c.n; i += kThreads)
-        dst[i] = Vec<D>::round(Vec<S>::one(src[i]) * f);
+        dst[i] = Vec<D>::round(Vec<S>::one(src[i]) * pre * f);
 }
 
 // Three blocks an SM: 64 bytes of loads a thread in flight for either type fit 78 registers (two
@@ -213,9 +215,12 @@ __global__ void __launch_bounds__(kThreads, 3) k_clip(const sn_grad_chunk *__res
     griddep_start();
     const double norm = sqrt(*sumsq);
     // NaN stays NaN; an infinite norm gives 0
-    const float f = norm > (double)max_norm ? (float)((double)max_norm / norm)
-                    : norm == norm          ? 1.f
-                                            : (float)norm;
+    const double factor = norm > (double)max_norm ? (double)max_norm / norm : norm == norm ? 1.0 : norm;
+    // (in whole numbers: an fp64 comparison and product took 0.3 us of a short list's call)
+    const int high = __double2hiint(factor);
+    const bool small = high > 0 && high < (1023 - 126) << 20;          // 0 < factor < 2^-126
+    const float pre = small ? 0x1p-126f : 1.f;
+    const float f = (float)__hiloint2double(small ? high + (126 << 20) : high, __double2loint(factor));
     if (blockIdx.x == 0 && threadIdx.x == 0)
         *norm_out = (float)norm;
     // from the list's end, whose elements the sum has left in L2
@@ -229,10 +234,10 @@ __global__ void __launch_bounds__(kThreads, 3) k_clip(const sn_grad_chunk *__res
         if (f == 1.f && (c.flags & IN_PLACE))
             continue;
         switch (c.flags & (SRC_BF16 | DST_BF16)) {
-        case 0: scale_chunk<float, float>(c, f); break;
-        case SRC_BF16: scale_chunk<__nv_bfloat16, float>(c, f); break;
-        case DST_BF16: scale_chunk<float, __nv_bfloat16>(c, f); break;
-        default: scale_chunk<__nv_bfloat16, __nv_bfloat16>(c, f); break;
+        case 0: scale_chunk<float, float>(c, f, pre); break;
+        case SRC_BF16: scale_chunk<__nv_bfloat16, float>(c, f, pre); break;
+        case DST_BF16: scale_chunk<float, __nv_bfloat16>(c, f, pre); break;
+        default: scale_chunk<__nv_bfloat16, __nv_bfloat16>(c, f, pre); break;
         }
     }
 }
