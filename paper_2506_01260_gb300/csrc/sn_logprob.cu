@@ -1169,7 +1169,7 @@ template <typename T, int LANES>
 cudaError_t bwd_launch(const LogpBwdArgs &a, cudaStream_t s)
 {
     const bool same = (((uintptr_t)a.x ^ (uintptr_t)a.dx) & 15) == 0 && (a.ld - a.ldd) % Vec<T>::N == 0;
-    constexpr int per = Vec<T>::N * kBwdPieces * LANES, kRows = kBwdThreads / LANES;
+    constexpr int64_t per = Vec<T>::N * kBwdPieces * LANES, kRows = kBwdThreads / LANES;
     count_launch();
     const cudaError_t e = launch_dependent(same ? k_logprob_bwd<T, LANES, false> : k_logprob_bwd<T, LANES, true>,
                                            dim3((unsigned)((a.V + per - 1) / per),
