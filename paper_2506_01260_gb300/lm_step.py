@@ -70,14 +70,15 @@ class TwoStage:
 
     def backward(self, ids, target):
         """The loss (mean negative log probability of the targets that there are) as a tensor, and
-        every gradient in self.grads.  ids, target: int32 [T]; a negative target is none."""
+        every gradient in self.grads.  ids, target: int32 [T]; a negative target is none, and so is
+        one past the vocabulary, which sn_check_errors reports."""
         g = self.grads
         y0, h0, up, x0 = self._stage0(ids)
         x1 = self._boundary(x0, ids)
         y1, _ = sn.sn_rmsnorm_fwd(x1, self.w1, EPS)
         logits = y1 @ self.W_head.T
         logp, lse, _, _, _ = sn.sn_logprob_fwd(logits, target, entropy=False, basis=self.basis)
-        n = (target >= 0).sum().clamp(min=1).float()
+        n = ((target >= 0) & (target < self.vocab)).sum().clamp(min=1).float()
         # back through stage 1; the logits' gradient takes the logits' place
         dlogp = (-1.0 / n).expand(ids.shape[0]).contiguous()
         dlogits = sn.sn_logprob_bwd(logits, lse, target, dlogp, out=logits)
