@@ -561,7 +561,8 @@ def sn_embed_fwd(table, ids, scale=1.0, out=None, out_dtype=None, basis=None, st
     V, d = table.shape
     T = ids.shape[0]
     if out is None:
-        out = _empty((T, d), out_dtype or table.dtype, table.device, stream)
+        empty = torch.empty if stream is None else _maker(stream, table.device)
+        out = empty((T, d), dtype=out_dtype or table.dtype, device=table.device)
     else:
         _given(out, "out", (T, d), out_dtype)
     _check(_lib.sn_embed_fwd(_error_basis(basis), _dtype(table), table.data_ptr(), V, d,
@@ -621,9 +622,10 @@ def sn_rmsnorm_fwd(X, w, eps, R=None, H=None, out=None, stream=None):
     """h = X + R, Y = h / sqrt(mean(h^2) + eps) * w; returns (Y, h), h = X without a residual.
     H may be R (the residual stream updated in place).  X may be a row-strided view."""
     ldx, H = _norm_inputs(X, w, R, H, stream)
+    empty = torch.empty if stream is None else _maker(stream, X.device)
     T, d = X.shape
     if out is None:
-        out = _empty((T, d), X.dtype, X.device, stream)
+        out = empty((T, d), dtype=X.dtype, device=X.device)
     else:
         _given(out, "out", (T, d), X.dtype)
     _check(_lib.sn_rmsnorm_fwd(_dtype(X), X.data_ptr(), ldx, _ptr(R), _ptr(H), _dtype(w),
@@ -637,9 +639,9 @@ def sn_rmsnorm_fwd_quant(X, w, eps, fmt, R=None, H=None, group=0, codes=None, sc
     """The norm's output as 8-bit codes (uint8 [T, d]; fmt "int8" or "e4m3") and fp32 scales, one
     a row or one for every `group` (32, 64, 128) columns; returns (codes, scale, h)."""
     ldx, H = _norm_inputs(X, w, R, H, stream)
+    empty = torch.empty if stream is None else _maker(stream, X.device)
     T, d = X.shape
     shape = (T, -(-d // group)) if group else (T,)
-    empty = torch.empty if stream is None else _maker(stream, X.device)
     if codes is None:
         codes = empty((T, d), dtype=torch.uint8, device=X.device)
     else:
@@ -736,7 +738,8 @@ def sn_logprob_bwd(logits, lse, target=None, dlogp=None, scale=1.0, entropy=None
     if target is not None:
         _given(target, "target", (T,), torch.int32)
     if out is None:
-        out = _empty((T, V), logits.dtype, logits.device, stream)
+        empty = torch.empty if stream is None else _maker(stream, logits.device)
+        out = empty((T, V), dtype=logits.dtype, device=logits.device)
         ldd = V
     else:
         ldd = _rows(out, "out", logits.dtype)
@@ -806,7 +809,8 @@ def sn_grads_sumsq(grads, out=None, accumulate=False, stream=None):
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
-        out = _empty((1,), torch.float64, grads.device, stream)
+        empty = torch.empty if stream is None else _maker(stream, grads.device)
+        out = empty((1,), dtype=torch.float64, device=grads.device)
     else:
         _need(out, "out", torch.float64)
         if out.numel() < 1:
@@ -821,7 +825,8 @@ def sn_grads_clip(grads, sumsq, max_norm, norm=None, stream=None):
     (device fp32 [1])."""
     _need(sumsq, "sumsq", torch.float64)
     if norm is None:
-        norm = _empty((1,), torch.float32, grads.device, stream)
+        empty = torch.empty if stream is None else _maker(stream, grads.device)
+        norm = empty((1,), dtype=torch.float32, device=grads.device)
     else:
         _need(norm, "norm", torch.float32)
     if sumsq.numel() < 1 or norm.numel() < 1:
