@@ -264,3 +264,38 @@ def test_step_on_another_stream_is_compared_whole(sn):
     torch.cuda.synchronize()
     for a, b in zip(calls(side), want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_on_a_forked_stream_of_a_capture(sn):
+    """Calls on a second stream of a captured graph make their memory in the graph's pool: replays
+    give the eager calls' bits."""
+    T, d, V = 3000, 512, 900
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, h = (torch.randn(T, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    w = torch.randn(d, generator=g, device="cuda")
+    ids = torch.randint(V, (T,), generator=g, device="cuda", dtype=I32)
+    side = torch.cuda.Stream()
+
+    def run():
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        dX, dw = sn.sn_rmsnorm_bwd(x, h, w, 1e-5, stream=side)
+        dE = sn.sn_embed_bwd(dX, ids, V, stream=side)
+        Y = sn.sn_rmsnorm_fwd(h, w, 1e-5)[0]             # meanwhile
+        here.wait_stream(side)
+        return [dX, dw, dE, Y]
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for seed in (1, 2):
+        x.copy_(torch.randn(T, d, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), i
