@@ -111,7 +111,8 @@ class TwoStage:
 
     def score(self, ids, top=5):
         """For every position: the log probability of the token that follows (none for the last),
-        the entropy and the `top` alternatives, with stage 1's products from 8-bit activations."""
+        the entropy and the `top` alternatives.  Stage 1's activations pass through 8 bits (e4m3, a
+        scale a row), to show what that does to the scores; the products themselves are bf16."""
         _, _, _, x0 = self._stage0(ids)
         codes, scale, _ = sn.sn_rmsnorm_fwd_quant(self._boundary(x0, ids), self.w1, EPS, "e4m3")
         y1 = sn.sn_quant_restore(codes, scale, "e4m3")
