@@ -170,6 +170,13 @@ __device__ __forceinline__ bool in_range(const A &a, float sum) { return sum >= 
 template <typename A>
 __device__ __forceinline__ float factor_of(const A &a, float sum) { return sum < a.least ? 0x1p100f : 0x1p-80f; }
 __device__ __forceinline__ float root_of(float mean) { return mean <= kMost ? rsqrtf(mean) : NAN; }
+// A scaled row's dx, of y w, n, mean(g n), 1 / rms(h f) and f: the factor's root on either side of the
+// reciprocal root, so that nothing on the way is smaller or larger than fp32 holds where dx is not
+__device__ __forceinline__ float scaled_dx(float g, float n, float m, float rs, float f, float r)
+{
+    const float half = f > 1.f ? 0x1p50f : 0x1p-40f;
+    return fmaf(fmaf(-n, m, g) * half * rs, half, r);
+}
 
 // ---- forward, rows in registers ------------------------------------------------------------
 
@@ -516,12 +523,12 @@ __device__ float norm_bwd_singly(const NormBwdArgs &a, int64_t t, float f, float
         return s[0];
     const float mean = s[0] / (float)d + (SCALED ? a.eps * f * f : a.eps);
     const float rs = SCALED ? root_of(mean) : rsqrtf(mean);
-    const float c = s[1] / (float)d * rs * rs;
+    const float m = s[1] / (float)d * rs, c = m * rs;
     for (int i = lane * M; i < d; i += G * M)
         for (int j = i; j < i + M; ++j) {
             const float h = h_at(j), y = Vec<T>::one(dY[j]);
-            const float r = dH ? Vec<T>::one(dH[j]) : 0.f, g = fmaf(-h, c, y * weight_at(a, j));
-            dX[j] = Vec<T>::round(SCALED ? fmaf(rs * g, f, r) : fmaf(rs, g, r));
+            const float r = dH ? Vec<T>::one(dH[j]) : 0.f, g = y * weight_at(a, j);
+            dX[j] = Vec<T>::round(SCALED ? scaled_dx(g, h * rs, m, rs, f, r) : fmaf(rs, fmaf(-h, c, g), r));
             part[j] = fmaf(y * h, rs, part[j]);
         }
     return s[0];
@@ -631,7 +638,7 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                 row_reduce<S, 2, false>(s, red, turn);
             };
             const auto finish = [&](auto scaled, float rs, float f) {
-                const float c = s[1] / (float)a.d * rs * rs;
+                const float m = s[1] / (float)a.d * rs, c = m * rs;
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     const int j = lane + G * i;
@@ -643,8 +650,8 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                     Vec<T>::unpack(rv[i], x);
 #pragma unroll
                     for (int k = 0; k < N; ++k) {
-                        const float hk = scaled ? h[k] * f : h[k], g = fmaf(-hk, c, y[k] * wv[i][k]);
-                        x[k] = scaled ? fmaf(rs * g, f, x[k]) : fmaf(rs, g, x[k]);
+                        const float hk = scaled ? h[k] * f : h[k], g = y[k] * wv[i][k];
+                        x[k] = scaled ? scaled_dx(g, hk * rs, m, rs, f, x[k]) : fmaf(rs, fmaf(-hk, c, g), x[k]);
                         dw[i][k] = fmaf(y[k] * hk, rs, dw[i][k]);
                     }
                     *((uint4 *)(dX + t * a.d) + j) = Vec<T>::pack(x);

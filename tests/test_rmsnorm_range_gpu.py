@@ -127,3 +127,26 @@ def test_no_gradient_at_tiny_rows(sn):
         h = torch.full((3, 256), 1e-40, device="cuda").to(dt)
         dx, dw = sn.sn_rmsnorm_bwd(torch.zeros_like(h), h, torch.ones(256, device="cuda"), 0.0)
         assert bool((dx == 0).all()) and bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("dt", DT)
+@pytest.mark.parametrize("d", WIDTHS)
+def test_gradient_where_the_weight_is_zero(sn, dt, d):
+    """Columns whose weight is 0 have the second term of dx alone, far smaller than the others' dx
+    at rows that eps outweighs (n is small there); it keeps its bits as long as fp32 holds it."""
+    g = gen(3 * d)
+    h, size = rows(d, dt, g, T=3)
+    dy = (torch.randn(h.shape, generator=g, device="cuda") * size.clamp(1e-6, 1e6)).to(h.dtype)
+    w = torch.randn(d, generator=g, device="cuda")
+    w[::2] = 0.0
+    h64, dy64, w64 = h.double(), dy.double(), w.double()
+    for eps in (0.0, 1e-33):
+        dx, _ = sn.sn_rmsnorm_bwd(dy, h, w, eps)
+        rs = (h64.square().mean(1, keepdim=True) + eps).rsqrt()
+        n, q = h64 * rs, dy64 * w64
+        first, second = rs * q, rs * n * (q * n).mean(1, keepdim=True)
+        worst = rs * n.abs() * (q * n).abs().mean(1, keepdim=True)
+        ref = first - second
+        # (n mean(g n) itself below fp32's normal numbers: a unit of those, times the reciprocal root)
+        bound = (first.abs() + 4 * second.abs()) * RS + worst * 2.0 ** -17 + 2 * SMALLEST[h.dtype] + rs * 2.0 ** -148
+        within(dx, ref, bound + ref.abs() * UNIT[h.dtype] * 1.02)
