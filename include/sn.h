@@ -390,6 +390,41 @@ sn_status sn_logprob_bwd(sn_dtype dtype, const void *logits, int64_t T, int64_t 
                          const float *entropy, const float *dentropy, float scale, void *dlogits,
                          int64_t ldd, sn_stream_t stream);
 
+/* ---- Gated projections of a feed-forward block -----------------------------------------
+ *   G = X W_gate^T,   U = X W_up^T,   H = act(G) * U   (element by element)
+ * What a block computes in front of its down projection (W_p2, the weight that is kept in
+ * S).  act (sn_act): silu g / (1 + e^-g); gelu g Phi(g), Phi the normal distribution
+ * function; gelu_tanh, its approximation g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2;
+ * relu.  bf16 only (SN_ERR_UNSUPPORTED for SN_F32); products accumulate in fp32, and every
+ * output is rounded once.  d and f are multiples of 8 (SN_ERR_ALIGNMENT), at most 2^20.
+ * `errors` is a basis, whose error word records a wait that expired, or NULL. */
+typedef enum { SN_ACT_SILU = 0, SN_ACT_GELU = 1, SN_ACT_GELU_TANH = 2, SN_ACT_RELU = 3 } sn_act;
+
+/* X: [T, d] with row stride ldx (elements, a multiple of 8); W_gate, W_up: [f, d]; H:
+ * [T, f].  G and U, [T, f] each, are what the gradient reads; both may be NULL (nothing is
+ * kept).  No output may overlap anything else. */
+sn_status sn_glu_fwd(sn_basis_t errors, sn_dtype dtype, const void *X, int64_t ldx,
+                     const void *W_gate, const void *W_up, int64_t T, int32_t d, int32_t f,
+                     int32_t act, void *G, void *U, void *H, sn_stream_t stream);
+
+/* Bytes of device workspace that sn_glu_bwd needs. */
+sn_status sn_glu_bwd_workspace(int64_t T, int32_t d, int32_t f, size_t *bytes);
+
+/* The gradients, from the G and U that the forward stored:
+ *   dG = dH * U * act'(G),   dU = dH * act(G)
+ *   dX = dG W_gate + dU W_up,   dW_gate = dG^T X,   dW_up = dU^T X
+ * dH: [T, f] with row stride lddh (a multiple of 8).  dG and dU, [T, f] each, are rounded to
+ * bf16, and the products read them as they are stored; dG may be G and dU may be U.  dX:
+ * [T, d], or NULL (not computed; W_gate and W_up may then be NULL).  dW_gate, dW_up: [f, d]
+ * in grad_dtype, added to with accumulate != 0, or both NULL (X may then be NULL).  No other
+ * overlaps.  Sums are taken in a fixed order: the same inputs give the same bits.
+ * workspace: 16-byte aligned, at least sn_glu_bwd_workspace bytes. */
+sn_status sn_glu_bwd(sn_basis_t errors, sn_dtype dtype, const void *dH, int64_t lddh, const void *X,
+                     int64_t ldx, const void *W_gate, const void *W_up, const void *G, const void *U,
+                     int64_t T, int32_t d, int32_t f, int32_t act, void *dG, void *dU, void *dX,
+                     sn_dtype grad_dtype, void *dW_gate, void *dW_up, int32_t accumulate,
+                     void *workspace, size_t workspace_bytes, sn_stream_t stream);
+
 /* ---- Global gradient norm and clipping ------------------------------------------------
  * A list of gradient tensors is described once (the handle keeps a table of them in
  * device memory), then summed and scaled in one launch each:

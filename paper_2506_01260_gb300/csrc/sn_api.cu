@@ -885,6 +885,99 @@ sn_status sn_logprob_bwd(sn_dtype dt, const void *x, int64_t T, int64_t V, int64
                                        (cudaStream_t)stream));
 }
 
+namespace {
+sn_status check_glu(sn_dtype dt, int64_t T, int32_t d, int32_t f, int32_t act, std::initializer_list<int64_t> lds)
+{
+    if (!is_dtype(dt) || T < 0 || T >= kMaxTokens || d < 1 || d > kMaxWidth || f < 1 || f > kMaxWidth ||
+        act < SN_ACT_SILU || act > SN_ACT_RELU)
+        return SN_ERR_INVALID_ARG;
+    for (const int64_t ld : lds)
+        if (ld >= kMaxRows)
+            return SN_ERR_INVALID_ARG;
+    if (dt != SN_BF16)
+        return SN_ERR_UNSUPPORTED;
+    if (d % 8 || f % 8)
+        return SN_ERR_ALIGNMENT;
+    for (const int64_t ld : lds)
+        if (ld % 8)
+            return SN_ERR_ALIGNMENT;
+    return SN_OK;
+}
+}  // namespace
+
+sn_status sn_glu_fwd(sn_basis_t errors, sn_dtype dt, const void *X, int64_t ldx, const void *Wg, const void *Wu,
+                     int64_t T, int32_t d, int32_t f, int32_t act, void *G, void *U, void *H, sn_stream_t stream)
+{
+    unsigned int *err;
+    sn_status st = error_word(errors, &err);
+    if (st == SN_OK)
+        st = ldx < d ? SN_ERR_INVALID_ARG : check_glu(dt, T, d, f, act, {ldx});
+    if (st != SN_OK || T == 0)
+        return st;
+    if (!X || !Wg || !Wu || !H || (G == nullptr) != (U == nullptr))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(X, 16) || !aligned(Wg, 16) || !aligned(Wu, 16) || !aligned(G, 16) || !aligned(U, 16) ||
+        !aligned(H, 16))
+        return SN_ERR_ALIGNMENT;
+    const Buf x(X, T, d, ldx, 2), wg(Wg, f, d, d, 2), wu(Wu, f, d, d, 2), g(G, T, f, f, 2), u(U, T, f, f, 2),
+        h(H, T, f, f, 2);
+    if (clashes(h, {x, wg, wu, g, u}) || clashes(g, {x, wg, wu, u}) || clashes(u, {x, wg, wu}) ||
+        !on_device({X, Wg, Wu, G, U, H}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::glu_fwd(X, ldx, Wg, Wu, T, d, f, act, G, U, H, err, (cudaStream_t)stream));
+}
+
+sn_status sn_glu_bwd_workspace(int64_t T, int32_t d, int32_t f, size_t *bytes)
+{
+    const sn_status st = check_glu(SN_BF16, T, d, f, SN_ACT_SILU, {});
+    if (st != SN_OK || !bytes)
+        return st != SN_OK ? st : SN_ERR_INVALID_ARG;
+    *bytes = sn::glu_bwd_workspace(T, d, f);
+    return SN_OK;
+}
+
+sn_status sn_glu_bwd(sn_basis_t errors, sn_dtype dt, const void *dH, int64_t lddh, const void *X, int64_t ldx,
+                     const void *Wg, const void *Wu, const void *G, const void *U, int64_t T, int32_t d, int32_t f,
+                     int32_t act, void *dG, void *dU, void *dX, sn_dtype gdt, void *dWg, void *dWu,
+                     int32_t accumulate, void *ws, size_t ws_bytes, sn_stream_t stream)
+{
+    unsigned int *err;
+    sn_status st = error_word(errors, &err);
+    if (st != SN_OK)
+        return st;
+    const bool dx = dX != nullptr, dw = dWg != nullptr;
+    if (!is_dtype(gdt) || lddh < f || (dw && ldx < d) || dw != (dWu != nullptr))
+        return SN_ERR_INVALID_ARG;
+    st = check_glu(dt, T, d, f, act, {lddh, dw ? ldx : 0});
+    if (st != SN_OK)
+        return st;
+    const size_t need = sn::glu_bwd_workspace(T, d, f), es = esize(gdt);
+    if (T > 0 && (!dH || !G || !U || !dG || !dU || (dx && (!Wg || !Wu)) || (dw && !X) ||
+                  (need > 0 && (!ws || ws_bytes < need))))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(dH, 16) || !aligned(X, 16) || !aligned(Wg, 16) || !aligned(Wu, 16) || !aligned(G, 16) ||
+        !aligned(U, 16) || !aligned(dG, 16) || !aligned(dU, 16) || !aligned(dX, 16) || !aligned(dWg, 16) ||
+        !aligned(dWu, 16) || !aligned(ws, 16))
+        return SN_ERR_ALIGNMENT;
+    const Buf h(dH, T, f, lddh, 2), x(dw ? X : nullptr, T, d, ldx, 2), wg(dx ? Wg : nullptr, f, d, d, 2),
+        wu(dx ? Wu : nullptr, f, d, d, 2), g(G, T, f, f, 2), u(U, T, f, f, 2), dg(dG, T, f, f, 2), du(dU, T, f, f, 2),
+        dxb(dX, T, d, d, 2), a(dWg, f, d, d, es), b(dWu, f, d, d, es), p(T > 0 ? ws : nullptr, 1, need, need, 1);
+    if (clashes_unless_same(dg, g, true) || clashes_unless_same(du, u, true) || clashes(dg, {h, x, wg, wu, u, du}) ||
+        clashes(du, {h, x, wg, wu, g}) || clashes(dxb, {h, x, wg, wu, g, u, dg, du, a, b}) ||
+        clashes(a, {h, x, wg, wu, g, u, dg, du, b}) || clashes(b, {h, x, wg, wu, g, u, dg, du}) ||
+        clashes(p, {h, x, wg, wu, g, u, dg, du, dxb, a, b}) ||
+        !on_device({dH, X, Wg, Wu, G, U, dG, dU, dX, dWg, dWu, ws}))
+        return SN_ERR_INVALID_ARG;
+    if (T == 0) {
+        if (!dw || accumulate)
+            return SN_OK;
+        const cudaError_t e = cudaMemsetAsync(dWg, 0, (size_t)f * d * es, (cudaStream_t)stream);
+        return cuda_status(e != cudaSuccess ? e : cudaMemsetAsync(dWu, 0, (size_t)f * d * es, (cudaStream_t)stream));
+    }
+    return cuda_status(sn::glu_bwd(dH, lddh, X, ldx, Wg, Wu, G, U, T, d, f, act, dG, dU, dX, gdt, dWg, dWu,
+                                   accumulate != 0, ws, err, (cudaStream_t)stream));
+}
+
 sn_status sn_grads_create(int32_t n, const void *const *src, const sn_dtype *sdt, const int64_t *count,
                           void *const *dst, const sn_dtype *ddt, sn_grads_t *out, sn_stream_t stream)
 try {

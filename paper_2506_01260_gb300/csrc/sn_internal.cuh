@@ -215,6 +215,14 @@ cudaError_t logprob_fwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld
 cudaError_t logprob_bwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld, const int32_t *target,
                         const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
                         float scale, void *dx, int64_t ldd, cudaStream_t s);
+// Gated projections of a feed-forward block; their gradients (err: null or a basis' error word)
+cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, int64_t T, int d, int f, int act,
+                    void *G, void *U, void *H, unsigned int *err, cudaStream_t s);
+size_t glu_bwd_workspace(int64_t T, int d, int f);
+cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, const void *Wg, const void *Wu,
+                    const void *G, const void *U, int64_t T, int d, int f, int act, void *dG, void *dU, void *dX,
+                    sn_dtype grad_dt, void *dWg, void *dWu, bool accumulate, void *ws, unsigned int *err,
+                    cudaStream_t s);
 // Global gradient norm and clipping (grads_create may throw std::bad_alloc)
 cudaError_t grads_create(int n, const void *const *src, const sn_dtype *src_dt, const int64_t *count,
                          void *const *dst, const sn_dtype *dst_dt, sn_grads **out, cudaStream_t s);

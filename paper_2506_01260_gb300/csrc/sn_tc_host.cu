@@ -217,6 +217,13 @@ int current_device()
 }
 
 }  // namespace
+
+bool tensor_map_2d(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t row_bytes,
+                   uint32_t box_inner, uint32_t box_outer, bool sw128)
+{
+    return map2d(m, ptr, inner, outer, row_bytes, box_inner, box_outer, sw128);
+}
+
 }  // namespace tc
 
 // Last-round split of the compress contractions and of the fp32 table

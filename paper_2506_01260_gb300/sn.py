@@ -79,6 +79,10 @@ _sig("sn_rmsnorm_bwd_workspace", [_I64, _I32, ctypes.POINTER(_SZ)])
 _sig("sn_rmsnorm_bwd", [_ST, _P, _I64, _P, _P, _ST, _P, _I64, _I32, _F, _P, _P, _I32, _P, _SZ, _P])
 _sig("sn_logprob_fwd", [_P, _ST, _P, _I64, _I64, _I64, _P, _F, _P, _P, _P, _I32, _P, _P, _P])
 _sig("sn_logprob_bwd", [_ST, _P, _I64, _I64, _I64, _P, _P, _P, _P, _P, _F, _P, _I64, _P])
+_sig("sn_glu_fwd", [_P, _ST, _P, _I64, _P, _P, _I64, _I32, _I32, _I32, _P, _P, _P, _P])
+_sig("sn_glu_bwd_workspace", [_I64, _I32, _I32, ctypes.POINTER(_SZ)])
+_sig("sn_glu_bwd", [_P, _ST, _P, _I64, _P, _I64, _P, _P, _P, _P, _I64, _I32, _I32, _I32, _P, _P, _P, _ST,
+                    _P, _P, _I32, _P, _SZ, _P])
 _sig("sn_grads_create", [_I32, _P, _P, _P, _P, _P, ctypes.POINTER(_P), _P])
 _sig("sn_grads_destroy", [_P])
 _sig("sn_grads_sumsq", [_P, _P, _I32, _P])
@@ -102,7 +106,7 @@ EXPORTS = ["sn_basis_create", "sn_basis_destroy", "sn_basis_shape", "sn_compress
            "sn_sign_compress", "sn_sign_restore", "sn_quant_compress", "sn_quant_restore",
            "sn_embed_fwd", "sn_embed_bwd_workspace", "sn_embed_bwd", "sn_rmsnorm_fwd",
            "sn_rmsnorm_fwd_quant", "sn_rmsnorm_bwd_workspace", "sn_rmsnorm_bwd", "sn_logprob_fwd",
-           "sn_logprob_bwd", "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
+           "sn_logprob_bwd", "sn_glu_fwd", "sn_glu_bwd_workspace", "sn_glu_bwd", "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
            "sn_wire_bytes", "sn_wire_send",
            "sn_wire_recv", "sn_check_errors", "sn_selftest_wait_timeout",
            "sn_selftest_barrier_timeout", "sn_launch_count",
@@ -748,6 +752,94 @@ def sn_logprob_bwd(logits, lse, target=None, dlogp=None, scale=1.0, entropy=None
                                lse.data_ptr(), _ptr(dlogp), _ptr(entropy), _ptr(dentropy), scale,
                                out.data_ptr(), ldd, _stream_of(logits, stream)), "sn_logprob_bwd")
     return out
+
+
+#: activations of sn_glu_fwd
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+
+
+def _given_or(t, name, shape, dtype, empty, device):
+    if t is None:
+        return empty(shape, dtype=dtype, device=device)
+    _given(t, name, shape, dtype)
+    return t
+
+
+def sn_glu_fwd(X, W_gate, W_up, act="silu", keep=False, out=None, G=None, U=None, basis=None,
+               stream=None):
+    """H = act(X W_gate^T) * (X W_up^T) for X [T, d] and weights [f, d]; returns (H, G, U): the two
+    products, bf16 as the gradient reads them, with keep=True (or where given), else None.  X may
+    be a row-strided view; act "silu", "gelu", "gelu_tanh" or "relu"."""
+    ldx = _rows(X, "X")
+    T, d = X.shape
+    _need(W_gate, "W_gate", X.dtype)
+    if W_gate.dim() != 2 or W_gate.shape[1] != d:
+        raise ValueError("W_gate must be [f, d]")
+    _given(W_up, "W_up", W_gate.shape, X.dtype)
+    f = W_gate.shape[0]
+    empty = torch.empty if stream is None else _maker(stream, X.device)
+    out = _given_or(out, "out", (T, f), X.dtype, empty, X.device)
+    if keep or G is not None or U is not None:
+        G = _given_or(G, "G", (T, f), X.dtype, empty, X.device)
+        U = _given_or(U, "U", (T, f), X.dtype, empty, X.device)
+    _check(_lib.sn_glu_fwd(_error_basis(basis), _dtype(X), X.data_ptr(), ldx, W_gate.data_ptr(),
+                           W_up.data_ptr(), T, d, f, ACTIVATIONS[act], _ptr(G), _ptr(U),
+                           out.data_ptr(), _stream_of(X, stream)), "sn_glu_fwd")
+    return out, G, U
+
+
+@functools.lru_cache(maxsize=256)
+def sn_glu_bwd_workspace(T, d, f):
+    n = _SZ()
+    _check(_lib.sn_glu_bwd_workspace(T, d, f, ctypes.byref(n)), "sn_glu_bwd_workspace")
+    return n.value
+
+
+def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None, dW_gate=None,
+               dW_up=None, need_dX=True, need_dW=True, grad_dtype=None, accumulate=False,
+               workspace=None, basis=None, stream=None):
+    """(dX, dW_gate, dW_up, dG, dU) from dH and the forward's G and U.  dG may be G and dU may be U.
+    need_dX=False or need_dW=False leave those products out (None); the weights' gradients are in
+    `grad_dtype` (by default the weights' type) and added to with accumulate=True.  dH and X may be
+    row-strided views."""
+    ldh = _rows(dH, "dH")
+    T, f = dH.shape
+    ldx = _rows(X, "X", dH.dtype)
+    d = X.shape[1]
+    if X.shape[0] != T:
+        raise ValueError("X must have dH's rows")
+    for t, name in ((W_gate, "W_gate"), (W_up, "W_up")):
+        _given(t, name, (f, d), dH.dtype)
+    for t, name in ((G, "G"), (U, "U")):
+        _given(t, name, (T, f), dH.dtype)
+    dev = dH.device
+    empty = torch.empty if stream is None else _maker(stream, dev)
+    dG = _given_or(dG, "dG", (T, f), dH.dtype, empty, dev)
+    dU = _given_or(dU, "dU", (T, f), dH.dtype, empty, dev)
+    dX = _given_or(dX, "dX", (T, d), dH.dtype, empty, dev) if need_dX else None
+    if need_dW:
+        if accumulate and (dW_gate is None or dW_up is None):
+            raise ValueError("accumulate=True needs dW_gate and dW_up")
+        if dW_gate is not None and grad_dtype is None:
+            grad_dtype = dW_gate.dtype
+        grad_dtype = grad_dtype or W_gate.dtype
+        dW_gate = _given_or(dW_gate, "dW_gate", (f, d), grad_dtype, empty, dev)
+        dW_up = _given_or(dW_up, "dW_up", (f, d), grad_dtype, empty, dev)
+    else:
+        dW_gate = dW_up = None
+    if workspace is None:
+        nbytes = max(16, sn_glu_bwd_workspace(T, d, f))
+        workspace = empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        _need(workspace, "workspace")
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(_lib.sn_glu_bwd(_error_basis(basis), _dtype(dH), dH.data_ptr(), ldh, X.data_ptr(), ldx,
+                           W_gate.data_ptr(), W_up.data_ptr(), G.data_ptr(), U.data_ptr(), T, d, f,
+                           ACTIVATIONS[act], dG.data_ptr(), dU.data_ptr(), _ptr(dX),
+                           _dtype(dW_gate) if need_dW else SN_BF16, _ptr(dW_gate), _ptr(dW_up),
+                           bool(accumulate), workspace.data_ptr(), nbytes, _stream_of(dH, stream)),
+           "sn_glu_bwd")
+    return dX, dW_gate, dW_up, dG, dU
 
 
 class GradList:
