@@ -358,6 +358,45 @@ sn_status sn_rmsnorm_bwd(sn_dtype dtype, const void *dY, int64_t ldy, const void
                          float *dw, int32_t accumulate, void *workspace, size_t workspace_bytes,
                          sn_stream_t stream);
 
+/* ---- Norms after and before a block, with its gate and residual scale --------------------
+ *   n = y / sqrt(mean(y^2) + eps),   h = r + scale * gate * (n * w_post)
+ *   z = h / sqrt(mean(h^2) + eps) * w_pre                      (row by row)
+ * What follows a block's last product and precedes the next block's first: y is the block's
+ * output, r the residual stream, h the stream behind the block, z what the next block reads.
+ * Y, R, gate, H, Z and the gradients share `dtype`; w_post, w_pre: [d] in w_dtype.  gate:
+ * [gates, d], T a multiple of gates, row i for the tokens i T / gates and on (a sequence, or
+ * with gates = 1 every token, or with gates = T one token); NULL with gates = 0: none (1).
+ * Y: [T, d] with row stride ldy (elements); the others contiguous.  h and z come from fp32
+ * and are rounded once each, z from the unrounded h.  H and Z may each be R or (where ldy =
+ * d) Y, not one another; other overlaps are SN_ERR_INVALID_ARG.  eps >= 0, eps and scale
+ * finite; 1 <= d <= 2^20.  Rows of y and h of any finite size are right, also where their squares
+ * pass fp32's range; a row whose y or h has an infinity or a NaN is NaN whole. */
+sn_status sn_blocknorm_fwd(sn_dtype dtype, const void *Y, int64_t ldy, const void *R,
+                           const void *gate, int64_t gates, sn_dtype w_dtype, const void *w_post,
+                           const void *w_pre, int64_t T, int32_t d, float eps, float scale, void *H,
+                           void *Z, sn_stream_t stream);
+
+/* Bytes of device workspace that sn_blocknorm_bwd needs. */
+sn_status sn_blocknorm_bwd_workspace(int64_t T, int32_t d, int64_t gates, size_t *bytes);
+
+/* The gradients, from Y and the h that the forward stored:
+ *   g = dz * w_pre,  n2 = h / sqrt(mean(h^2) + eps)
+ *   dr = (g - n2 mean(g n2)) / sqrt(mean(h^2) + eps) + dH,   dw_pre = sum_t dz n2
+ *   e = scale * gate * w_post * dr,   dy = (e - n mean(e n)) / sqrt(mean(y^2) + eps)
+ *   dw_post = sum_t scale * gate * dr * n,   dgate = sum over its tokens of scale * w_post * dr * n
+ * dZ: [T, d] with row stride lddz; dH: the gradient that reaches h along the residual stream,
+ * or NULL.  dw_post, dw_pre: fp32 [d]; dgate: fp32 [gates, d] (NULL without a gate); added to
+ * with accumulate != 0.  Products and sums of magnitudes have to fit fp32.  dY and dR may each be
+ * an input with its rows (contiguous), not one another.  Sums are taken in a fixed order: the same
+ * inputs give the same bits.  workspace: 16-byte aligned, at least sn_blocknorm_bwd_workspace
+ * bytes. */
+sn_status sn_blocknorm_bwd(sn_dtype dtype, const void *dZ, int64_t lddz, const void *H,
+                           const void *Y, int64_t ldy, const void *dH, const void *gate,
+                           int64_t gates, sn_dtype w_dtype, const void *w_post, const void *w_pre,
+                           int64_t T, int32_t d, float eps, float scale, void *dY, void *dR,
+                           float *dw_post, float *dw_pre, float *dgate, int32_t accumulate,
+                           void *workspace, size_t workspace_bytes, sn_stream_t stream);
+
 /* ---- Log probabilities of given tokens ----------------------------------------------
  * The last stage's loss and a server's scores.  logits: [T, vocab] in dtype with
  * row stride ld (elements); z = scale * logits, 0 < scale < 2.35e38 (the inverse

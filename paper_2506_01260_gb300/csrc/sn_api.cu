@@ -815,6 +815,101 @@ sn_status sn_rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H
 }
 
 namespace {
+// A gate has a row for every T / gates tokens in a run
+bool is_gating(const void *gate, int64_t gates, int64_t T)
+{
+    return gate ? gates >= 1 && T % gates == 0 && (T == 0 || gates <= T) : gates == 0;
+}
+}  // namespace
+
+sn_status sn_blocknorm_fwd(sn_dtype dt, const void *Y, int64_t ldy, const void *R, const void *gate, int64_t gates,
+                           sn_dtype wdt, const void *w_post, const void *w_pre, int64_t T, int32_t d, float eps,
+                           float scale, void *H, void *Z, sn_stream_t stream)
+{
+    const sn_status st = check_norm(dt, wdt, T, d, ldy, eps);
+    if (st != SN_OK)
+        return st;
+    if (!std::isfinite(scale) || !is_gating(gate, gates, T))
+        return SN_ERR_INVALID_ARG;
+    if (T == 0)
+        return SN_OK;
+    if (!Y || !R || !w_post || !w_pre || !H || !Z)
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(Y, 16) || !aligned(R, 16) || !aligned(gate, 16) || !aligned(w_post, 16) || !aligned(w_pre, 16) ||
+        !aligned(H, 16) || !aligned(Z, 16))
+        return SN_ERR_ALIGNMENT;
+    const size_t es = esize(dt);
+    const Buf y(Y, T, d, ldy, es), r(R, T, d, d, es), g(gate, gates, d, d, es), p(w_post, 1, d, d, esize(wdt)),
+        q(w_pre, 1, d, d, esize(wdt)), h(H, T, d, d, es), z(Z, T, d, d, es);
+    if (clashes_unless_same(h, y, ldy == d) || clashes_unless_same(h, r, true) || clashes_unless_same(z, y, ldy == d) ||
+        clashes_unless_same(z, r, true) || clashes(h, {g, p, q, z}) || clashes(z, {g, p, q}) ||
+        !on_device({Y, R, gate, w_post, w_pre, H, Z}))
+        return SN_ERR_INVALID_ARG;
+    return cuda_status(sn::blocknorm_fwd(dt, Y, ldy, R, gate, gates, wdt, w_post, w_pre, T, d, eps, scale, H, Z,
+                                         (cudaStream_t)stream));
+}
+
+sn_status sn_blocknorm_bwd_workspace(int64_t T, int32_t d, int64_t gates, size_t *bytes)
+{
+    if (!bytes || T < 0 || T >= kMaxRows || d < 1 || d > kMaxWidth || gates < 0 || (gates > 0 && T % gates))
+        return SN_ERR_INVALID_ARG;
+    *bytes = T == 0 ? 0 : sn::blocknorm_bwd_workspace(T, d, gates);
+    return SN_OK;
+}
+
+sn_status sn_blocknorm_bwd(sn_dtype dt, const void *dZ, int64_t lddz, const void *H, const void *Y, int64_t ldy,
+                           const void *dH, const void *gate, int64_t gates, sn_dtype wdt, const void *w_post,
+                           const void *w_pre, int64_t T, int32_t d, float eps, float scale, void *dY, void *dR,
+                           float *dw_post, float *dw_pre, float *dgate, int32_t accumulate, void *ws,
+                           size_t ws_bytes, sn_stream_t stream)
+{
+    sn_status st = check_norm(dt, wdt, T, d, ldy, eps);
+    if (st == SN_OK)
+        st = check_norm(dt, wdt, T, d, lddz, eps);
+    if (st != SN_OK)
+        return st;
+    if (!std::isfinite(scale) || !is_gating(gate, gates, T) || !dw_post || !dw_pre ||
+        (gate == nullptr) != (dgate == nullptr))
+        return SN_ERR_INVALID_ARG;
+    const size_t need = T > 0 ? sn::blocknorm_bwd_workspace(T, d, gates) : 0;
+    if (T > 0 && (!dZ || !H || !Y || !w_post || !w_pre || !dY || !dR || !ws || ws_bytes < need))
+        return SN_ERR_INVALID_ARG;
+    if (!aligned(dZ, 16) || !aligned(H, 16) || !aligned(Y, 16) || !aligned(dH, 16) || !aligned(gate, 16) ||
+        !aligned(w_post, 16) || !aligned(w_pre, 16) || !aligned(dY, 16) || !aligned(dR, 16) ||
+        !aligned(dw_post, 16) || !aligned(dw_pre, 16) || !aligned(dgate, 16) || !aligned(ws, 16))
+        return SN_ERR_ALIGNMENT;
+    const size_t es = esize(dt);
+    const Buf z(dZ, T, d, lddz, es), h(H, T, d, d, es), y(Y, T, d, ldy, es), r(dH, T, d, d, es),
+        g(gate, gates, d, d, es), p(T > 0 ? w_post : nullptr, 1, d, d, esize(wdt)),
+        q(T > 0 ? w_pre : nullptr, 1, d, d, esize(wdt)), oy(dY, T, d, d, es), orr(dR, T, d, d, es),
+        a(dw_post, 1, d, d, 4), b(dw_pre, 1, d, d, 4), c(dgate, gates, d, d, 4), w(T > 0 ? ws : nullptr, 1, need, need, 1);
+    for (const Buf *o : {&oy, &orr})
+        if (clashes_unless_same(*o, z, lddz == d) || clashes_unless_same(*o, h, true) ||
+            clashes_unless_same(*o, y, ldy == d) || clashes_unless_same(*o, r, true) ||
+            clashes(*o, {g, p, q, a, b, c, w}))
+            return SN_ERR_INVALID_ARG;
+    if (clashes(oy, {orr}) || clashes(a, {z, h, y, r, g, p, q, b, c, w}) || clashes(b, {z, h, y, r, g, p, q, c, w}) ||
+        clashes(c, {z, h, y, r, g, p, q, w}) || clashes(w, {z, h, y, r, g, p, q}) ||
+        !on_device({dZ, H, Y, dH, gate, w_post, w_pre, dY, dR, dw_post, dw_pre, dgate, ws}))
+        return SN_ERR_INVALID_ARG;
+    if (T == 0) {
+        const cudaStream_t s = (cudaStream_t)stream;
+        cudaError_t e = cudaSuccess;
+        if (!accumulate) {
+            e = cudaMemsetAsync(dw_post, 0, (size_t)d * 4, s);
+            if (e == cudaSuccess)
+                e = cudaMemsetAsync(dw_pre, 0, (size_t)d * 4, s);
+            if (e == cudaSuccess && dgate)
+                e = cudaMemsetAsync(dgate, 0, (size_t)gates * d * 4, s);
+        }
+        return cuda_status(e);
+    }
+    return cuda_status(sn::blocknorm_bwd(dt, dZ, lddz, H, Y, ldy, dH, gate, gates, wdt, w_post, w_pre, T, d, eps,
+                                         scale, dY, dR, dw_post, dw_pre, dgate, accumulate != 0, (float *)ws,
+                                         (cudaStream_t)stream));
+}
+
+namespace {
 sn_status check_logits(sn_dtype dt, int64_t T, int64_t V, int64_t ld, float scale)
 {
     // (the kernels' exponents are scale * log2(e) times a difference of logits)

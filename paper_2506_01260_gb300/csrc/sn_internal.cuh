@@ -208,6 +208,15 @@ size_t rmsnorm_bwd_workspace(int64_t T, int d);
 cudaError_t rmsnorm_bwd(sn_dtype dt, const void *dY, int64_t ldy, const void *H, const void *dH, sn_dtype wdt,
                         const void *w, int64_t T, int d, float eps, void *dX, float *dw, bool accumulate,
                         float *part, cudaStream_t s);
+// Norms after and before a block, with its gate and residual scale; gates = 0: no gate
+cudaError_t blocknorm_fwd(sn_dtype dt, const void *Y, int64_t ldy, const void *R, const void *gate, int64_t gates,
+                          sn_dtype wdt, const void *w_post, const void *w_pre, int64_t T, int d, float eps,
+                          float scale, void *H, void *Z, cudaStream_t s);
+size_t blocknorm_bwd_workspace(int64_t T, int d, int64_t gates);
+cudaError_t blocknorm_bwd(sn_dtype dt, const void *dZ, int64_t lddz, const void *H, const void *Y, int64_t ldy,
+                          const void *dH, const void *gate, int64_t gates, sn_dtype wdt, const void *w_post,
+                          const void *w_pre, int64_t T, int d, float eps, float scale, void *dY, void *dR,
+                          float *dw_post, float *dw_pre, float *dgate, bool accumulate, float *ws, cudaStream_t s);
 // Log probabilities of given tokens, entropy and alternatives; their gradient
 cudaError_t logprob_fwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld, const int32_t *target,
                         float scale, float *logp, float *lse, float *entropy, int top, int32_t *top_ids,

@@ -77,6 +77,10 @@ _sig("sn_rmsnorm_fwd_quant", [_ST, _P, _I64, _P, _P, _ST, _P, _I64, _I32, _F, _I
                               _P])
 _sig("sn_rmsnorm_bwd_workspace", [_I64, _I32, ctypes.POINTER(_SZ)])
 _sig("sn_rmsnorm_bwd", [_ST, _P, _I64, _P, _P, _ST, _P, _I64, _I32, _F, _P, _P, _I32, _P, _SZ, _P])
+_sig("sn_blocknorm_fwd", [_ST, _P, _I64, _P, _P, _I64, _ST, _P, _P, _I64, _I32, _F, _F, _P, _P, _P])
+_sig("sn_blocknorm_bwd_workspace", [_I64, _I32, _I64, ctypes.POINTER(_SZ)])
+_sig("sn_blocknorm_bwd", [_ST, _P, _I64, _P, _P, _I64, _P, _P, _I64, _ST, _P, _P, _I64, _I32, _F, _F, _P,
+                          _P, _P, _P, _P, _I32, _P, _SZ, _P])
 _sig("sn_logprob_fwd", [_P, _ST, _P, _I64, _I64, _I64, _P, _F, _P, _P, _P, _I32, _P, _P, _P])
 _sig("sn_logprob_bwd", [_ST, _P, _I64, _I64, _I64, _P, _P, _P, _P, _P, _F, _P, _I64, _P])
 _sig("sn_glu_fwd", [_P, _ST, _P, _I64, _P, _P, _I64, _I32, _I32, _I32, _P, _P, _P, _P])
@@ -105,7 +109,8 @@ EXPORTS = ["sn_basis_create", "sn_basis_destroy", "sn_basis_shape", "sn_compress
            "sn_grassmann_step", "sn_adamw_rowconst", "sn_topk_compress", "sn_topk_restore",
            "sn_sign_compress", "sn_sign_restore", "sn_quant_compress", "sn_quant_restore",
            "sn_embed_fwd", "sn_embed_bwd_workspace", "sn_embed_bwd", "sn_rmsnorm_fwd",
-           "sn_rmsnorm_fwd_quant", "sn_rmsnorm_bwd_workspace", "sn_rmsnorm_bwd", "sn_logprob_fwd",
+           "sn_rmsnorm_fwd_quant", "sn_rmsnorm_bwd_workspace", "sn_rmsnorm_bwd",
+           "sn_blocknorm_fwd", "sn_blocknorm_bwd_workspace", "sn_blocknorm_bwd", "sn_logprob_fwd",
            "sn_logprob_bwd", "sn_glu_fwd", "sn_glu_bwd_workspace", "sn_glu_bwd", "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
            "sn_wire_bytes", "sn_wire_send",
            "sn_wire_recv", "sn_check_errors", "sn_selftest_wait_timeout",
@@ -546,6 +551,13 @@ def _given(t, name, shape, dtype):
         raise ValueError("%s must have shape %s" % (name, tuple(shape)))
 
 
+def _given_or(t, name, shape, dtype, empty, device):
+    if t is None:
+        return empty(shape, dtype=dtype, device=device)
+    _given(t, name, shape, dtype)
+    return t
+
+
 def _stream_of(t, stream):
     """As _stream; by default the current stream of t's device."""
     return _raw_stream(t.get_device()) if stream is None else _stream(stream)
@@ -702,6 +714,91 @@ def sn_rmsnorm_bwd(dY, H, w, eps, dH=None, out=None, dw=None, accumulate=False, 
     return out, dw
 
 
+def _gating(gate, T, d, dtype):
+    """Rows of a gate for T tokens, each for T / rows of them; 0 without one."""
+    if gate is None:
+        return 0
+    _need(gate, "gate", dtype)
+    if gate.dim() != 2 or gate.shape[1] != d or gate.shape[0] == 0 or T % gate.shape[0]:
+        raise ValueError("gate must be [gates, d] with a number of tokens that gates divides")
+    return gate.shape[0]
+
+
+def _norm_weights(w_post, w_pre, d):
+    _given(w_post, "w_post", (d,), None)
+    _given(w_pre, "w_pre", (d,), w_post.dtype)
+
+
+def sn_blocknorm_fwd(Y, R, w_post, w_pre, eps, scale=1.0, gate=None, H=None, out=None, stream=None):
+    """The norm after a block, its gate and residual scale, and the norm before the next one:
+    h = R + scale * gate * norm(Y) * w_post, Z = norm(h) * w_pre; returns (Z, h).  gate: [gates, d],
+    a row for every T / gates tokens in a run, or None.  H may be R (the residual stream updated in
+    place).  Y may be a row-strided view."""
+    ldy = _rows(Y, "Y")
+    T, d = Y.shape
+    _given(R, "R", (T, d), Y.dtype)
+    _norm_weights(w_post, w_pre, d)
+    gates = _gating(gate, T, d, Y.dtype)
+    empty = torch.empty if stream is None else _maker(stream, Y.device)
+    out = _given_or(out, "out", (T, d), Y.dtype, empty, Y.device)
+    H = _given_or(H, "H", (T, d), Y.dtype, empty, Y.device)
+    _check(_lib.sn_blocknorm_fwd(_dtype(Y), Y.data_ptr(), ldy, R.data_ptr(), _ptr(gate), gates,
+                                 _dtype(w_post), w_post.data_ptr(), w_pre.data_ptr(), T, d, eps, scale,
+                                 H.data_ptr(), out.data_ptr(), _stream_of(Y, stream)),
+           "sn_blocknorm_fwd")
+    return out, H
+
+
+@functools.lru_cache(maxsize=256)
+def sn_blocknorm_bwd_workspace(T, d, gates):
+    n = _SZ()
+    _check(_lib.sn_blocknorm_bwd_workspace(T, d, gates, ctypes.byref(n)),
+           "sn_blocknorm_bwd_workspace")
+    return n.value
+
+
+def sn_blocknorm_bwd(dZ, H, Y, w_post, w_pre, eps, scale=1.0, gate=None, dH=None, dY=None, dR=None,
+                     dw_post=None, dw_pre=None, dgate=None, accumulate=False, workspace=None,
+                     stream=None):
+    """(dY, dR, dw_post, dw_pre, dgate) from Y and the forward's h; dH is the gradient that reaches h
+    along the residual stream.  The weights' and the gate's gradients are fp32 (dgate None without a
+    gate), added to with accumulate=True.  dZ and Y may be row-strided views."""
+    lddz, ldy = _rows(dZ, "dZ"), _rows(Y, "Y", dZ.dtype)
+    T, d = dZ.shape
+    if Y.shape != (T, d):
+        raise ValueError("Y must have dZ's shape")
+    _given(H, "H", (T, d), dZ.dtype)
+    _norm_weights(w_post, w_pre, d)
+    if dH is not None:
+        _given(dH, "dH", (T, d), dZ.dtype)
+    gates = _gating(gate, T, d, dZ.dtype)
+    if gate is None and dgate is not None:
+        raise ValueError("dgate needs a gate")
+    if accumulate and (dw_post is None or dw_pre is None or (gates and dgate is None)):
+        raise ValueError("accumulate=True needs dw_post, dw_pre and with a gate dgate")
+    dev, f32 = dZ.device, torch.float32
+    empty = torch.empty if stream is None else _maker(stream, dev)
+    dY = _given_or(dY, "dY", (T, d), dZ.dtype, empty, dev)
+    dR = _given_or(dR, "dR", (T, d), dZ.dtype, empty, dev)
+    dw_post = _given_or(dw_post, "dw_post", (d,), f32, empty, dev)
+    dw_pre = _given_or(dw_pre, "dw_pre", (d,), f32, empty, dev)
+    if gates:
+        dgate = _given_or(dgate, "dgate", (gates, d), f32, empty, dev)
+    if workspace is None:
+        nbytes = max(16, sn_blocknorm_bwd_workspace(T, d, gates))
+        workspace = empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        _need(workspace, "workspace")
+        nbytes = workspace.numel() * workspace.element_size()
+    _check(_lib.sn_blocknorm_bwd(_dtype(dZ), dZ.data_ptr(), lddz, H.data_ptr(), Y.data_ptr(), ldy,
+                                 _ptr(dH), _ptr(gate), gates, _dtype(w_post), w_post.data_ptr(),
+                                 w_pre.data_ptr(), T, d, eps, scale, dY.data_ptr(), dR.data_ptr(),
+                                 dw_post.data_ptr(), dw_pre.data_ptr(), _ptr(dgate), bool(accumulate),
+                                 workspace.data_ptr(), nbytes, _stream_of(dZ, stream)),
+           "sn_blocknorm_bwd")
+    return dY, dR, dw_post, dw_pre, dgate
+
+
 def sn_logprob_fwd(logits, target=None, scale=1.0, top=0, entropy=True, basis=None, stream=None):
     """(logp, lse, entropy, top_ids, top_logp) of softmax(scale * logits): logp and entropy fp32
     [T], the `top` alternatives [T, top] (ids int32), and lse fp32 [T, 2], the log-sum-exp as the
@@ -756,13 +853,6 @@ def sn_logprob_bwd(logits, lse, target=None, dlogp=None, scale=1.0, entropy=None
 
 #: activations of sn_glu_fwd
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
-
-
-def _given_or(t, name, shape, dtype, empty, device):
-    if t is None:
-        return empty(shape, dtype=dtype, device=device)
-    _given(t, name, shape, dtype)
-    return t
 
 
 def sn_glu_fwd(X, W_gate, W_up, act="silu", keep=False, out=None, G=None, U=None, basis=None,
