@@ -35,15 +35,17 @@ struct Args {
     int64_t T, ldy, lddz;
     int64_t per_gate;           // tokens that share a row of the gate
     int d;
-    float eps, scale;
+    float eps, scale, inverse_d;
     float least, most;          // of a row's sum of squares that is taken as it is
     void *H, *Z;                // the gradient: dR, dY
-    // the gradient's work: chunks of `rows` tokens, `split` of them to a gate's tokens
-    int64_t chunks, rows, split;
-    float *dgate;               // written where a chunk has all of a gate's tokens
+    int64_t workers;            // the gradient's, at most T
+    float *dgate;               // written where a worker has all of a gate's tokens
     bool add;
-    float *part_pre, *part_post;    // [workers, d]
-    float *part_gate;               // [chunks, d], where split > 1
+    bool gated;                 // by more than one row: S is every gate's own
+    // [parts, d], a part a block, of dw_pre and (gated: a part a worker) of dw_post, which is S
+    // itself where it is one for all tokens
+    float *part_pre, *part_post;
+    float *part_gate;           // gated: [workers + gates, d], S of worker w and gate i at w + i
     bool prefetch;
 };
 
@@ -212,98 +214,207 @@ __global__ void __launch_bounds__(kAnyThreads) k_blocknorm_any(const Args a)
 
 // ---- gradient ----------------------------------------------------------------------------------
 
-// A row's sums, of h and y scaled by their factors where their squares ask for it
+// Of T tokens, worker w of W takes those from w T / W on; token t is worker ((t + 1) W - 1) / T's.
+__device__ __forceinline__ int64_t first_token(int64_t w, int64_t W, int64_t T) { return w * T / W; }
+__device__ __forceinline__ int64_t worker_of(int64_t t, int64_t W, int64_t T) { return ((t + 1) * W - 1) / T; }
+
+// The six sums of a row, over its elements or pairs of them
+template <typename F>
 struct Sums {
-    float s[6];     // h h, g h, y y, m y g, m y h, m y dh
-    __device__ __forceinline__ void add(float h, float g, float y, float m, float r)
-    {
-        const float my = m * y;
-        s[0] = fmaf(h, h, s[0]);
-        s[1] = fmaf(g, h, s[1]);
-        s[2] = fmaf(y, y, s[2]);
-        s[3] = fmaf(my, g, s[3]);
-        s[4] = fmaf(my, h, s[4]);
-        s[5] = fmaf(my, r, s[5]);
-    }
+    F s[6];         // h h, g h, y y, m y g, m y h, m y dh
 };
-// What the elements of a row share
+__device__ __forceinline__ float fma_of(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float mul_of(float a, float b) { return a * b; }
+__device__ __forceinline__ float2 fma_of(float2 a, float2 b, float2 c) { return fma2(a, b, c); }
+__device__ __forceinline__ float2 mul_of(float2 a, float2 b) { return mul2(a, b); }
+template <typename F>
+__device__ __forceinline__ void add_element(Sums<F> &m, F h, F z, F y, F r, F pw, F mw)
+{
+    const F g = mul_of(z, pw), my = mul_of(y, mw);
+    m.s[0] = fma_of(h, h, m.s[0]);
+    m.s[1] = fma_of(g, h, m.s[1]);
+    m.s[2] = fma_of(y, y, m.s[2]);
+    m.s[3] = fma_of(my, g, m.s[3]);
+    m.s[4] = fma_of(my, h, m.s[4]);
+    m.s[5] = fma_of(my, r, m.s[5]);
+}
+template <typename F>
+__device__ __forceinline__ F every(float x);
+template <>
+__device__ __forceinline__ float every<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float2 every<float2>(float x) { return both(x); }
+
+// What the elements of a row share; h and y are scaled by factors where their squares ask for it
 struct Row {
-    float fh, fy;               // the factors, 1 for almost every row
-    float r2, c2, a2, half2;    // 1 / rms(h f), mean(g n2), and 1 / rms(h) in two factors
+    float fh = 1.f, fy = 1.f;   // the factors, 1 for almost every row
+    float r2, c2, a2, half2;    // 1 / rms(h f), -mean(g n2), and 1 / rms(h) in two factors
     float r1, c1, a1, half1;
+    // whether h or y has to be taken again by a factor
+    __device__ __forceinline__ bool again(const Args &a, const float (&s)[6])
+    {
+        const bool h = fh == 1.f && !in_range(a, s[0]), y = fy == 1.f && !in_range(a, s[2]);
+        if (h)
+            fh = factor_of(a, s[0]);
+        if (y)
+            fy = factor_of(a, s[2]);
+        return h || y;
+    }
     __device__ __forceinline__ void finish(const Args &a, const float (&s)[6])
     {
-        const float n = (float)a.d;
-        r2 = root_of(s[0] / n + a.eps * fh * fh);
-        r1 = root_of(s[2] / n + a.eps * fy * fy);
+        r2 = root_of(fmaf(s[0], a.inverse_d, a.eps * fh * fh));
+        r1 = root_of(fmaf(s[2], a.inverse_d, a.eps * fy * fy));
         half2 = half_of(fh);
         half1 = half_of(fy);
         a2 = r2 * half2;
         a1 = r1 * half1;
-        c2 = s[1] / n * r2;
-        const float ey = fmaf(fmaf(-r2 * c2, s[4], s[3]) * a2, half2, s[5]);
-        c1 = ey / n * r1;
+        c2 = -(s[1] * a.inverse_d) * r2;
+        c1 = -(fmaf(fmaf(r2 * c2, s[4], s[3]) * a2, half2, s[5]) * a.inverse_d) * r1;
     }
-    // dh' and dy of an element, and n1 and n2
-    __device__ __forceinline__ void element(float h, float g, float y, float m, float r, float &dh, float &dy,
-                                            float &n1, float &n2) const
+    // dh' and dy of an element, and its parts of dw_pre and S
+    template <typename F>
+    __device__ __forceinline__ void element(F h, F z, F y, F r, F pw, F mw, F &dh, F &dy, F &pre, F &sum) const
     {
-        n2 = h * r2;
-        n1 = y * r1;
-        dh = fmaf(fmaf(-n2, c2, g) * a2, half2, r);
-        dy = fmaf(-n1, c1, m * dh) * a1 * half1;
+        const F n2 = mul_of(h, every<F>(r2)), n1 = mul_of(y, every<F>(r1));
+        dh = fma_of(mul_of(fma_of(n2, every<F>(c2), mul_of(z, pw)), every<F>(a2)), every<F>(half2), r);
+        dy = mul_of(mul_of(fma_of(n1, every<F>(c1), mul_of(mw, dh)), every<F>(a1)), every<F>(half1));
+        pre = fma_of(z, n2, pre);
+        sum = fma_of(dh, n1, sum);
     }
 };
 
+// The sums of six values over the lanes of a row, in every lane.  Three halvings leave a lane one
+// value of its eighth of the warp (9 shuffles for the six, not 30), a lane then adds four warps'
+// parts of one value.  `red`: 2 * 8 * 32 floats that calls alternate between (`turn`).
+template <int S>
+__device__ __forceinline__ void row_sums(float (&v)[6], float *red, int &turn)
+{
+    const int lane = threadIdx.x % 32;
+    const bool b4 = lane & 16, b3 = lane & 8, b2 = lane & 4;
+    // lanes with b4 keep values 4 and 5 (and two zeros), the others 0 to 3; then halves of those
+    float x[4];
+    x[0] = (b4 ? v[4] : v[0]) + __shfl_xor_sync(0xffffffffu, b4 ? v[0] : v[4], 16);
+    x[1] = (b4 ? v[5] : v[1]) + __shfl_xor_sync(0xffffffffu, b4 ? v[1] : v[5], 16);
+    x[2] = __shfl_xor_sync(0xffffffffu, v[2], 16) + v[2];
+    x[3] = __shfl_xor_sync(0xffffffffu, v[3], 16) + v[3];
+    if (b4)
+        x[2] = x[3] = 0.f;
+    float y[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        y[i] = (b3 ? x[2 + i] : x[i]) + __shfl_xor_sync(0xffffffffu, b3 ? x[i] : x[2 + i], 8);
+    float z = (b2 ? y[1] : y[0]) + __shfl_xor_sync(0xffffffffu, b2 ? y[0] : y[1], 4);
+    z += __shfl_xor_sync(0xffffffffu, z, 2);
+    z += __shfl_xor_sync(0xffffffffu, z, 1);            // value lane / 4 of the warp
+    if (S > 32) {
+        const int warps = blockDim.x / 32, warp = threadIdx.x / 32;
+        float *at = red + turn * (8 * 32);
+        turn ^= 1;
+        if (lane % 4 == 0)
+            at[lane * 8 + warp] = z;                    // value lane / 4: 32 warps
+        __syncthreads();
+        z = 0.f;
+#pragma unroll
+        for (int w = 0; w < S / 32; w += 16) {
+            const int first = w + lane % 4 * 4;
+            if (first < warps) {
+                const float4 p = *(const float4 *)(at + lane / 4 * 32 + first);
+                z += (p.x + (first + 1 < warps ? p.y : 0.f)) +
+                     ((first + 2 < warps ? p.z : 0.f) + (first + 3 < warps ? p.w : 0.f));
+            }
+        }
+        z += __shfl_xor_sync(0xffffffffu, z, 2);
+        z += __shfl_xor_sync(0xffffffffu, z, 1);
+    }
+#pragma unroll
+    for (int k = 0; k < 6; ++k)
+        v[k] = __shfl_sync(0xffffffffu, z, 4 * k);
+}
+
+// Piece j of an array of fours (see k_blocknorm_bwd), as pairs
+template <int P>
+__device__ __forceinline__ void from_fours(const float4 *w, int nv, int j, float2 (&f)[P])
+{
+#pragma unroll
+    for (int k = 0; k < P; k += 2) {
+        const float4 v = w[k / 2 * nv + j];
+        f[k] = make_float2(v.x, v.y);
+        f[k + 1] = make_float2(v.z, v.w);
+    }
+}
+
 // Threads of an SM that registers are kept low enough for
 template <typename T, int S, int C>
-constexpr int kBwdResident = S > 512 ? S : S == 320 ? 640 : S == 32 && C == 1 ? 768 : 512;
+constexpr int kBwdResident = S > 512 ? S : S == 320 ? 640 : 512;
 
-// A worker (a warp or a block) walks its chunks of tokens, a row at a time, and keeps dw_pre and
-// S of its columns in registers; m and w_pre lie in shared memory, each thread's own columns.
+// A worker (a warp or a block) walks its run of tokens, a row at a time, and keeps dw_pre and the
+// present gate's S of its columns in registers; m and w_pre lie in shared memory, each thread's own
+// columns.
 template <typename T, int S, int C>
 __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Shape<S>::kThreads)
     k_blocknorm_bwd(const Args a)
 {
     griddep_start();
-    extern __shared__ __align__(16) float weights[];
-    constexpr int N = Vec<T>::N, kRows = Shape<S>::kRows;
-    __shared__ __align__(16) float red[2 * 6 * 32];
+    extern __shared__ float4 weights[];
+    constexpr int N = Vec<T>::N, P = N / 2, kRows = Shape<S>::kRows;
+    __shared__ __align__(16) float red[2 * 8 * 32];
     int turn = 0;
     const int G = Shape<S>::lanes(), lane = S == 32 ? threadIdx.x % 32 : threadIdx.x;
     const int warp = S == 32 ? threadIdx.x / 32 : 0, nv = a.d / N;
     const T *Y = (const T *)a.Y, *H = (const T *)a.R, *dZ = (const T *)a.dZ, *dH = (const T *)a.dH;
     T *dR = (T *)a.H, *dY = (T *)a.Z;
-    float *wp = weights + (int64_t)warp * 2 * a.d, *wm = wp + a.d;
-    const int64_t worker = (int64_t)blockIdx.x * kRows + warp, workers = (int64_t)gridDim.x * kRows;
-    float pre[C][N];
+    // fours of a piece's elements, the pieces' first fours in front: lanes read neighbouring 16 bytes
+    float4 *wp = weights + warp * (2 * (N / 4)) * nv, *wm = wp + (N / 4) * nv;
+    const int64_t worker = (int64_t)blockIdx.x * kRows + warp, workers = a.workers;
+    float2 pre[C][P];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         const int j = lane + G * i;
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            pre[i][k] = 0.f;
+        for (int k = 0; k < P; ++k)
+            pre[i][k] = both(0.f);
         if (j < nv) {
             float w[N];
             load_weight(a.pre, j * N, w);
 #pragma unroll
             for (int k = 0; k < N; k += 4)
-                *(float4 *)(wp + j * N + k) = make_float4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+                wp[k / 4 * nv + j] = make_float4(w[k], w[k + 1], w[k + 2], w[k + 3]);
         }
     }
     // The next row's loads run before this row's sums meet, where registers allow
-    constexpr bool kEarly = C == 1 || sizeof(T) == 4;
-    bool first = true;
-    for (int64_t c = worker; c < a.chunks; c += workers, first = false) {
-        const int64_t i_gate = c / a.split, in = c - i_gate * a.split;
-        const int64_t t0 = i_gate * a.per_gate + in * a.rows, t1 = min(t0 + a.rows, (i_gate + 1) * a.per_gate);
-        float sum[C][N];
+    constexpr bool kEarly = C == 1 || (sizeof(T) == 4 && C == 2);
+    uint4 hv[C], yv[C], zv[C], rv[C], hn[C], yn[C], zn[C], rn[C];
+    // (of the last block's warps some may have none)
+    const int64_t t1 = worker < workers ? first_token(worker + 1, workers, a.T) : 0;
+    auto load = [&](int64_t t, uint4 (&h)[C], uint4 (&y)[C], uint4 (&z)[C], uint4 (&r)[C]) {
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
+            const bool live = t < t1 && j < nv;
+            h[i] = live ? *((const uint4 *)(H + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+            y[i] = live ? *((const uint4 *)(Y + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
+            z[i] = live ? *((const uint4 *)(dZ + t * a.lddz) + j) : make_uint4(0, 0, 0, 0);
+            r[i] = live && dH ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    int64_t t = first_token(worker, workers, a.T);
+    if (kEarly)
+        load(t, hn, yn, zn, rn);
+    float2 sum[C][P];
+    const auto clear = [&] {
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                sum[i][k] = 0.f;
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int k = 0; k < P; ++k)
+                sum[i][k] = both(0.f);
+    };
+    clear();
+    for (bool first = true; t < t1; first = false) {
+        const int64_t i_gate = a.gated ? gate_of(a, t) : 0, t0 = t;
+        const int64_t end = a.gated ? min(t1, (i_gate + 1) * a.per_gate) : t1;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int j = lane + G * i;
             if (j < nv) {
                 float w[N], g[N];
                 load_weight(a.post, j * N, w);
@@ -314,24 +425,10 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                     w[k] = a.scale * (a.gate ? g[k] * w[k] : w[k]);
 #pragma unroll
                 for (int k = 0; k < N; k += 4)
-                    *(float4 *)(wm + j * N + k) = make_float4(w[k], w[k + 1], w[k + 2], w[k + 3]);
+                    wm[k / 4 * nv + j] = make_float4(w[k], w[k + 1], w[k + 2], w[k + 3]);
             }
         }
-        uint4 hv[C], yv[C], zv[C], rv[C], hn[C], yn[C], zn[C], rn[C];
-        auto load = [&](int64_t t, uint4 (&h)[C], uint4 (&y)[C], uint4 (&z)[C], uint4 (&r)[C]) {
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int j = lane + G * i;
-                const bool live = t < t1 && j < nv;
-                h[i] = live ? *((const uint4 *)(H + t * a.d) + j) : make_uint4(0, 0, 0, 0);
-                y[i] = live ? *((const uint4 *)(Y + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
-                z[i] = live ? *((const uint4 *)(dZ + t * a.lddz) + j) : make_uint4(0, 0, 0, 0);
-                r[i] = live && dH ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        if (kEarly)
-            load(t0, hn, yn, zn, rn);
-        for (int64_t t = t0; t < t1; ++t) {
+        for (; t < end; ++t) {
             if (kEarly) {
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
@@ -351,64 +448,78 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                 if (p)
                     prefetch_l2(p, (uint32_t)(a.d * sizeof(T)));
             }
-            Sums m;
             Row row;
-            row.fh = row.fy = 1.f;
+            float m[6];
 #pragma unroll 1
-            while (true) {                     // again for a row out of range
+            while (true) {
+                Sums<float2> sums;
 #pragma unroll
                 for (int k = 0; k < 6; ++k)
-                    m.s[k] = 0.f;
+                    sums.s[k] = both(0.f);
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     const int j = lane + G * i;
                     if (j < nv) {
-                        float h[N], y[N], z[N], r[N];
-                        Vec<T>::unpack(hv[i], h);
-                        Vec<T>::unpack(yv[i], y);
-                        Vec<T>::unpack(zv[i], z);
-                        Vec<T>::unpack(rv[i], r);
+                        float2 h[P], y[P], z[P], r[P], pw[P], mw[P];
+                        from_fours(wp, nv, j, pw);
+                        from_fours(wm, nv, j, mw);
+                        unpack_pairs(hv[i], h);
+                        unpack_pairs(yv[i], y);
+                        unpack_pairs(zv[i], z);
+                        unpack_pairs(rv[i], r);
 #pragma unroll
-                        for (int k = 0; k < N; ++k)
-                            m.add(h[k] * row.fh, z[k] * wp[j * N + k], y[k] * row.fy, wm[j * N + k], r[k]);
+                        for (int k = 0; k < P; ++k)
+                            add_element(sums, h[k], z[k], y[k], r[k], pw[k], mw[k]);
                     }
                 }
-                row_reduce<S, 6, false>(m.s, red, turn);
-                const bool h_again = row.fh == 1.f && !in_range(a, m.s[0]);
-                const bool y_again = row.fy == 1.f && !in_range(a, m.s[2]);
-                if (!(h_again || y_again))     // (every lane of the row)
+#pragma unroll
+                for (int k = 0; k < 6; ++k)
+                    m[k] = sums.s[k].x + sums.s[k].y;
+                row_sums<S>(m, red, turn);
+                const float fh = row.fh, fy = row.fy;
+                if (!row.again(a, m))          // (every lane of the row)
                     break;
-                if (h_again)
-                    row.fh = factor_of(a, m.s[0]);
-                if (y_again)
-                    row.fy = factor_of(a, m.s[2]);
+                // a row out of range is scaled where it lies: exact but for elements that vanish
+                // beside the row's largest
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    float2 x[P];
+                    unpack_pairs(hv[i], x);
+#pragma unroll
+                    for (int k = 0; k < P; ++k)
+                        x[k] = mul2(x[k], both(fh == row.fh ? 1.f : row.fh));
+                    hv[i] = pack_pairs(x);
+                    unpack_pairs(yv[i], x);
+#pragma unroll
+                    for (int k = 0; k < P; ++k)
+                        x[k] = mul2(x[k], both(fy == row.fy ? 1.f : row.fy));
+                    yv[i] = pack_pairs(x);
+                }
             }
-            row.finish(a, m.s);
+            row.finish(a, m);
 #pragma unroll
             for (int i = 0; i < C; ++i) {
                 const int j = lane + G * i;
                 if (j < nv) {
-                    float h[N], y[N], z[N], r[N];
-                    Vec<T>::unpack(hv[i], h);
-                    Vec<T>::unpack(yv[i], y);
-                    Vec<T>::unpack(zv[i], z);
-                    Vec<T>::unpack(rv[i], r);
+                    float2 h[P], y[P], z[P], r[P], pw[P], mw[P];
+                    from_fours(wp, nv, j, pw);
+                    from_fours(wm, nv, j, mw);
+                    unpack_pairs(hv[i], h);
+                    unpack_pairs(yv[i], y);
+                    unpack_pairs(zv[i], z);
+                    unpack_pairs(rv[i], r);
 #pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        float dh, dy, n1, n2;
-                        row.element(h[k] * row.fh, z[k] * wp[j * N + k], y[k] * row.fy, wm[j * N + k], r[k], dh, dy,
-                                    n1, n2);
-                        pre[i][k] = fmaf(z[k], n2, pre[i][k]);
-                        sum[i][k] = fmaf(dh, n1, sum[i][k]);
-                        h[k] = dh;
-                        y[k] = dy;
-                    }
-                    *((uint4 *)(dR + t * a.d) + j) = Vec<T>::pack(h);
-                    *((uint4 *)(dY + t * a.d) + j) = Vec<T>::pack(y);
+                    for (int k = 0; k < P; ++k)
+                        row.element(h[k], z[k], y[k], r[k], pw[k], mw[k], h[k], y[k], pre[i][k], sum[i][k]);
+                    *((uint4 *)(dR + t * a.d) + j) = pack_pairs(h);
+                    *((uint4 *)(dY + t * a.d) + j) = pack_pairs(y);
                 }
             }
         }
-        // the chunk's S goes to w_post's gradient and to its gate's
+        if (!a.gated)
+            break;
+        // S goes to w_post's gradient and to its gate's
+        const bool whole = end - t0 == a.per_gate;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
@@ -416,42 +527,61 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                 continue;
             float w[N], g[N];
             load_weight(a.post, j * N, w);
-            if (a.gate)
-                Vec<T>::unpack(__ldg((const uint4 *)((const T *)a.gate + i_gate * a.d) + j), g);
+            Vec<T>::unpack(__ldg((const uint4 *)((const T *)a.gate + i_gate * a.d) + j), g);
             float *post = a.part_post + worker * a.d + j * N;
-            float *to = a.split > 1 ? a.part_gate + c * a.d + j * N : a.dgate + i_gate * a.d + j * N;
+            float *to = whole ? a.dgate + i_gate * a.d + j * N : a.part_gate + (worker + i_gate) * a.d + j * N;
 #pragma unroll
             for (int k = 0; k < N; k += 4) {
+                float4 q = make_float4(sum[i][k / 2].x, sum[i][k / 2].y, sum[i][k / 2 + 1].x, sum[i][k / 2 + 1].y);
                 float4 p = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *(float4 *)(post + k);
-                p.x = fmaf(a.scale * (a.gate ? g[k] : 1.f), sum[i][k], p.x);
-                p.y = fmaf(a.scale * (a.gate ? g[k + 1] : 1.f), sum[i][k + 1], p.y);
-                p.z = fmaf(a.scale * (a.gate ? g[k + 2] : 1.f), sum[i][k + 2], p.z);
-                p.w = fmaf(a.scale * (a.gate ? g[k + 3] : 1.f), sum[i][k + 3], p.w);
-                *(float4 *)(post + k) = p;
-                if (a.gate) {
-                    float4 q = make_float4(sum[i][k], sum[i][k + 1], sum[i][k + 2], sum[i][k + 3]);
-                    if (a.split == 1) {
-                        const float4 was = a.add ? *(float4 *)(to + k) : make_float4(0.f, 0.f, 0.f, 0.f);
-                        q = make_float4(fmaf(a.scale * w[k], q.x, was.x), fmaf(a.scale * w[k + 1], q.y, was.y),
-                                        fmaf(a.scale * w[k + 2], q.z, was.z), fmaf(a.scale * w[k + 3], q.w, was.w));
-                    }
-                    *(float4 *)(to + k) = q;
+                *(float4 *)(post + k) = make_float4(fmaf(a.scale * g[k], q.x, p.x), fmaf(a.scale * g[k + 1], q.y, p.y),
+                                                    fmaf(a.scale * g[k + 2], q.z, p.z),
+                                                    fmaf(a.scale * g[k + 3], q.w, p.w));
+                if (whole) {
+                    p = a.add ? *(float4 *)(to + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    q = make_float4(fmaf(a.scale * w[k], q.x, p.x), fmaf(a.scale * w[k + 1], q.y, p.y),
+                                    fmaf(a.scale * w[k + 2], q.z, p.z), fmaf(a.scale * w[k + 3], q.w, p.w));
                 }
+                *(float4 *)(to + k) = q;
             }
         }
+        clear();
     }
+    // What a block has summed: a row's lanes each their columns, or with a row a warp the sum of its
+    // warps', through their shared memory
+    if (S == 32)
+        __syncwarp();
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         const int j = lane + G * i;
         if (j < nv)
 #pragma unroll
             for (int k = 0; k < N; k += 4) {
-                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-                *(float4 *)(a.part_pre + worker * a.d + j * N + k) =
-                    make_float4(pre[i][k], pre[i][k + 1], pre[i][k + 2], pre[i][k + 3]);
-                if (first)                     // no chunk was this worker's
-                    *(float4 *)(a.part_post + worker * a.d + j * N + k) = zero;
+                const float4 p = make_float4(pre[i][k / 2].x, pre[i][k / 2].y, pre[i][k / 2 + 1].x, pre[i][k / 2 + 1].y);
+                const float4 q = make_float4(sum[i][k / 2].x, sum[i][k / 2].y, sum[i][k / 2 + 1].x, sum[i][k / 2 + 1].y);
+                if (S == 32) {
+                    wp[k / 4 * nv + j] = p;
+                    wm[k / 4 * nv + j] = q;
+                } else {
+                    *(float4 *)(a.part_pre + worker * a.d + j * N + k) = p;
+                    if (!a.gated)
+                        *(float4 *)(a.part_post + worker * a.d + j * N + k) = q;
+                }
             }
+    }
+    if (S == 32) {
+        __syncthreads();
+        const int fours = N / 4 * nv;
+        for (int e = threadIdx.x; e < (a.gated ? fours : 2 * fours); e += blockDim.x) {
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = 0; w < kRows; ++w) {
+                const float4 v = weights[w * 2 * fours + e];
+                s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+            }
+            const int at = e % fours;
+            float *to = (e < fours ? a.part_pre : a.part_post) + (int64_t)blockIdx.x * a.d;
+            *(float4 *)(to + at % nv * N + at / nv * 4) = s;
+        }
     }
 }
 
@@ -460,99 +590,138 @@ template <typename T>
 __global__ void __launch_bounds__(kAnyThreads) k_blocknorm_bwd_any(const Args a)
 {
     griddep_start();
-    __shared__ __align__(16) float red[2 * 6 * 32];
+    __shared__ __align__(16) float red[2 * 8 * 32];
     int turn = 0;
     float *pre = a.part_pre + (int64_t)blockIdx.x * a.d, *post = a.part_post + (int64_t)blockIdx.x * a.d;
     for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
         pre[j] = post[j] = 0.f;
-    for (int64_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-        const int64_t i = c / a.split, in = c - i * a.split;
-        const int64_t t0 = i * a.per_gate + in * a.rows, t1 = min(t0 + a.rows, (i + 1) * a.per_gate);
-        float *to = !a.gate ? nullptr : a.split > 1 ? a.part_gate + c * a.d : a.dgate + i * a.d;
-        if (to && (a.split > 1 || !a.add))
+    const int64_t t1 = first_token(blockIdx.x + 1, gridDim.x, a.T);
+    for (int64_t t = first_token(blockIdx.x, gridDim.x, a.T); t < t1;) {
+        const int64_t i = a.gated ? gate_of(a, t) : 0, end = a.gated ? min(t1, (i + 1) * a.per_gate) : t1;
+        const bool whole = end - t == a.per_gate;
+        float *to = !a.gated ? nullptr : whole ? a.dgate + i * a.d : a.part_gate + (blockIdx.x + i) * a.d;
+        if (to && !(whole && a.add))
             for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
                 to[j] = 0.f;
-        for (int64_t t = t0; t < t1; ++t) {
+        for (; t < end; ++t) {
             const T *H = (const T *)a.R + t * a.d, *Y = (const T *)a.Y + t * a.ldy, *dZ = (const T *)a.dZ + t * a.lddz;
             const T *dH = a.dH ? (const T *)a.dH + t * a.d : nullptr;
-            Sums m;
+            float m[6];
             Row row;
-            row.fh = row.fy = 1.f;
             auto m_at = [&](int j) { return a.scale * (gate_at<T>(a, i, j) * weight_at(a.post, j)); };
-            while (true) {
-                for (int k = 0; k < 6; ++k)
-                    m.s[k] = 0.f;
+            do {
+                Sums<float> sums = {};
                 for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
-                    m.add(Vec<T>::one(H[j]) * row.fh, Vec<T>::one(dZ[j]) * weight_at(a.pre, j),
-                          Vec<T>::one(Y[j]) * row.fy, m_at(j), dH ? Vec<T>::one(dH[j]) : 0.f);
-                row_reduce<kAnyThreads, 6, false, true>(m.s, red, turn);
-                const bool h_again = row.fh == 1.f && !in_range(a, m.s[0]);
-                const bool y_again = row.fy == 1.f && !in_range(a, m.s[2]);
-                if (!(h_again || y_again))
-                    break;
-                if (h_again)
-                    row.fh = factor_of(a, m.s[0]);
-                if (y_again)
-                    row.fy = factor_of(a, m.s[2]);
-            }
-            row.finish(a, m.s);
+                    add_element(sums, Vec<T>::one(H[j]) * row.fh, Vec<T>::one(dZ[j]), Vec<T>::one(Y[j]) * row.fy,
+                                dH ? Vec<T>::one(dH[j]) : 0.f, weight_at(a.pre, j), m_at(j));
+                for (int k = 0; k < 6; ++k)
+                    m[k] = sums.s[k];
+                row_sums<kAnyThreads>(m, red, turn);
+            } while (row.again(a, m));
+            row.finish(a, m);
             for (int j = threadIdx.x; j < a.d; j += kAnyThreads) {
-                const float z = Vec<T>::one(dZ[j]), w = weight_at(a.post, j);
-                float dh, dy, n1, n2;
-                row.element(Vec<T>::one(H[j]) * row.fh, z * weight_at(a.pre, j), Vec<T>::one(Y[j]) * row.fy, m_at(j),
-                            dH ? Vec<T>::one(dH[j]) : 0.f, dh, dy, n1, n2);
+                float dh, dy, s = 0.f, p = pre[j];
+                row.element(Vec<T>::one(H[j]) * row.fh, Vec<T>::one(dZ[j]), Vec<T>::one(Y[j]) * row.fy,
+                            dH ? Vec<T>::one(dH[j]) : 0.f, weight_at(a.pre, j), m_at(j), dh, dy, p, s);
                 ((T *)a.H)[t * a.d + j] = Vec<T>::round(dh);
                 ((T *)a.Z)[t * a.d + j] = Vec<T>::round(dy);
-                pre[j] = fmaf(z, n2, pre[j]);
-                post[j] = fmaf(a.scale * gate_at<T>(a, i, j), dh * n1, post[j]);
+                pre[j] = p;
+                post[j] = fmaf(a.gated ? a.scale * gate_at<T>(a, i, j) : 1.f, s, post[j]);
                 if (to)
-                    to[j] = fmaf(a.split > 1 ? 1.f : a.scale * w, dh * n1, to[j]);
+                    to[j] = fmaf(whole ? a.scale * weight_at(a.post, j) : 1.f, s, to[j]);
             }
         }
     }
 }
 
-// The sums of parts, in their order: 32 columns and 32 runs of parts a block, so that the result
-// is the same bits every time.  blockIdx.y: dw_pre, dw_post, then the gates whose tokens were split.
+// The sums of the workers' parts, in their order, so that the result is the same bits every time.
 struct JoinArgs {
     const float *pre, *post, *gate;
+    int pre_parts, post_parts;
     float *dw_pre, *dw_post, *dgate;
     Weight w_post;
+    const void *one_gate;       // the gate where it is one row for all tokens, in T
+    bool one_bf16;
     float scale;
-    int parts, split, d;
-    int64_t gates;          // rows of dgate that are joined
+    int d;
+    int64_t T, workers, gates, per_gate, looked;
+    int runs;
     bool add;
 };
-__global__ void __launch_bounds__(1024) k_blocknorm_join(const JoinArgs a)
+// dw_pre and dw_post (blockIdx.y): 32 columns and 32 runs of parts a block.  Where S is one for all
+// tokens, it makes dw_post and dgate.
+__global__ void __launch_bounds__(1024) k_blocknorm_dw(const JoinArgs a)
 {
     griddep_start();
     __shared__ float red[32][33];
-    for (int64_t y = blockIdx.y; y < 2 + a.gates; y += gridDim.y) {
-        const float *part = y == 0 ? a.pre : y == 1 ? a.post : a.gate + (y - 2) * a.split * a.d;
-        const int parts = y < 2 ? a.parts : a.split, per = (parts + 31) / 32;
-        const int j = blockIdx.x * 32 + threadIdx.x;
-        float s = 0.f;
-        if (j < a.d)
+    const float *part = blockIdx.y == 0 ? a.pre : a.post;
+    const int parts = blockIdx.y == 0 ? a.pre_parts : a.post_parts, per = (parts + 31) / 32;
+    const int j = blockIdx.x * 32 + threadIdx.x;
+    float s = 0.f;
+    if (j < a.d)
 #pragma unroll 8
-            for (int p = threadIdx.y * per, end = min(parts, p + per); p < end; ++p)
-                s += __ldg(part + (int64_t)p * a.d + j);
-        red[threadIdx.y][threadIdx.x] = s;
-        __syncthreads();
-        s = warp_sum(red[threadIdx.x][threadIdx.y]);
-        const int c = blockIdx.x * 32 + threadIdx.y;
-        if (threadIdx.x == 0 && c < a.d) {
-            float *to = y == 0 ? a.dw_pre : y == 1 ? a.dw_post : a.dgate + (y - 2) * a.d;
-            if (y >= 2)
-                s *= a.scale * weight_at(a.w_post, c);
-            to[c] = a.add ? to[c] + s : s;
+        for (int p = threadIdx.y * per, end = min(parts, p + per); p < end; ++p)
+            s += __ldg(part + (int64_t)p * a.d + j);
+    red[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    s = warp_sum(red[threadIdx.x][threadIdx.y]);       // row y of the transpose: column y
+    const int c = blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x > 0 || c >= a.d)
+        return;
+    if (blockIdx.y == 1 && a.gates <= 1) {
+        s *= a.scale;
+        if (a.one_gate) {
+            const float g = s * weight_at(a.w_post, c);
+            a.dgate[c] = a.add ? a.dgate[c] + g : g;
+            s *= weight_at(Weight{a.one_gate, a.one_bf16}, c);
         }
-        __syncthreads();
+    }
+    float *to = (blockIdx.y == 0 ? a.dw_pre : a.dw_post) + c;
+    *to = a.add ? *to + s : s;
+}
+// The gates whose tokens several workers had, looked for among all gates, or with more gates than
+// workers among those in which a worker's tokens start.  A warp sums 32 columns of a gate's parts, or
+// 8 warps do where a gate has many.
+__global__ void __launch_bounds__(256) k_blocknorm_dgate(const JoinArgs a)
+{
+    griddep_start();
+    __shared__ float red[8][32];
+    const int at_once = 8 / a.runs, run = threadIdx.y % a.runs, j = blockIdx.x * 32 + threadIdx.x;
+    for (int64_t y0 = (int64_t)blockIdx.y * at_once; y0 < a.looked; y0 += (int64_t)gridDim.y * at_once) {
+        const int64_t y = y0 + threadIdx.y / a.runs;
+        float s = 0.f, *to = nullptr;
+        if (y < a.looked && j < a.d) {
+            const int64_t i = a.looked == a.gates ? y : first_token(y + 1, a.workers, a.T) / a.per_gate;
+            const int64_t w0 = worker_of(i * a.per_gate, a.workers, a.T);
+            const int64_t w1 = worker_of((i + 1) * a.per_gate - 1, a.workers, a.T);
+            if (w0 < w1 && (a.looked == a.gates || w0 == y)) {       // not one worker's, nor another warp's
+                to = a.dgate + i * a.d + j;
+                const float *part = a.gate + (w0 + i) * a.d + j;
+                const int parts = (int)(w1 - w0 + 1), per = (parts + a.runs - 1) / a.runs;
+#pragma unroll 8
+                for (int p = run * per, end = min(parts, p + per); p < end; ++p)
+                    s += __ldg(part + (int64_t)p * a.d);
+            }
+        }
+        if (a.runs > 1) {
+            red[threadIdx.y][threadIdx.x] = s;
+            __syncthreads();
+            s = 0.f;
+            if (run == 0)
+                for (int r = 0; r < a.runs; ++r)
+                    s += red[threadIdx.y + r][threadIdx.x];
+            __syncthreads();
+        }
+        if (to && run == 0) {
+            s *= a.scale * weight_at(a.w_post, j);
+            *to = a.add ? *to + s : s;
+        }
     }
 }
 
 // ---- launches ------------------------------------------------------------------------------------
 
-constexpr int kPieces = 4, kBwdPieces = 2;
+constexpr int kPieces = 4;
 
 template <typename T>
 bool pieces(int d, int64_t ld, int most)
@@ -580,6 +749,8 @@ cudaError_t fwd(const Args &a, cudaStream_t s)
         return nv <= 32 ? fwd_rows<T, 32, false, 1>(a, g, s)
              : nv <= 64 ? fwd_rows<T, 32, false, 2>(a, g, s)
                         : fwd_rows<T, 32, false, kPieces>(a, g, s);
+    if (g == 64 && nv == 64 * kPieces)
+        return fwd_rows<T, 64, true, kPieces>(a, g, s);
     if (g == 128 && nv == 128 * kPieces)
         return fwd_rows<T, 128, true, kPieces>(a, g, s);
     if (g == 256 && nv == 256 * kPieces)
@@ -589,12 +760,13 @@ cudaError_t fwd(const Args &a, cudaStream_t s)
                     : fwd_rows<T, 1024, false, kPieces>(a, g, s);
 }
 
-// The gradient's grid and its division of the tokens.  Without a gate, and with one row of it, every
-// worker has one chunk; with more, a gate's tokens are divided into about four chunks a worker, of
-// at least eight tokens (a chunk writes its S).
+// Pieces a lane of wide fp32 rows holds
+constexpr int kFew = 4;
+
+// The gradient's grid
 struct Plan {
     int threads, rows_at_once;
-    int64_t workers, chunks, rows, split;
+    int64_t workers;
     size_t part, gate_parts;          // floats
 };
 
@@ -602,32 +774,27 @@ template <typename T>
 Plan plan_of(int64_t T_, int d, bool registers, int64_t gates)
 {
     Plan p;
-    const int nv = d / Vec<T>::N, sms = device_sms();
+    const int nv = d / Vec<T>::N;
     int per_sm;
     if (!registers) {
         p.threads = kAnyThreads;
         p.rows_at_once = 1;
         per_sm = 2;
     } else {
-        const int g = nv <= 64 ? 32 : lanes_of(nv, nv <= 512 ? 1 : kBwdPieces);
+        const int g = nv <= 64 ? 32 : lanes_of(nv, nv <= 512 ? 2 : sizeof(T) == 4 ? kFew : 2);
         p.threads = g == 32 ? 256 : g;
         p.rows_at_once = g == 32 ? 8 : 1;
-        per_sm = std::max(1, std::min(4, (g <= 320 && sizeof(T) == 4 ? 640 : 512) / p.threads));
+        // (bf16 rows of a little more than 256 lanes: two blocks of up to 320)
+        per_sm = std::max(1, std::min(8, (sizeof(T) == 2 && g > 256 && g <= 320 ? 640 : 512) / p.threads));
     }
-    p.workers = std::min<int64_t>((T_ + p.rows_at_once - 1) / p.rows_at_once, (int64_t)sms * per_sm) * p.rows_at_once;
-    const int64_t n = std::max<int64_t>(1, gates), per_gate = T_ / n;
-    const int64_t want = n == 1 ? (T_ + p.workers - 1) / p.workers
-                                : std::max<int64_t>(8, (T_ + 4 * p.workers - 1) / (4 * p.workers));
-    p.rows = std::min(want, per_gate);
-    p.split = (per_gate + p.rows - 1) / p.rows;
-    p.chunks = n * p.split;
+    p.workers = std::min<int64_t>(T_, (int64_t)device_sms() * per_sm * p.rows_at_once);
     p.part = (size_t)p.workers * d;
-    p.gate_parts = gates > 0 && p.split > 1 ? (size_t)p.chunks * d : 0;
+    p.gate_parts = gates > 1 ? (size_t)(p.workers + gates) * d : 0;
     return p;
 }
 
 template <typename T>
-bool bwd_registers(const Args &a) { return pieces<T>(a.d, a.ldy, kBwdPieces) && a.lddz % Vec<T>::N == 0; }
+bool bwd_registers(const Args &a) { return pieces<T>(a.d, a.ldy, 2) && a.lddz % Vec<T>::N == 0; }
 
 template <typename T, int S, int C>
 cudaError_t bwd_rows(const Plan &p, const Args &a, cudaStream_t s)
@@ -638,7 +805,7 @@ cudaError_t bwd_rows(const Plan &p, const Args &a, cudaStream_t s)
     if (e != cudaSuccess)
         return e;
     count_launch();
-    e = launch_dependent(k_blocknorm_bwd<T, S, C>, dim3((unsigned)(p.workers / p.rows_at_once)), dim3(p.threads), smem,
+    e = launch_dependent(k_blocknorm_bwd<T, S, C>, dim3((unsigned)((p.workers + p.rows_at_once - 1) / p.rows_at_once)), dim3(p.threads), smem,
                          s, a);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -648,9 +815,8 @@ cudaError_t bwd(Args a, int64_t gates, float *dw_post, float *dw_pre, float *ws,
 {
     const bool registers = bwd_registers<T>(a);
     const Plan p = plan_of<T>(a.T, a.d, registers, gates);
-    a.chunks = p.chunks;
-    a.rows = p.rows;
-    a.split = p.split;
+    a.workers = p.workers;
+    a.gated = gates > 1;
     a.part_pre = ws;
     a.part_post = ws + p.part;
     a.part_gate = ws + 2 * p.part;
@@ -661,20 +827,29 @@ cudaError_t bwd(Args a, int64_t gates, float *dw_post, float *dw_pre, float *ws,
     else if (p.rows_at_once > 1)
         e = nv <= 32 ? bwd_rows<T, 32, 1>(p, a, s) : bwd_rows<T, 32, 2>(p, a, s);
     else if (nv <= 512)
-        e = p.threads <= 256 ? bwd_rows<T, 256, 1>(p, a, s) : bwd_rows<T, 512, 1>(p, a, s);
-    else if (sizeof(T) == 4 && p.threads <= 320)
-        e = bwd_rows<T, 320, kBwdPieces>(p, a, s);
+        e = bwd_rows<T, 256, 2>(p, a, s);
+    else if constexpr (sizeof(T) == 4)
+        e = p.threads <= 256 ? bwd_rows<T, 256, kFew>(p, a, s) : bwd_rows<T, 512, kFew>(p, a, s);
     else
-        e = p.threads <= 512 ? bwd_rows<T, 512, kBwdPieces>(p, a, s) : bwd_rows<T, 1024, kBwdPieces>(p, a, s);
+        e = p.threads <= 320   ? bwd_rows<T, 320, 2>(p, a, s)
+            : p.threads <= 512 ? bwd_rows<T, 512, 2>(p, a, s)
+                               : bwd_rows<T, 1024, 2>(p, a, s);
     if (e != cudaSuccess)
         return e;
-    const int64_t joined = p.gate_parts ? gates : 0;
-    const JoinArgs j{a.part_pre, a.part_post, a.part_gate, dw_pre, dw_post, a.dgate, a.post, a.scale,
-                     (int)p.workers, (int)p.split, a.d, joined, a.add};
+    const int64_t looked = gates > 1 ? std::min(gates, p.workers - 1) : 0;
+    const int blocks = (int)((p.workers + p.rows_at_once - 1) / p.rows_at_once);
+    const JoinArgs j{a.part_pre, a.part_post, a.part_gate, blocks, gates > 1 ? (int)p.workers : blocks, dw_pre, dw_post,
+                     a.dgate, a.post, gates == 1 ? a.gate : nullptr, sizeof(T) == 2, a.scale, a.d, a.T, p.workers,
+                     gates, a.per_gate, looked, p.workers >= 8 * gates ? 8 : 1, a.add};
+    const unsigned across = (unsigned)((a.d - 1) / 32 + 1);
     count_launch();
-    e = launch_dependent(k_blocknorm_join, dim3((unsigned)((a.d - 1) / 32 + 1),
-                                                (unsigned)std::min<int64_t>(2 + joined, 65535)),
-                         dim3(32, 32), 0, s, j);
+    e = launch_dependent(k_blocknorm_dw, dim3(across, 2), dim3(32, 32), 0, s, j);
+    if (e == cudaSuccess && looked > 0) {
+        count_launch();
+        e = launch_dependent(k_blocknorm_dgate,
+                             dim3(across, (unsigned)std::min<int64_t>((looked * j.runs + 7) / 8, 65535)), dim3(32, 8),
+                             0, s, j);
+    }
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -694,6 +869,7 @@ cudaError_t blocknorm_fwd(sn_dtype dt, const void *Y, int64_t ldy, const void *R
     a.ldy = ldy;
     a.per_gate = T / std::max<int64_t>(1, gates);
     a.d = d;
+    a.inverse_d = 1.f / (float)d;
     a.eps = eps;
     a.scale = scale;
     a.least = least_sum(d, eps);
@@ -709,9 +885,9 @@ size_t blocknorm_bwd_workspace(int64_t T, int d, int64_t gates)
     size_t most = 0;
     auto take = [&](const Plan &p) { most = std::max(most, 2 * p.part + p.gate_parts); };
     take(plan_of<float>(T, d, false, gates));
-    if (pieces<float>(d, d, kBwdPieces))
+    if (pieces<float>(d, d, 2))
         take(plan_of<float>(T, d, true, gates));
-    if (pieces<__nv_bfloat16>(d, d, kBwdPieces))
+    if (pieces<__nv_bfloat16>(d, d, 2))
         take(plan_of<__nv_bfloat16>(T, d, true, gates));
     return most * sizeof(float);
 }
@@ -734,6 +910,7 @@ cudaError_t blocknorm_bwd(sn_dtype dt, const void *dZ, int64_t lddz, const void 
     a.lddz = lddz;
     a.per_gate = T / std::max<int64_t>(1, gates);
     a.d = d;
+    a.inverse_d = 1.f / (float)d;
     a.eps = eps;
     a.scale = scale;
     a.least = least_sum(d, eps);
