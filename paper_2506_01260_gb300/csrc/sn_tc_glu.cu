@@ -146,11 +146,9 @@ __device__ __forceinline__ void arrive_leader(uint32_t bar)
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders(bar))
                      : "memory");
 }
-template <int CG>
-__device__ __forceinline__ bool test(uint32_t bar, uint32_t parity)
+// Whether a phase has completed, with acquire semantics toward the other CTA's threads too
+__device__ __forceinline__ bool mbar_test_cluster(uint32_t bar, uint32_t parity)
 {
-    if (CG == 1)
-        return mbar_test(bar, parity);
     uint32_t ok;
     asm volatile(
         "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; "
@@ -160,37 +158,58 @@ __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// A bounded wait as mbar_wait's; `err` may be null
-template <int CG>
+// A bounded wait of a whole warp, as warp_wait's; `err` may be null.  The votes tell the compiler
+// that the warp stays together.  CLUSTER: for what the other CTA's threads have done.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *abort, unsigned int *err)
 {
-    if (test<CG>(bar, parity))
+    const auto test = [&] {
+        return __all_sync(0xffffffffu, CLUSTER ? mbar_test_cluster(bar, parity) : mbar_test(bar, parity));
+    };
+    if (test())
         return true;
     const uint64_t t0 = global_ns();
     while (true) {
-        if (test<CG>(bar, parity))
+        if (test())
             return true;
-        if (*abort)
+        if (__any_sync(0xffffffffu, *abort))
             return false;
-        if (global_ns() - t0 > kWaitLimitNs) {
+        if (__any_sync(0xffffffffu, global_ns() - t0 > kWaitLimitNs)) {
             *abort = 1;
-            if (err)
+            if (err && threadIdx.x % 32 == 0)
                 atomicOr(err, SN_EBIT_TIMEOUT);
             return false;
         }
     }
 }
-template <int CG>
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int *abort, unsigned int *err)
+// Whether a phase has completed, without waiting at all
+__device__ __forceinline__ uint32_t peek(uint32_t bar, uint32_t parity)
 {
-    int ok = 1;
-    if ((threadIdx.x & 31) == 0)
-        ok = wait<CG>(bar, parity, abort, err);
-    ok = __shfl_sync(0xffffffffu, ok, 0);
-    if (ok && (threadIdx.x & 31))
-        test<CG>(bar, parity);
-    return ok != 0;
+    uint32_t ok;
+    asm volatile(
+        "{ .reg .pred p; mbarrier.test_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2; "
+        "selp.u32 %0, 1, 0, p; }"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok;
 }
+// One lane of the warp
+__device__ __forceinline__ bool elected()
+{
+    uint32_t is;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(is));
+    return is != 0;
+}
+
+// A stage operand's descriptor at 16-element step kk (see sdesc_sw128, sdesc_mn_sw128): 32 bytes on in
+// a K-major row, two groups of 8 rows on in MN-major tiles
+template <bool MN>
+__device__ __forceinline__ uint64_t step_desc(uint32_t at, int kk)
+{
+    return MN ? sdesc_mn_sw128(at + kk * 2048, 8192, 1024) : sdesc_sw128(at + kk * 32);
+}
+
 // Instruction descriptor as idesc_bf16's, with either operand MN-major
 constexpr uint32_t idesc_of(int M, int N, bool a_mn, bool b_mn)
 {
@@ -201,7 +220,8 @@ constexpr uint32_t idesc_of(int M, int N, bool a_mn, bool b_mn)
 
 constexpr int kRows = 128, kCols = 256, kK = 64;
 constexpr uint32_t kABytes = kRows * kK * 2;
-constexpr int kEpilogueWarps = 4;
+constexpr int kEpilogueWarps = 8;
+constexpr uint32_t kOutBytes = 32 * 128;       // an epilogue warp's rows of 128 bytes of an output
 constexpr int kGluThreads = 64 + 32 * kEpilogueWarps;
 
 template <int CG>
@@ -209,12 +229,13 @@ struct Stage {
     static constexpr uint32_t kBBytes = kCols / CG * kK * 2;
     static constexpr uint32_t kBytes = kABytes + kBBytes;      // of one CTA
     static constexpr int kStages = CG == 1 ? 4 : 6;
-    static constexpr uint32_t kSmem = kStages * kBytes + 1024 /* alignment */ + 256 /* barriers */;
+    static constexpr uint32_t kOut = kStages * kBytes, kBar = kOut + kEpilogueWarps * kOutBytes;
+    static constexpr uint32_t kSmem = kBar + 1024 /* alignment */ + 256 /* barriers */;
 };
 static_assert(Stage<1>::kSmem <= 232448 && Stage<2>::kSmem <= 232448, "shared memory of a CTA");
 
 struct GluParams {
-    CUtensorMap A[2], B[2];
+    CUtensorMap A[2], B[2], out[3];
     int64_t rows;           // of an output
     int cols;               // of an output (the forward: f)
     int64_t mt;             // tiles along the rows and the columns
@@ -223,8 +244,8 @@ struct GluParams {
     int64_t chunks;         // of 64 along a product's inner dimension
     int act;
     bool add;               // to what the output holds
-    bool out_f32;
-    void *out[3];           // forward: H, G, U (G and U may be null); else the outputs
+    bool out_f32, keep;     // dW's type; whether the forward stores G and U
+    void *at[2];            // dW, where it is added to
     unsigned int *err;
 };
 
@@ -253,50 +274,61 @@ __device__ __forceinline__ Item item_at(const GluParams &p, int64_t i)
     return t;
 }
 
-// 16 columns of a row, from `col` on, as bf16 or fp32
-__device__ __forceinline__ void store_bf16(__nv_bfloat16 *row, int col, int cols, const float (&v)[16])
+// Two fours of packed bf16 pairs, or eight fp32, of a warp's row `lane` at 16-byte pieces `c` and on
+// of its 128 bytes
+__device__ __forceinline__ void stage(uint32_t out, int lane, int c, const uint32_t *w)
+{
+    sts128(out + sw128(lane, c), make_uint4(w[0], w[1], w[2], w[3]));
+    sts128(out + sw128(lane, c + 1), make_uint4(w[4], w[5], w[6], w[7]));
+}
+__device__ __forceinline__ void pack16(const float (&v)[16], uint32_t *w)
 {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-        if (col + 8 * h < cols) {
-            uint4 w;
-            w.x = pack_bf16(v[8 * h], v[8 * h + 1]);
-            w.y = pack_bf16(v[8 * h + 2], v[8 * h + 3]);
-            w.z = pack_bf16(v[8 * h + 4], v[8 * h + 5]);
-            w.w = pack_bf16(v[8 * h + 6], v[8 * h + 7]);
-            *(uint4 *)(row + col + 8 * h) = w;
-        }
+    for (int j = 0; j < 8; ++j)
+        w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+}
+// The warp's 32 rows of 128 bytes go to the output's box at (x, y); what lies past its edges stays
+__device__ __forceinline__ void send(const CUtensorMap *m, uint32_t out, int lane, int x, int64_t y, bool in)
+{
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0 && in) {
+        tma_store_2d(m, out, x, (int)y);
+        bulk_commit();
+    }
+}
+// The staging rows have been read and may be written again
+__device__ __forceinline__ void sent(int lane)
+{
+    if (lane == 0)
+        bulk_wait_read0();
+    __syncwarp();
 }
 
-template <int MODE>
-__device__ __forceinline__ void put(const GluParams &p, int which, int64_t row, int col, float (&v)[16])
+// 16 columns of dW added to what it holds
+__device__ __forceinline__ void add_to(const GluParams &p, int which, int64_t row, int col, const float (&v)[16])
 {
-    if (MODE == GLU_DW && p.out_f32) {
-        float *at = (float *)p.out[which] + row * p.cols + col;
+    if (p.out_f32) {
+        float *at = (float *)p.at[which] + row * p.cols + col;
 #pragma unroll
         for (int j = 0; j < 16; j += 4)
             if (col + j < p.cols) {
-                float4 x = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                if (p.add) {
-                    const float4 y = *(const float4 *)(at + j);
-                    x = make_float4(y.x + x.x, y.y + x.y, y.z + x.z, y.w + x.w);
-                }
-                *(float4 *)(at + j) = x;
+                const float4 y = *(const float4 *)(at + j);
+                *(float4 *)(at + j) = make_float4(y.x + v[j], y.y + v[j + 1], y.z + v[j + 2], y.w + v[j + 3]);
             }
         return;
     }
-    __nv_bfloat16 *at = (__nv_bfloat16 *)p.out[which] + row * p.cols;
-    if (MODE == GLU_DW && p.add)
+    __nv_bfloat16 *at = (__nv_bfloat16 *)p.at[which] + row * p.cols + col;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (col + 8 * h < p.cols) {
-                float y[8];
-                Vec<__nv_bfloat16>::unpack(*(const uint4 *)(at + col + 8 * h), y);
+    for (int j = 0; j < 16; j += 8)
+        if (col + j < p.cols) {
+            float y[8];
+            Vec<__nv_bfloat16>::unpack(*(const uint4 *)(at + j), y);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    v[8 * h + j] += y[j];
-            }
-    store_bf16(at, col, p.cols, v);
+            for (int k = 0; k < 8; ++k)
+                y[k] += v[j + k];
+            *(uint4 *)(at + j) = Vec<__nv_bfloat16>::pack(y);
+        }
 }
 
 template <int MODE, int CG>
@@ -308,10 +340,10 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
     uint32_t base = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
     base += pad;
-    const uint32_t bar = base + S * St::kBytes;
+    const uint32_t bar = base + St::kBar;
     const uint32_t full_b = bar, empty_b = bar + 8 * S, accf_b = bar + 16 * S, acce_b = accf_b + 16,
                    drain_b = acce_b + 16;
-    uint32_t *tmem_slot = (uint32_t *)(smem_raw + pad + S * St::kBytes + 8 * (2 * S + 5));
+    uint32_t *tmem_slot = (uint32_t *)(smem_raw + pad + St::kBar + 8 * (2 * S + 5));
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 1 ? 0 : cluster_rank();
@@ -344,30 +376,33 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
     const int64_t first = blockIdx.x / CG, step = gridDim.x / CG;
     constexpr int kSegments = MODE == GLU_DX ? 2 : 1;
 
+    // A warp issues copies and one issues products: all its lanes walk the loop and one is elected
+    // at each issue, so that what the instructions read is the warp's alike and lies in uniform
+    // registers.  (With one lane in the loop, a chunk's four products took that lane 630 cycles to
+    // issue, and the tensor cores 512 to do.)
     if (warp == 0) {
         // ---------------------------------------------------------------- TMA producer
-        if (lane == 0) {
-            Ring ring;
-            int64_t g = 0;
-            bool ok = true;
-            for (int64_t i = first; i < p.items && ok; i += step) {
-                const Item t = item_at<MODE, CG>(p, i);
-                const int m = (int)t.m0 + kRows * (int)rank;
-                const int n = MODE == GLU_FWD ? t.n0 : t.n0 + (kCols / CG) * (int)rank;
-                for (int seg = 0; seg < kSegments && ok; ++seg)
-                    for (int64_t c = 0; c < p.chunks; ++c, ++g, ring.next(S)) {
-                        if (!wait<CG>(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
-                            ok = false;
-                            break;
-                        }
-                        const uint32_t a = base + ring.s * St::kBytes, b = a + kABytes;
-                        uint32_t fb = full_b + 8 * ring.s;
+        Ring ring;
+        int64_t g = 0;
+        bool ok = true;
+        for (int64_t i = first; i < p.items && ok; i += step) {
+            const Item t = item_at<MODE, CG>(p, i);
+            const int m = (int)t.m0 + kRows * (int)rank;
+            const int n = MODE == GLU_FWD ? t.n0 : t.n0 + (kCols / CG) * (int)rank;
+            for (int seg = 0; seg < kSegments && ok; ++seg)
+                for (int64_t c = 0; c < p.chunks; ++c, ++g, ring.next(S)) {
+                    if (!wait(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t a = base + ring.s * St::kBytes, b = a + kABytes;
+                    const uint32_t own = full_b + 8 * ring.s, fb = CG == 2 ? leaders(own) : own;
+                    const int k = (int)c * kK;
+                    if (elected()) {
                         if (rank == 0)
-                            mbar_arrive_tx(fb, CG * St::kBytes);
-                        if (CG == 2)
-                            fb = leaders(fb);
-                        const int k = (int)c * kK;
+                            mbar_arrive_tx(own, CG * St::kBytes);
                         if (MODE == GLU_DW) {
+#pragma unroll
                             for (int j = 0; j < 2; ++j)
                                 load_tile<CG>(a + 8192 * j, &p.A[t.which], m + 64 * j, k, fb);
                         } else {
@@ -381,51 +416,63 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
                                 load_tile<CG>(b + 16384, &p.B[1], k, n, fb);
                             }
                         } else {
+#pragma unroll
                             for (int j = 0; j < 4 / CG; ++j)
                                 load_tile<CG>(b + 8192 * j, &p.B[seg], n + 64 * j, k, fb);
                         }
                     }
-            }
-            if (!ok && rank == 0)      // copies already issued land before the CTAs exit
-                for (int64_t j = g > S ? g - S : 0; j < g; ++j)
-                    drain_wait(full_b + 8 * (uint32_t)(j % S), (uint32_t)(j / S) & 1);
+                    __syncwarp();
+                }
         }
+        if (!ok && rank == 0 && lane == 0)     // copies already issued land before the CTAs exit
+            for (int64_t j = g > S ? g - S : 0; j < g; ++j)
+                drain_wait(full_b + 8 * (uint32_t)(j % S), (uint32_t)(j / S) & 1);
         __syncwarp();
     } else if (warp == 1) {
         // ---------------------------------------------------------------- products
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             constexpr bool kAmn = MODE == GLU_DW, kBmn = MODE != GLU_FWD;
             constexpr uint32_t idesc = idesc_of(kRows * CG, kCols, kAmn, kBmn);
             Ring ring;
-            uint32_t it = 0;
+            uint32_t it = 0, ready = 0;
             bool ok = true;
             for (int64_t i = first; i < p.items && ok; i += step, ++it) {
                 const uint32_t b = it & 1, nb = it >> 1;
-                if (!wait<CG>(acce_b + 8 * b, (nb & 1) ^ 1, abort_flag, p.err)) {
+                if (!wait<CG == 2>(acce_b + 8 * b, (nb & 1) ^ 1, abort_flag, p.err)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem + b * kCols;
-                for (int64_t c = 0; c < p.chunks * kSegments; ++c, ring.next(S)) {
-                    if (!wait<CG>(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
+                for (int64_t c = 0; c < p.chunks * kSegments; ++c) {
+                    if (!__all_sync(0xffffffffu, ready) && !wait(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t a = base + ring.s * St::kBytes, w = a + kABytes;
+                    const uint32_t a = base + ring.s * St::kBytes, w = a + kABytes, done = empty_b + 8 * ring.s;
+                    // the next stage is looked at ahead of this one's products, which hide the look
+                    ring.next(S);
+                    ready = peek(full_b + 8 * ring.s, ring.ph);
+                    uint64_t ad[kK / 16], bd[kK / 16];
 #pragma unroll
                     for (int kk = 0; kk < kK / 16; ++kk) {
-                        const uint64_t ad = kAmn ? sdesc_mn_sw128(a + kk * 2048, 8192, 1024) : sdesc_sw128(a + kk * 32);
-                        const uint64_t bd = kBmn ? sdesc_mn_sw128(w + kk * 2048, 8192, 1024) : sdesc_sw128(w + kk * 32);
-                        multiply<CG>(d_tmem, ad, bd, idesc, c > 0 || kk > 0 ? 1u : 0u);
+                        ad[kk] = step_desc<kAmn>(a, kk);
+                        bd[kk] = step_desc<kBmn>(w, kk);
                     }
-                    commit<CG>(empty_b + 8 * ring.s);
+                    if (elected()) {
+#pragma unroll
+                        for (int kk = 0; kk < kK / 16; ++kk)
+                            multiply<CG>(d_tmem, ad[kk], bd[kk], idesc, c > 0 || kk > 0 ? 1u : 0u);
+                        commit<CG>(done);
+                    }
+                    __syncwarp();
                 }
-                if (ok)
+                if (ok && elected())
                     commit<CG>(accf_b + 8 * b);
+                __syncwarp();
             }
-            if (!ok) {                 // products already issued end before TMEM is freed
+            if (!ok && lane == 0) {    // products already issued end before TMEM is freed
                 commit<CG>(drain_b);
                 drain_wait(drain_b, 0);
             }
@@ -433,51 +480,108 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- epilogue
-        const int q = warp & 3;        // TMEM lane quarter of this warp
+        // A warp has 32 rows (its TMEM lane quarter) and half of the columns, and sends 128 bytes
+        // of its rows at a time through its staging rows: stored by the threads, a row each, the
+        // outputs took 5 to 10% of the products' time.
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t out = base + St::kOut + (warp - 2) * kOutBytes;
         uint32_t it = 0;
         for (int64_t i = first; i < p.items; i += step, ++it) {
             const Item t = item_at<MODE, CG>(p, i);
             const uint32_t b = it & 1, nb = it >> 1;
-            if (!wait_warp<CG>(accf_b + 8 * b, nb & 1, abort_flag, p.err))
+            if (!wait(accf_b + 8 * b, nb & 1, abort_flag, p.err))
                 break;
             tc_fence_after();
             const uint32_t taddr = tmem + b * kCols + ((uint32_t)(32 * q) << 16);
-            const int64_t row = t.m0 + kRows * rank + 32 * q + lane;
-            const bool in = row < p.rows;
+            const int64_t row0 = t.m0 + kRows * rank + 32 * q;
+            const auto release = [&] {          // the accumulator has been read
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    arrive_leader<CG>(acce_b + 8 * b);
+            };
             if (MODE == GLU_FWD) {
-                for (int c = 0; c < kCols / 2; c += 16) {
+                const int col = t.n0 + 64 * half;
+                const bool in = row0 < p.rows && col < p.cols;
+                uint32_t gw[32], uw[32];
+                sent(lane);
+#pragma unroll
+                for (int c = 0; c < 64; c += 16) {
                     float g[16], u[16];
-                    __syncwarp();
-                    tmem_ld16(taddr + c, g);
-                    tmem_ld16(taddr + kCols / 2 + c, u);
+                    tmem_ld16(taddr + 64 * half + c, g);
+                    tmem_ld16(taddr + kCols / 2 + 64 * half + c, u);
                     tmem_ld_wait();
-                    const int col = t.n0 + c;
-                    if (!in || col >= p.cols)
-                        continue;
-                    if (p.out[1]) {
-                        store_bf16((__nv_bfloat16 *)p.out[1] + row * p.cols, col, p.cols, g);
-                        store_bf16((__nv_bfloat16 *)p.out[2] + row * p.cols, col, p.cols, u);
+                    if (p.keep) {
+                        pack16(g, gw + c / 2);
+                        pack16(u, uw + c / 2);
                     }
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         g[j] = activate<false>(g[j], p.act, nullptr) * u[j];
-                    store_bf16((__nv_bfloat16 *)p.out[0] + row * p.cols, col, p.cols, g);
+                    uint32_t hw[8];
+                    pack16(g, hw);
+                    stage(out, lane, c / 8, hw);
                 }
-            } else {
-                for (int c = 0; c < kCols; c += 16) {
+                release();
+                send(&p.out[0], out, lane, col, row0, in);
+                if (p.keep) {
+                    sent(lane);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 16)
+                        stage(out, lane, c / 8, gw + c / 2);
+                    send(&p.out[1], out, lane, col, row0, in);
+                    sent(lane);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 16)
+                        stage(out, lane, c / 8, uw + c / 2);
+                    send(&p.out[2], out, lane, col, row0, in);
+                }
+            } else if (MODE == GLU_DW && p.add) {
+                for (int c = 128 * half; c < 128 * half + 128; c += 16) {
                     float v[16];
                     __syncwarp();
                     tmem_ld16(taddr + c, v);
                     tmem_ld_wait();
-                    if (in && t.n0 + c < p.cols)
-                        put<MODE>(p, t.which, row, t.n0 + c, v);
+                    if (row0 + lane < p.rows && t.n0 + c < p.cols)
+                        add_to(p, t.which, row0 + lane, t.n0 + c, v);
+                }
+                release();
+            } else {
+                // 128 bytes: 64 columns in bf16, 32 in fp32
+                const bool wide = MODE == GLU_DW && p.out_f32;
+                const int each = wide ? 32 : 64;
+                for (int c0 = 128 * half; c0 < 128 * half + 128; c0 += each) {
+                    const int col = t.n0 + c0;
+                    sent(lane);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 16) {
+                        if (c >= each)
+                            break;
+                        float v[16];
+                        tmem_ld16(taddr + c0 + c, v);
+                        tmem_ld_wait();
+                        if (wide) {
+                            uint32_t w[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                w[j] = __float_as_uint(v[j]);
+                            stage(out, lane, c / 4, w);
+                            stage(out, lane, c / 4 + 2, w + 8);
+                        } else {
+                            uint32_t w[8];
+                            pack16(v, w);
+                            stage(out, lane, c / 8, w);
+                        }
+                    }
+                    if (c0 + each == 128 * half + 128)
+                        release();
+                    send(&p.out[t.which], out, lane, wide ? 2 * col : col, row0, row0 < p.rows && col < p.cols);
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0)
-                arrive_leader<CG>(acce_b + 8 * b);
         }
+        if (lane == 0)
+            bulk_wait_all0();
+        __syncwarp();
     }
 
     tc_fence_before();
@@ -550,46 +654,47 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
     griddep_start();
 
     if (warp == 0) {
-        if (lane == 0) {
-            Ring ring;
-            int g = 0;
-            bool ok = true;
-            for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x)
-                for (int c = 0; c < p.chunks; ++c, ++g, ring.next(S)) {
-                    if (!wait<1>(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t at = base + ring.s * p.stage_bytes, fb = full_b + 8 * ring.s;
+        Ring ring;
+        int g = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x)
+            for (int c = 0; c < p.chunks; ++c, ++g, ring.next(S)) {
+                if (!wait(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t at = base + ring.s * p.stage_bytes, fb = full_b + 8 * ring.s;
+                if (elected()) {
                     mbar_arrive_tx(fb, p.stage_bytes);
                     tma_load_2d(at, &p.Wg, c * kK, tile * p.take, fb);
                     tma_load_2d(at + w_bytes, &p.Wu, c * kK, tile * p.take, fb);
                     tma_load_2d(at + 2 * w_bytes, &p.X, c * kK, 0, fb);
                 }
-            if (!ok)
-                for (int j = g > S ? g - S : 0; j < g; ++j)
-                    drain_wait(full_b + 8 * (uint32_t)(j % S), (uint32_t)(j / S) & 1);
-        }
+                __syncwarp();
+            }
+        if (!ok && lane == 0)
+            for (int j = g > S ? g - S : 0; j < g; ++j)
+                drain_wait(full_b + 8 * (uint32_t)(j % S), (uint32_t)(j / S) & 1);
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t idesc = idesc_bf16(128, p.n);
-            Ring ring;
-            uint32_t it = 0;
-            bool ok = true;
-            for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x, ++it) {
-                if (!wait<1>(acce_b, (it & 1) ^ 1, abort_flag, p.err)) {
+        const uint32_t idesc = idesc_bf16(128, p.n);
+        Ring ring;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x, ++it) {
+            if (!wait(acce_b, (it & 1) ^ 1, abort_flag, p.err)) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            for (int c = 0; c < p.chunks; ++c, ring.next(S)) {
+                if (!wait(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                for (int c = 0; c < p.chunks; ++c, ring.next(S)) {
-                    if (!wait<1>(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t at = base + ring.s * p.stage_bytes;
+                const uint32_t at = base + ring.s * p.stage_bytes;
+                if (elected()) {
 #pragma unroll
                     for (int kk = 0; kk < kK / 16; ++kk) {
                         const uint64_t bd = sdesc_sw128(at + 2 * w_bytes + kk * 32);
@@ -599,20 +704,22 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
                     }
                     mma_commit(empty_b + 8 * ring.s);
                 }
-                if (ok)
-                    mma_commit(accf_b);
+                __syncwarp();
             }
-            if (!ok) {
-                mma_commit(drain_b);
-                drain_wait(drain_b, 0);
-            }
+            if (ok && elected())
+                mma_commit(accf_b);
+            __syncwarp();
+        }
+        if (!ok && lane == 0) {
+            mma_commit(drain_b);
+            drain_wait(drain_b, 0);
         }
         __syncwarp();
     } else {
         const int q = warp & 3;
         uint32_t it = 0;
         for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++it) {
-            if (!wait_warp<1>(accf_b, it & 1, abort_flag, p.err))
+            if (!wait(accf_b, it & 1, abort_flag, p.err))
                 break;
             tc_fence_after();
             const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16);
@@ -702,6 +809,13 @@ cudaError_t launch_tiles(GluParams p, int sms, cudaStream_t s)
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
+// An output of `rows` rows of `cols` elements, written in boxes of 32 rows of 128 bytes; fp32 ones as
+// twice as many of 16 bits, which a copy does not tell apart
+bool out_map(CUtensorMap *m, const void *out, int cols, int64_t rows, bool f32)
+{
+    return tensor_map_2d(m, out, (uint64_t)cols * (f32 ? 2 : 1), rows, (uint64_t)cols * (f32 ? 4 : 2), 64, 32, true);
+}
+
 // Pairs of CTAs where the stream's context has the whole GPU; with a part of it a pair might find
 // no place.
 template <int MODE>
@@ -763,11 +877,11 @@ cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, 
     p.cols = f;
     p.chunks = (d + kK - 1) / kK;
     p.act = act;
-    p.out[0] = H;
-    p.out[1] = G;
-    p.out[2] = U;
+    p.keep = G != nullptr;
     p.err = err;
-    if (!tensor_map_2d(&p.A[0], X, d, T, (uint64_t)ldx * 2, kK, kRows, true) ||
+    if (!out_map(&p.out[0], H, f, T, false) || (G && (!out_map(&p.out[1], G, f, T, false) ||
+                                                       !out_map(&p.out[2], U, f, T, false))) ||
+        !tensor_map_2d(&p.A[0], X, d, T, (uint64_t)ldx * 2, kK, kRows, true) ||
         !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, kK, 128, true) ||
         !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, kK, 128, true))
         return cudaErrorInvalidValue;
@@ -796,9 +910,8 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
         p.rows = T;
         p.cols = d;
         p.chunks = (f + kK - 1) / kK;
-        p.out[0] = dX;
         p.err = err;
-        if (!tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, kK, kRows, true) ||
+        if (!out_map(&p.out[0], dX, d, T, false) || !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, kK, kRows, true) ||
             !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, kK, kRows, true) ||
             !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, 64, kK, true) ||
             !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, 64, kK, true))
@@ -810,12 +923,13 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
         p.rows = f;
         p.cols = d;
         p.chunks = (T + kK - 1) / kK;
-        p.out[0] = dWg;
-        p.out[1] = dWu;
+        p.at[0] = dWg;
+        p.at[1] = dWu;
         p.out_f32 = grad_dt == SN_F32;
         p.add = accumulate;
         p.err = err;
-        if (!tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, 64, kK, true) ||
+        if (!out_map(&p.out[0], dWg, d, f, p.out_f32) || !out_map(&p.out[1], dWu, d, f, p.out_f32) ||
+            !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, 64, kK, true) ||
             !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, 64, kK, true) ||
             !tensor_map_2d(&p.B[0], X, d, T, (uint64_t)ldx * 2, 64, kK, true))
             return cudaErrorInvalidValue;
