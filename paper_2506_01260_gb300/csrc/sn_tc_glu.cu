@@ -9,7 +9,7 @@
 // outputs and the operands of the products behind them, so they are rounded to bf16 in between, as
 // the stored G and U are: the tensor cores read 16 bits.
 #include <algorithm>
-#include <atomic>
+#include <type_traits>
 
 #include "sn_tc.cuh"
 #include "sn_tc_kernels.cuh"
@@ -28,35 +28,57 @@ __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f +
 // gelu's tanh form is g sigmoid(2 x), x = sqrt(2 / pi) (g + 0.044715 g^3)
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.044715f;
 
-// act(g); with `slope` also act'(g).  The shares p of g are taken as sigmoids and as erfc, whose
+// act(g); with SLOPE also act'(g).  The shares p of g are taken as sigmoids and as erfc, whose
 // relative error does not grow where they vanish.
-template <bool SLOPE>
-__device__ __forceinline__ float activate(float g, int act, float *slope)
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activate(float g, float &slope)
 {
-    float p;
-    switch (act) {
-    case SN_ACT_SILU:
-        p = sigmoid(g);
+    if (ACT == SN_ACT_RELU) {
         if (SLOPE)
-            *slope = fmaf(g * p, 1.f - p, p);
-        return g * p;
-    case SN_ACT_GELU:
-        p = 0.5f * erfcf(-0.7071067811865476f * g);
-        if (SLOPE)
-            *slope = fmaf(g, 0.3989422804014327f * __expf(-0.5f * g * g), p);
-        return g * p;
-    case SN_ACT_GELU_TANH:
-        p = sigmoid(kTanhA * g * fmaf(kTanhB * g, g, 1.f));
-        if (SLOPE) {
-            const float q = p * (1.f - p);                  // 0 where g^2 may pass fp32's range
-            *slope = q > 0.f ? fmaf(g * q, kTanhA * fmaf(3.f * kTanhB * g, g, 1.f), p) : p;
-        }
-        return g * p;
-    default:
-        if (SLOPE)
-            *slope = g > 0.f ? 1.f : 0.f;
+            slope = g > 0.f ? 1.f : 0.f;
         return fmaxf(g, 0.f);
     }
+    if (ACT == SN_ACT_SILU) {
+        const float p = sigmoid(g);
+        if (SLOPE)
+            slope = fmaf(g * p, 1.f - p, p);
+        return g * p;
+    }
+    if (ACT == SN_ACT_GELU) {
+        const float p = 0.5f * erfcf(-0.7071067811865476f * g);
+        if (SLOPE)
+            slope = fmaf(g, 0.3989422804014327f * __expf(-0.5f * g * g), p);
+        return g * p;
+    }
+    const float p = sigmoid(kTanhA * g * fmaf(kTanhB * g, g, 1.f));
+    if (SLOPE) {
+        const float q = p * (1.f - p);                  // 0 where g^2 may pass fp32's range
+        slope = q > 0.f ? fmaf(g * q, kTanhA * fmaf(3.f * kTanhB * g, g, 1.f), p) : p;
+    }
+    return g * p;
+}
+// F with the activation as a constant: a branch for many elements, whose chains of exponentials and
+// divisions then run beside one another (decided at each element, the epilogue of 75 tokens took 8 us)
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F f)
+{
+    switch (act) {
+    case SN_ACT_SILU: f(std::integral_constant<int, SN_ACT_SILU>()); break;
+    case SN_ACT_GELU: f(std::integral_constant<int, SN_ACT_GELU>()); break;
+    case SN_ACT_GELU_TANH: f(std::integral_constant<int, SN_ACT_GELU_TANH>()); break;
+    default: f(std::integral_constant<int, SN_ACT_RELU>()); break;
+    }
+}
+// g = act(g) u
+__device__ __forceinline__ void gate_all(float (&g)[16], const float (&u)[16], int act)
+{
+    with_activation(act, [&](auto a) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float none;
+            g[j] = activate<decltype(a)::value, false>(g[j], none) * u[j];
+        }
+    });
 }
 
 // ---- pairs of CTAs -----------------------------------------------------------------------
@@ -194,6 +216,17 @@ __device__ __forceinline__ uint32_t peek(uint32_t bar, uint32_t parity)
         : "memory");
     return ok;
 }
+// Whether `is` holds in all 256 threads of the eight epilogue warps; a barrier for them
+__device__ __forceinline__ bool all_of_eight(bool is)
+{
+    uint32_t all;
+    asm volatile(
+        "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; bar.red.and.pred q, 1, 256, p; selp.u32 %0, 1, 0, q; }"
+        : "=r"(all)
+        : "r"((uint32_t)is)
+        : "memory");
+    return all != 0;
+}
 // One lane of the warp
 __device__ __forceinline__ bool elected()
 {
@@ -240,26 +273,29 @@ struct GluParams {
     int cols;               // of an output (the forward: f)
     int64_t mt;             // tiles along the rows and the columns
     int nt;
-    int64_t items;
-    int64_t chunks;         // of 64 along a product's inner dimension
+    int64_t chunks;         // of 64 along a product's inner dimension (dX: of each of its two)
+    // Work: whole tiles, then the tiles that would leave most pairs idle, cut into runs of `run`
+    // chunks, a pair each (0: none is cut)
+    int64_t whole, cut, run;
+    float *parts;           // of cut tiles, fp32: pair u's of tile j at u + j
     int act;
     bool add;               // to what the output holds
     bool out_f32, keep;     // dW's type; whether the forward stores G and U
-    void *at[2];            // dW, where it is added to
+    void *at[2];            // dX or dW, where threads write it
     unsigned int *err;
 };
 
-struct Item {
+// Tiles run down the rows in bands, so that the tiles at work share rows and columns in L2.
+constexpr int kBand = 8;
+struct Tile {
     int which;              // dW: gate or up
     int64_t m0;
     int n0;
 };
-// Tiles run down the rows in bands, so that the tiles at work share rows and columns in L2.
-constexpr int kBand = 8;
 template <int MODE, int CG>
-__device__ __forceinline__ Item item_at(const GluParams &p, int64_t i)
+__device__ __forceinline__ Tile tile_at(const GluParams &p, int64_t i)
 {
-    Item t;
+    Tile t;
     const int64_t all = p.mt * p.nt;
     t.which = 0;
     if (MODE == GLU_DW && i >= all) {
@@ -272,6 +308,37 @@ __device__ __forceinline__ Item item_at(const GluParams &p, int64_t i)
     t.m0 = (band * kBand + in % h) * (kRows * CG);
     t.n0 = in / h * (MODE == GLU_FWD ? kCols / 2 : kCols);
     return t;
+}
+// A pair's n-th piece of work: a tile, and its chunks k0 to k1
+struct Work {
+    Tile t;
+    int64_t k0, k1, part;   // part: where its sums go, -1 where they are the output
+};
+template <int MODE, int CG>
+__device__ __forceinline__ bool work_at(const GluParams &p, int64_t n, Work &w)
+{
+    const int64_t u = blockIdx.x / CG, units = gridDim.x / CG, all = p.chunks * (MODE == GLU_DX ? 2 : 1);
+    const int64_t i = u + n * units;
+    w.k0 = 0;
+    w.k1 = all;
+    w.part = -1;
+    if (i < p.whole) {
+        w.t = tile_at<MODE, CG>(p, i);
+        return true;
+    }
+    if (MODE == GLU_FWD || p.run == 0)
+        return false;
+    // (p.whole is a multiple of units where tiles are cut)
+    const int64_t lo = u * p.run, hi = min(lo + p.run, p.cut * all);
+    const int64_t j = lo / all + (n - p.whole / units);
+    w.k0 = max(lo, j * all) - j * all;
+    w.k1 = min(hi, (j + 1) * all) - j * all;
+    if (w.k0 >= w.k1)
+        return false;
+    if (w.k1 - w.k0 < all)
+        w.part = u + j;
+    w.t = tile_at<MODE, CG>(p, p.whole + j);
+    return true;
 }
 
 // Two fours of packed bf16 pairs, or eight fp32, of a warp's row `lane` at 16-byte pieces `c` and on
@@ -373,9 +440,6 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
     const uint32_t tmem = *tmem_slot;
     griddep_start();
 
-    const int64_t first = blockIdx.x / CG, step = gridDim.x / CG;
-    constexpr int kSegments = MODE == GLU_DX ? 2 : 1;
-
     // A warp issues copies and one issues products: all its lanes walk the loop and one is elected
     // at each issue, so that what the instructions read is the warp's alike and lies in uniform
     // registers.  (With one lane in the loop, a chunk's four products took that lane 630 cycles to
@@ -385,44 +449,44 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
         Ring ring;
         int64_t g = 0;
         bool ok = true;
-        for (int64_t i = first; i < p.items && ok; i += step) {
-            const Item t = item_at<MODE, CG>(p, i);
-            const int m = (int)t.m0 + kRows * (int)rank;
-            const int n = MODE == GLU_FWD ? t.n0 : t.n0 + (kCols / CG) * (int)rank;
-            for (int seg = 0; seg < kSegments && ok; ++seg)
-                for (int64_t c = 0; c < p.chunks; ++c, ++g, ring.next(S)) {
-                    if (!wait(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t a = base + ring.s * St::kBytes, b = a + kABytes;
-                    const uint32_t own = full_b + 8 * ring.s, fb = CG == 2 ? leaders(own) : own;
-                    const int k = (int)c * kK;
-                    if (elected()) {
-                        if (rank == 0)
-                            mbar_arrive_tx(own, CG * St::kBytes);
-                        if (MODE == GLU_DW) {
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                load_tile<CG>(a + 8192 * j, &p.A[t.which], m + 64 * j, k, fb);
-                        } else {
-                            load_tile<CG>(a, &p.A[seg], k, m, fb);
-                        }
-                        if (MODE == GLU_FWD) {
-                            if (CG == 2) {
-                                load_tile<CG>(b, &p.B[rank], k, n, fb);
-                            } else {
-                                load_tile<CG>(b, &p.B[0], k, n, fb);
-                                load_tile<CG>(b + 16384, &p.B[1], k, n, fb);
-                            }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 4 / CG; ++j)
-                                load_tile<CG>(b + 8192 * j, &p.B[seg], n + 64 * j, k, fb);
-                        }
-                    }
-                    __syncwarp();
+        Work w;
+        for (int64_t i = 0; ok && work_at<MODE, CG>(p, i, w); ++i) {
+            const int m = (int)w.t.m0 + kRows * (int)rank;
+            const int n = MODE == GLU_FWD ? w.t.n0 : w.t.n0 + (kCols / CG) * (int)rank;
+            for (int64_t c = w.k0; c < w.k1; ++c, ++g, ring.next(S)) {
+                if (!wait(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
+                    ok = false;
+                    break;
                 }
+                const uint32_t a = base + ring.s * St::kBytes, b = a + kABytes;
+                const uint32_t own = full_b + 8 * ring.s, fb = CG == 2 ? leaders(own) : own;
+                const int seg = MODE == GLU_DX && c >= p.chunks;
+                const int k = (int)(seg ? c - p.chunks : c) * kK;
+                if (elected()) {
+                    if (rank == 0)
+                        mbar_arrive_tx(own, CG * St::kBytes);
+                    if (MODE == GLU_DW) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            load_tile<CG>(a + 8192 * j, &p.A[w.t.which], m + 64 * j, k, fb);
+                    } else {
+                        load_tile<CG>(a, &p.A[seg], k, m, fb);
+                    }
+                    if (MODE == GLU_FWD) {
+                        if (CG == 2) {
+                            load_tile<CG>(b, &p.B[rank], k, n, fb);
+                        } else {
+                            load_tile<CG>(b, &p.B[0], k, n, fb);
+                            load_tile<CG>(b + 16384, &p.B[1], k, n, fb);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4 / CG; ++j)
+                            load_tile<CG>(b + 8192 * j, &p.B[seg], n + 64 * j, k, fb);
+                    }
+                }
+                __syncwarp();
+            }
         }
         if (!ok && rank == 0 && lane == 0)     // copies already issued land before the CTAs exit
             for (int64_t j = g > S ? g - S : 0; j < g; ++j)
@@ -436,7 +500,8 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
             Ring ring;
             uint32_t it = 0, ready = 0;
             bool ok = true;
-            for (int64_t i = first; i < p.items && ok; i += step, ++it) {
+            Work v;
+            for (; ok && work_at<MODE, CG>(p, it, v); ++it) {
                 const uint32_t b = it & 1, nb = it >> 1;
                 if (!wait<CG == 2>(acce_b + 8 * b, (nb & 1) ^ 1, abort_flag, p.err)) {
                     ok = false;
@@ -444,7 +509,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
                 }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem + b * kCols;
-                for (int64_t c = 0; c < p.chunks * kSegments; ++c) {
+                for (int64_t c = v.k0; c < v.k1; ++c) {
                     if (!__all_sync(0xffffffffu, ready) && !wait(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
                         ok = false;
                         break;
@@ -463,7 +528,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
                     if (elected()) {
 #pragma unroll
                         for (int kk = 0; kk < kK / 16; ++kk)
-                            multiply<CG>(d_tmem, ad[kk], bd[kk], idesc, c > 0 || kk > 0 ? 1u : 0u);
+                            multiply<CG>(d_tmem, ad[kk], bd[kk], idesc, c > v.k0 || kk > 0 ? 1u : 0u);
                         commit<CG>(done);
                     }
                     __syncwarp();
@@ -485,9 +550,9 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
         // outputs took 5 to 10% of the products' time.
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t out = base + St::kOut + (warp - 2) * kOutBytes;
-        uint32_t it = 0;
-        for (int64_t i = first; i < p.items; i += step, ++it) {
-            const Item t = item_at<MODE, CG>(p, i);
+        Work w;
+        for (uint32_t it = 0; work_at<MODE, CG>(p, it, w); ++it) {
+            const Tile &t = w.t;
             const uint32_t b = it & 1, nb = it >> 1;
             if (!wait(accf_b + 8 * b, nb & 1, abort_flag, p.err))
                 break;
@@ -515,9 +580,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
                         pack16(g, gw + c / 2);
                         pack16(u, uw + c / 2);
                     }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        g[j] = activate<false>(g[j], p.act, nullptr) * u[j];
+                    gate_all(g, u, p.act);
                     uint32_t hw[8];
                     pack16(g, hw);
                     stage(out, lane, c / 8, hw);
@@ -536,6 +599,21 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
                         stage(out, lane, c / 8, uw + c / 2);
                     send(&p.out[2], out, lane, col, row0, in);
                 }
+            } else if (w.part >= 0) {
+                // lanes next to one another, four columns each
+                float *to = p.parts + w.part * (kRows * CG * kCols) + (kRows * rank + 32 * q) * kCols + 4 * lane;
+                const bool in = row0 + lane < p.rows;
+                for (int c = 128 * half; c < 128 * half + 128; c += 16) {
+                    float v[16];
+                    __syncwarp();
+                    tmem_ld16(taddr + c, v);
+                    tmem_ld_wait();
+                    if (in && t.n0 + c < p.cols)
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4)
+                            *(float4 *)(to + (c + j) * 32) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                }
+                release();
             } else if (MODE == GLU_DW && p.add) {
                 for (int c = 128 * half; c < 128 * half + 128; c += 16) {
                     float v[16];
@@ -594,25 +672,76 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
     }
 }
 
+// The sums of cut tiles' parts, in the order of their chunks.  A thread takes eight columns of a row.
+template <int MODE>
+__global__ void __launch_bounds__(256) k_glu_join(const __grid_constant__ GluParams p)
+{
+    griddep_start();
+    const int64_t all = p.chunks * (MODE == GLU_DX ? 2 : 1), j = blockIdx.y;
+    const int64_t u0 = j * all / p.run, u1 = ((j + 1) * all - 1) / p.run;
+    if (u0 == u1)                      // one pair had it whole
+        return;
+    const Tile t = tile_at<MODE, 2>(p, p.whole + j);
+    const int at = blockIdx.x * 8 + threadIdx.x / 32;             // 32 rows x 8 columns of the tile
+    const int64_t row = t.m0 + at / 32 * 32 + threadIdx.x % 32;
+    const int col = t.n0 + at % 32 * 8;
+    if (row >= p.rows || col >= p.cols)
+        return;
+    const float *from = p.parts + (u0 + j) * (2 * kRows * kCols) + at / 32 * 32 * kCols + at % 32 * 256 +
+                        4 * (threadIdx.x % 32);
+    float v[8] = {};
+    for (int64_t u = u0; u <= u1; ++u, from += 2 * kRows * kCols) {
+        const float4 a = __ldcs((const float4 *)from), b = __ldcs((const float4 *)(from + 128));
+        v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+        v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+    }
+    if (MODE == GLU_DW && p.out_f32) {
+        float *to = (float *)p.at[t.which] + row * p.cols + col;
+#pragma unroll
+        for (int k = 0; k < 8; k += 4) {
+            const float4 y = p.add ? *(const float4 *)(to + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+            *(float4 *)(to + k) = make_float4(y.x + v[k], y.y + v[k + 1], y.z + v[k + 2], y.w + v[k + 3]);
+        }
+        return;
+    }
+    uint4 *to = (uint4 *)((__nv_bfloat16 *)p.at[t.which] + row * p.cols + col);
+    float y[8] = {};
+    if (p.add)
+        Vec<__nv_bfloat16>::unpack(*to, y);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        y[k] += v[k];
+    *to = Vec<__nv_bfloat16>::pack(y);
+}
+
 // ---- few tokens ------------------------------------------------------------------------------
 // A server's step: the weights are read once and bound the call.  Here the weights are the products'
 // M side: a CTA takes `take` rows of Wg and as many of Wu (so that the rows of a round divide over
-// the SMs), the tokens are the N side, and a lane of the accumulators is a feature.
+// the SMs), the tokens are the N side, and a lane of the accumulators is a feature.  Up to 64 rows of
+// each share one product's 128 (JOINED: Wu's are the upper lanes, and reach the lower lanes' threads
+// through shared memory); more take a product each.
 
-constexpr int kFewThreads = 192;
-constexpr int kFewTokens = 256;
+constexpr int kFewThreads = 320;
+
+// Up to how many tokens: 128, and 224 where a CTA has one round of more than 64 rows of each weight
+// (us, this kernel and the tiles': 160 tokens of 4096 x 14336 44.1 and 51.1, 224 47.1 and 51.4; 160 of
+// 8192 x 28672, two rounds, 162.8 and 162.7, of 1024 x 4096, 32 rows, 11.1 and 10.1; 128 of
+// 2048 x 8192 16.4 and 18.4)
+constexpr int kFewTokens = 128, kMoreTokens = 224;
 
 struct FewParams {
     CUtensorMap X, Wg, Wu;
     int T, f, n;            // n: T rounded up to 16
     int take;               // rows of each weight that a CTA takes at a time
-    int tiles, chunks, stages;
-    uint32_t stage_bytes, columns;
+    int tiles, steps, stages;
+    int per;                // chunks of 64 along d in a stage: `steps` stages have them all
+    uint32_t chunk_bytes, load_bytes, columns;
     int act;
     __nv_bfloat16 *H, *G, *U;
     unsigned int *err;
 };
 
+template <bool JOINED>
 __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constant__ FewParams p)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -620,15 +749,18 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
     const uint32_t pad = (1024u - (base & 1023u)) & 1023u;
     base += pad;
     const int S = p.stages;
-    const uint32_t w_bytes = (uint32_t)p.take * 128;
-    // (a product reads 128 rows of each weight; those past `take` lie in what follows, up to 16 KB
-    // past the last stage, and give lanes that nobody reads)
-    const uint32_t bar_off = (uint32_t)S * p.stage_bytes + 16384;
+    const uint32_t stage_bytes = p.per * p.chunk_bytes;
+    // Wu's rows lie behind Wg's `take`, or where they share a product behind 64.  (A product reads
+    // 128 rows; those that hold no row of its weight give lanes that nobody reads: they lie in what
+    // follows, up to 16 KB past the last stage.)
+    const uint32_t up = JOINED ? 64 * 128 : (uint32_t)p.take * 128, x_off = JOINED ? 2 * up : 2 * (uint32_t)p.take * 128;
+    const uint32_t bar_off = (uint32_t)S * stage_bytes + 16384;
     const uint32_t bar = base + bar_off;
     const uint32_t full_b = bar, empty_b = bar + 8 * S, accf_b = bar + 16 * S, acce_b = accf_b + 8,
                    drain_b = acce_b + 8;
     uint32_t *tmem_slot = (uint32_t *)(smem_raw + pad + bar_off + 8 * (2 * S + 3));
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    float *staged = (float *)(smem_raw + pad + (uint32_t)S * stage_bytes);      // (of the 16 KB)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -637,7 +769,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
             mbar_init(empty_b + 8 * s, 1);
         }
         mbar_init(accf_b, 1);
-        mbar_init(acce_b, 4);
+        mbar_init(acce_b, 8);
         mbar_init(drain_b, 1);
         *abort_flag = 0;
         mbar_fence_init();
@@ -658,17 +790,21 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
         int g = 0;
         bool ok = true;
         for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x)
-            for (int c = 0; c < p.chunks; ++c, ++g, ring.next(S)) {
+            for (int c = 0; c < p.steps; ++c, ++g, ring.next(S)) {
                 if (!wait(empty_b + 8 * ring.s, ring.ph ^ 1, abort_flag, p.err)) {
                     ok = false;
                     break;
                 }
-                const uint32_t at = base + ring.s * p.stage_bytes, fb = full_b + 8 * ring.s;
+                const uint32_t at = base + ring.s * stage_bytes, fb = full_b + 8 * ring.s;
                 if (elected()) {
-                    mbar_arrive_tx(fb, p.stage_bytes);
-                    tma_load_2d(at, &p.Wg, c * kK, tile * p.take, fb);
-                    tma_load_2d(at + w_bytes, &p.Wu, c * kK, tile * p.take, fb);
-                    tma_load_2d(at + 2 * w_bytes, &p.X, c * kK, 0, fb);
+                    mbar_arrive_tx(fb, p.load_bytes);
+                    for (int h = 0; h < p.per; ++h) {
+                        const int k = (c * p.per + h) * kK;
+                        const uint32_t to = at + h * p.chunk_bytes;
+                        tma_load_2d(to, &p.Wg, k, tile * p.take, fb);
+                        tma_load_2d(to + up, &p.Wu, k, tile * p.take, fb);
+                        tma_load_2d(to + x_off, &p.X, k, 0, fb);
+                    }
                 }
                 __syncwarp();
             }
@@ -679,7 +815,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
     } else if (warp == 1) {
         const uint32_t idesc = idesc_bf16(128, p.n);
         Ring ring;
-        uint32_t it = 0;
+        uint32_t it = 0, ready = 0;
         bool ok = true;
         for (int tile = blockIdx.x; tile < p.tiles && ok; tile += gridDim.x, ++it) {
             if (!wait(acce_b, (it & 1) ^ 1, abort_flag, p.err)) {
@@ -687,22 +823,28 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
                 break;
             }
             tc_fence_after();
-            for (int c = 0; c < p.chunks; ++c, ring.next(S)) {
-                if (!wait(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
+            for (int c = 0; c < p.steps; ++c) {
+                if (!__all_sync(0xffffffffu, ready) && !wait(full_b + 8 * ring.s, ring.ph, abort_flag, p.err)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t at = base + ring.s * p.stage_bytes;
+                const uint32_t at = base + ring.s * stage_bytes, done = empty_b + 8 * ring.s;
+                ring.next(S);
+                ready = peek(full_b + 8 * ring.s, ring.ph);
                 if (elected()) {
+                    for (int h = 0; h < p.per; ++h) {
+                        const uint32_t a = at + h * p.chunk_bytes;
 #pragma unroll
-                    for (int kk = 0; kk < kK / 16; ++kk) {
-                        const uint64_t bd = sdesc_sw128(at + 2 * w_bytes + kk * 32);
-                        const uint32_t more = c > 0 || kk > 0 ? 1u : 0u;
-                        mma_bf16(tmem, sdesc_sw128(at + kk * 32), bd, idesc, more);
-                        mma_bf16(tmem + p.n, sdesc_sw128(at + w_bytes + kk * 32), bd, idesc, more);
+                        for (int kk = 0; kk < kK / 16; ++kk) {
+                            const uint64_t bd = sdesc_sw128(a + x_off + kk * 32);
+                            const uint32_t more = c > 0 || h > 0 || kk > 0 ? 1u : 0u;
+                            mma_bf16(tmem, sdesc_sw128(a + kk * 32), bd, idesc, more);
+                            if (!JOINED)
+                                mma_bf16(tmem + p.n, sdesc_sw128(a + up + kk * 32), bd, idesc, more);
+                        }
                     }
-                    mma_commit(empty_b + 8 * ring.s);
+                    mma_commit(done);
                 }
                 __syncwarp();
             }
@@ -716,33 +858,67 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
         }
         __syncwarp();
     } else {
-        const int q = warp & 3;
+        const int q = warp & 3, second = (warp - 2) >> 2;
         uint32_t it = 0;
         for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++it) {
-            if (!wait(accf_b, it & 1, abort_flag, p.err))
+            const bool ok = wait(accf_b, it & 1, abort_flag, p.err);
+            if (!(JOINED ? all_of_eight(ok) : ok))       // (the warps meet below: all leave or none)
                 break;
             tc_fence_after();
             const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16);
-            const int feature = tile * p.take + 32 * q + lane;
-            const bool in = 32 * q + lane < p.take && feature < p.f;
-            for (int c = 0; c < p.n; c += 16) {
-                float g[16], u[16];
-                __syncwarp();
-                tmem_ld16(taddr + c, g);
-                tmem_ld16(taddr + p.n + c, u);
-                tmem_ld_wait();
-                if (!in)
-                    continue;
+            const int row = JOINED ? 32 * (q & 1) + lane : 32 * q + lane;
+            const int feature = tile * p.take + row;
+            const bool in = row < p.take && feature < p.f;
+            const auto store = [&](__nv_bfloat16 *to, int c, const float (&v)[16]) {
+                to += (int64_t)c * p.f + feature;
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c + j < p.T) {
-                        const int64_t at = (int64_t)(c + j) * p.f + feature;
-                        if (p.G) {
-                            p.G[at] = __float2bfloat16_rn(g[j]);
-                            p.U[at] = __float2bfloat16_rn(u[j]);
-                        }
-                        p.H[at] = __float2bfloat16_rn(activate<false>(g[j], p.act, nullptr) * u[j]);
+                for (int j = 0; j < 16; ++j, to += p.f)
+                    if (in && c + j < p.T)
+                        *to = __float2bfloat16_rn(v[j]);
+            };
+            const auto finish = [&](int c, float (&g)[16], const float (&u)[16]) {
+                if (p.G) {
+                    store(p.G, c, g);
+                    store(p.U, c, u);
+                }
+                gate_all(g, u, p.act);
+                store(p.H, c, g);
+            };
+            if (JOINED) {
+                // 32 tokens at a time, 16 for each of a lane quarter's two warps; U's lanes leave
+                // them in shared memory for G's
+                for (int c0 = 0; c0 < p.n; c0 += 32) {
+                    const int c = c0 + 16 * second;
+                    float v[16];
+                    __syncwarp();
+                    if (c < p.n) {
+                        tmem_ld16(taddr + c, v);
+                        tmem_ld_wait();
                     }
+                    if (q >= 2 && c < p.n)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            staged[(16 * second + j) * 64 + row] = v[j];
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    if (q < 2 && c < p.n) {
+                        float u[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            u[j] = staged[(16 * second + j) * 64 + row];
+                        finish(c, v, u);
+                    }
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                }
+            } else {
+                // (a lane quarter's two warps take the tokens in turn)
+                for (int c = 16 * second; c < p.n; c += 32) {
+                    float g[16], u[16];
+                    __syncwarp();
+                    tmem_ld16(taddr + c, g);
+                    tmem_ld16(taddr + p.n + c, u);
+                    tmem_ld_wait();
+                    finish(c, g, u);
+                }
             }
             tc_fence_before();
             __syncwarp();
@@ -778,13 +954,15 @@ __global__ void __launch_bounds__(256) k_glu_grad(const GradArgs a)
             Vec<__nv_bfloat16>::unpack(*((const uint4 *)(a.dH + t * a.lddh) + j), h);
             Vec<__nv_bfloat16>::unpack(*((const uint4 *)a.G + at), g);
             Vec<__nv_bfloat16>::unpack(*((const uint4 *)a.U + at), u);
+            with_activation(a.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float slope;
-                const float x = activate<true>(g[i], a.act, &slope);
-                g[i] = h[i] * u[i] * slope;
-                u[i] = h[i] * x;
-            }
+                for (int i = 0; i < 8; ++i) {
+                    float slope;
+                    const float x = activate<decltype(act)::value, true>(g[i], slope);
+                    g[i] = h[i] * u[i] * slope;
+                    u[i] = h[i] * x;
+                }
+            });
             *((uint4 *)a.dG + at) = Vec<__nv_bfloat16>::pack(g);
             *((uint4 *)a.dU + at) = Vec<__nv_bfloat16>::pack(u);
         }
@@ -792,20 +970,45 @@ __global__ void __launch_bounds__(256) k_glu_grad(const GradArgs a)
 
 // ---- launches ------------------------------------------------------------------------------------
 
+// The work of `tiles` tiles of `all` chunks on `units` pairs: rounds of whole tiles, and the last
+// round's cut where that ends it at least kSaved chunks earlier (a chunk is 0.3 us; the parts and
+// their sum take about 10).  A run is at least kRun chunks.
+constexpr int64_t kSaved = 32, kRun = 8;
+struct Cut {
+    int64_t whole, cut, run, parts;       // parts: places of 256 x 256
+};
+Cut cut_of(int64_t tiles, int64_t all, int64_t units)
+{
+    const int64_t left = tiles % units, run = std::max(kRun, (left * all + units - 1) / units);
+    if (left == 0 || all - run < kSaved)
+        return Cut{tiles, 0, 0, 0};
+    return Cut{tiles - left, left, run, (left * all + run - 1) / run + left};
+}
+
 template <int MODE, int CG>
 cudaError_t launch_tiles(GluParams p, int sms, cudaStream_t s)
 {
+    const int units = std::max(1, sms / CG);
     p.mt = (p.rows + kRows * CG - 1) / (kRows * CG);
-    const int width = MODE == GLU_FWD ? kCols / 2 : kCols;
+    constexpr int width = MODE == GLU_FWD ? kCols / 2 : kCols;
     p.nt = (p.cols + width - 1) / width;
-    p.items = p.mt * p.nt * (MODE == GLU_DW ? 2 : 1);
-    const int grid = (int)std::min<int64_t>(p.items, std::max(1, sms / CG)) * CG;
-    cudaError_t e = cudaFuncSetAttribute(k_glu<MODE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         Stage<CG>::kSmem);
+    const int64_t tiles = p.mt * p.nt * (MODE == GLU_DW ? 2 : 1);
+    const Cut c = MODE != GLU_FWD && CG == 2 ? cut_of(tiles, p.chunks * (MODE == GLU_DX ? 2 : 1), units)
+                                             : Cut{tiles, 0, 0, 0};
+    p.whole = c.whole;
+    p.cut = c.cut;
+    p.run = c.run;
+    const int grid = (int)(c.cut ? units : std::min<int64_t>(tiles, units)) * CG;
+    cudaError_t e = cudaFuncSetAttribute(k_glu<MODE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Stage<CG>::kSmem);
     if (e != cudaSuccess)
         return e;
     count_launch();
     e = launch_clusters(k_glu<MODE, CG>, CG, dim3(grid), dim3(kGluThreads), Stage<CG>::kSmem, s, p);
+    if constexpr (MODE != GLU_FWD)
+        if (e == cudaSuccess && c.cut) {
+            count_launch();
+            e = launch_dependent(k_glu_join<MODE>, dim3(32, (unsigned)c.cut), dim3(256), 0, s, p);
+        }
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -813,7 +1016,7 @@ cudaError_t launch_tiles(GluParams p, int sms, cudaStream_t s)
 // twice as many of 16 bits, which a copy does not tell apart
 bool out_map(CUtensorMap *m, const void *out, int cols, int64_t rows, bool f32)
 {
-    return tensor_map_2d(m, out, (uint64_t)cols * (f32 ? 2 : 1), rows, (uint64_t)cols * (f32 ? 4 : 2), 64, 32, true);
+    return tensor_map_2d(m, out, (uint64_t)cols * (f32 ? 2 : 1), rows, (uint64_t)cols * (f32 ? 4 : 2), 64, 32);
 }
 
 // Pairs of CTAs where the stream's context has the whole GPU; with a part of it a pair might find
@@ -825,31 +1028,47 @@ cudaError_t launch_products(const GluParams &p, cudaStream_t s)
     return sms < all ? launch_tiles<MODE, 1>(p, sms, s) : launch_tiles<MODE, 2>(p, sms, s);
 }
 
-cudaError_t launch_few(FewParams p, const __nv_bfloat16 *X, int64_t ldx, const __nv_bfloat16 *Wg,
-                       const __nv_bfloat16 *Wu, int d, cudaStream_t s)
+// Rows of each weight that a CTA takes at a time, in as few rounds as 128 rows allow
+int few_rounds(int f, int sms) { return (int)(((int64_t)f + sms * 128 - 1) / (sms * 128)); }
+int few_rows(int f, int sms)
 {
-    const int sms = stream_sms(s);
+    const int rounds = few_rounds(f, sms);
+    return std::min(128, ((f + sms * rounds - 1) / (sms * rounds) + 7) / 8 * 8);
+}
+bool is_few(int64_t T, int f, int sms)
+{
+    return T <= (few_rounds(f, sms) == 1 && few_rows(f, sms) > 64 ? kMoreTokens : kFewTokens);
+}
+
+cudaError_t launch_few(FewParams p, const __nv_bfloat16 *X, int64_t ldx, const __nv_bfloat16 *Wg,
+                       const __nv_bfloat16 *Wu, int d, int sms, cudaStream_t s)
+{
     p.n = (p.T + 15) / 16 * 16;
-    const int rounds = (int)(((int64_t)p.f + sms * 128 - 1) / (sms * 128));
-    p.take = std::min(128, ((p.f + sms * rounds - 1) / (sms * rounds) + 7) / 8 * 8);
+    p.take = few_rows(p.f, sms);
     p.tiles = (p.f + p.take - 1) / p.take;
-    p.chunks = (d + kK - 1) / kK;
-    p.stage_bytes = (uint32_t)(2 * p.take + p.n) * 128;
-    const uint32_t rest = 16384 + 1024 + 512;
-    p.stages = std::max(2, std::min(16, (int)((232448 - rest) / p.stage_bytes)));
+    const bool joined = p.take <= 64;
+    p.chunk_bytes = (uint32_t)((joined ? 128 : 2 * p.take) + p.n) * 128;
+    // two chunks a stage, which halves the waits, where four such stages fit
+    const uint32_t rest = 16384 + 1024 + 512, room = 232448 - rest;
+    const int chunks = (d + kK - 1) / kK;
+    p.per = room / (2 * p.chunk_bytes) >= 4 && chunks > 1 ? 2 : 1;
+    p.steps = (chunks + p.per - 1) / p.per;
+    p.load_bytes = (uint32_t)p.per * (2 * p.take + p.n) * 128;
+    p.stages = std::max(2, std::min(16, (int)(room / (p.per * p.chunk_bytes))));
     p.columns = 32;
-    while (p.columns < 2u * p.n)
+    while (p.columns < (joined ? 1u : 2u) * p.n)
         p.columns *= 2;
-    if (!tensor_map_2d(&p.X, X, d, p.T, (uint64_t)ldx * 2, kK, p.n, true) ||
-        !tensor_map_2d(&p.Wg, Wg, d, p.f, (uint64_t)d * 2, kK, p.take, true) ||
-        !tensor_map_2d(&p.Wu, Wu, d, p.f, (uint64_t)d * 2, kK, p.take, true))
+    if (!tensor_map_2d(&p.X, X, d, p.T, (uint64_t)ldx * 2, kK, p.n) ||
+        !tensor_map_2d(&p.Wg, Wg, d, p.f, (uint64_t)d * 2, kK, p.take) ||
+        !tensor_map_2d(&p.Wu, Wu, d, p.f, (uint64_t)d * 2, kK, p.take))
         return cudaErrorInvalidValue;
-    const uint32_t smem = (uint32_t)p.stages * p.stage_bytes + rest;
-    cudaError_t e = cudaFuncSetAttribute(k_glu_few, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
+    const uint32_t smem = (uint32_t)p.stages * p.per * p.chunk_bytes + rest;
+    const auto kernel = joined ? k_glu_few<true> : k_glu_few<false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
     if (e != cudaSuccess)
         return e;
     count_launch();
-    e = launch_dependent(k_glu_few, dim3(std::min(p.tiles, sms)), dim3(kFewThreads), smem, s, p);
+    e = launch_dependent(kernel, dim3(std::min(p.tiles, sms)), dim3(kFewThreads), smem, s, p);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -861,7 +1080,8 @@ cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, 
 {
     using namespace tc;
     typedef __nv_bfloat16 b16;
-    if (T <= 128) {
+    const int sms = stream_sms(s);
+    if (is_few(T, f, sms)) {
         FewParams p = {};
         p.T = (int)T;
         p.f = f;
@@ -870,7 +1090,7 @@ cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, 
         p.G = (b16 *)G;
         p.U = (b16 *)U;
         p.err = err;
-        return launch_few(p, (const b16 *)X, ldx, (const b16 *)Wg, (const b16 *)Wu, d, s);
+        return launch_few(p, (const b16 *)X, ldx, (const b16 *)Wg, (const b16 *)Wu, d, sms, s);
     }
     GluParams p = {};
     p.rows = T;
@@ -881,14 +1101,22 @@ cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, 
     p.err = err;
     if (!out_map(&p.out[0], H, f, T, false) || (G && (!out_map(&p.out[1], G, f, T, false) ||
                                                        !out_map(&p.out[2], U, f, T, false))) ||
-        !tensor_map_2d(&p.A[0], X, d, T, (uint64_t)ldx * 2, kK, kRows, true) ||
-        !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, kK, 128, true) ||
-        !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, kK, 128, true))
+        !tensor_map_2d(&p.A[0], X, d, T, (uint64_t)ldx * 2, kK, kRows) ||
+        !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, kK, 128) ||
+        !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, kK, 128))
         return cudaErrorInvalidValue;
     return launch_products<GLU_FWD>(p, s);
 }
 
-size_t glu_bwd_workspace(int64_t T, int d, int f) { return 0; }
+size_t glu_bwd_workspace(int64_t T, int d, int f)
+{
+    using namespace tc;
+    const int64_t units = std::max(1, device_sms() / 2);
+    const auto tiles = [](int64_t rows, int cols) { return ((rows + 255) / 256) * ((cols + 255) / 256); };
+    const Cut dx = cut_of(tiles(T, d), 2 * ((f + kK - 1) / kK), units);
+    const Cut dw = cut_of(2 * tiles(f, d), (T + kK - 1) / kK, units);
+    return (size_t)std::max(dx.parts, dw.parts) * (256 * 256 * sizeof(float));
+}
 
 cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, const void *Wg, const void *Wu,
                     const void *G, const void *U, int64_t T, int d, int f, int act, void *dG, void *dU, void *dX,
@@ -910,11 +1138,13 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
         p.rows = T;
         p.cols = d;
         p.chunks = (f + kK - 1) / kK;
+        p.at[0] = dX;
+        p.parts = (float *)ws;
         p.err = err;
-        if (!out_map(&p.out[0], dX, d, T, false) || !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, kK, kRows, true) ||
-            !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, kK, kRows, true) ||
-            !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, 64, kK, true) ||
-            !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, 64, kK, true))
+        if (!out_map(&p.out[0], dX, d, T, false) || !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, kK, kRows) ||
+            !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, kK, kRows) ||
+            !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, 64, kK) ||
+            !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, 64, kK))
             return cudaErrorInvalidValue;
         e = launch_products<GLU_DX>(p, s);
     }
@@ -925,13 +1155,14 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
         p.chunks = (T + kK - 1) / kK;
         p.at[0] = dWg;
         p.at[1] = dWu;
+        p.parts = (float *)ws;
         p.out_f32 = grad_dt == SN_F32;
         p.add = accumulate;
         p.err = err;
         if (!out_map(&p.out[0], dWg, d, f, p.out_f32) || !out_map(&p.out[1], dWu, d, f, p.out_f32) ||
-            !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, 64, kK, true) ||
-            !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, 64, kK, true) ||
-            !tensor_map_2d(&p.B[0], X, d, T, (uint64_t)ldx * 2, 64, kK, true))
+            !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, 64, kK) ||
+            !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, 64, kK) ||
+            !tensor_map_2d(&p.B[0], X, d, T, (uint64_t)ldx * 2, 64, kK))
             return cudaErrorInvalidValue;
         e = launch_products<GLU_DW>(p, s);
     }

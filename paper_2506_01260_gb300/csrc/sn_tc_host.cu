@@ -35,7 +35,8 @@ EncodeTiledFn encode_fn()
 
 // A 2-D bf16 tensor of `outer` rows x `inner` elements, `row_bytes` apart.
 bool map2d(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t row_bytes,
-           uint32_t box_inner, uint32_t box_outer, bool sw128)
+           uint32_t box_inner, uint32_t box_outer, bool sw128,
+           CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn)
@@ -47,7 +48,7 @@ bool map2d(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box,
               estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               sw128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              promotion,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -219,9 +220,9 @@ int current_device()
 }  // namespace
 
 bool tensor_map_2d(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t row_bytes,
-                   uint32_t box_inner, uint32_t box_outer, bool sw128)
+                   uint32_t box_inner, uint32_t box_outer)
 {
-    return map2d(m, ptr, inner, outer, row_bytes, box_inner, box_outer, sw128);
+    return map2d(m, ptr, inner, outer, row_bytes, box_inner, box_outer, true, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 }  // namespace tc
