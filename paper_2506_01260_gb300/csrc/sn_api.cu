@@ -871,6 +871,8 @@ sn_status sn_blocknorm_bwd(sn_dtype dt, const void *dZ, int64_t lddz, const void
     if (!std::isfinite(scale) || !is_gating(gate, gates, T) || !dw_post || !dw_pre ||
         (gate == nullptr) != (dgate == nullptr))
         return SN_ERR_INVALID_ARG;
+    if (T == 0 && accumulate)
+        return SN_OK;
     const size_t need = T > 0 ? sn::blocknorm_bwd_workspace(T, d, gates) : 0;
     if (T > 0 && (!dZ || !H || !Y || !w_post || !w_pre || !dY || !dR || !ws || ws_bytes < need))
         return SN_ERR_INVALID_ARG;
@@ -894,14 +896,11 @@ sn_status sn_blocknorm_bwd(sn_dtype dt, const void *dZ, int64_t lddz, const void
         return SN_ERR_INVALID_ARG;
     if (T == 0) {
         const cudaStream_t s = (cudaStream_t)stream;
-        cudaError_t e = cudaSuccess;
-        if (!accumulate) {
-            e = cudaMemsetAsync(dw_post, 0, (size_t)d * 4, s);
-            if (e == cudaSuccess)
-                e = cudaMemsetAsync(dw_pre, 0, (size_t)d * 4, s);
-            if (e == cudaSuccess && dgate)
-                e = cudaMemsetAsync(dgate, 0, (size_t)gates * d * 4, s);
-        }
+        cudaError_t e = cudaMemsetAsync(dw_post, 0, (size_t)d * 4, s);
+        if (e == cudaSuccess)
+            e = cudaMemsetAsync(dw_pre, 0, (size_t)d * 4, s);
+        if (e == cudaSuccess && dgate)
+            e = cudaMemsetAsync(dgate, 0, (size_t)gates * d * 4, s);
         return cuda_status(e);
     }
     return cuda_status(sn::blocknorm_bwd(dt, dZ, lddz, H, Y, ldy, dH, gate, gates, wdt, w_post, w_pre, T, d, eps,
@@ -1044,7 +1043,7 @@ sn_status sn_glu_bwd(sn_basis_t errors, sn_dtype dt, const void *dH, int64_t ldd
     if (!is_dtype(gdt) || lddh < f || (dw && ldx < d) || dw != (dWu != nullptr))
         return SN_ERR_INVALID_ARG;
     st = check_glu(dt, T, d, f, act, {lddh, dw ? ldx : 0});
-    if (st != SN_OK)
+    if (st != SN_OK || (T == 0 && (!dw || accumulate)))
         return st;
     const size_t need = sn::glu_bwd_workspace(T, d, f), es = esize(gdt);
     if (T > 0 && (!dH || !G || !U || !dG || !dU || (dx && (!Wg || !Wu)) || (dw && !X) ||
@@ -1064,8 +1063,6 @@ sn_status sn_glu_bwd(sn_basis_t errors, sn_dtype dt, const void *dH, int64_t ldd
         !on_device({dH, X, Wg, Wu, G, U, dG, dU, dX, dWg, dWu, ws}))
         return SN_ERR_INVALID_ARG;
     if (T == 0) {
-        if (!dw || accumulate)
-            return SN_OK;
         const cudaError_t e = cudaMemsetAsync(dWg, 0, (size_t)f * d * es, (cudaStream_t)stream);
         return cuda_status(e != cudaSuccess ? e : cudaMemsetAsync(dWu, 0, (size_t)f * d * es, (cudaStream_t)stream));
     }

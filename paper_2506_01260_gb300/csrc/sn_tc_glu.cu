@@ -941,14 +941,14 @@ struct GradArgs {
     const __nv_bfloat16 *dH, *G, *U;
     __nv_bfloat16 *dG, *dU;
     int64_t T, lddh;
-    int f8;                 // pieces of 8 in a row
+    int64_t f8;             // pieces of 8 in a row
     int act;
 };
 __global__ void __launch_bounds__(256) k_glu_grad(const GradArgs a)
 {
     griddep_start();
     for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y)
-        for (int j = blockIdx.x * 256 + threadIdx.x; j < a.f8; j += gridDim.x * 256) {
+        for (int64_t j = blockIdx.x * 256 + threadIdx.x; j < a.f8; j += gridDim.x * 256) {
             const int64_t at = t * a.f8 + j;
             float h[8], g[8], u[8];
             Vec<__nv_bfloat16>::unpack(*((const uint4 *)(a.dH + t * a.lddh) + j), h);
@@ -1125,12 +1125,14 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
 {
     using namespace tc;
     typedef __nv_bfloat16 b16;
-    const GradArgs a{(const b16 *)dH, (const b16 *)G, (const b16 *)U, (b16 *)dG, (b16 *)dU, T, lddh, f / 8, act};
-    const int across = (a.f8 + 255) / 256;
+    // (rows behind one another are one)
+    const bool one = lddh == f;
+    const GradArgs a{(const b16 *)dH, (const b16 *)G, (const b16 *)U, (b16 *)dG, (b16 *)dU, one ? 1 : T, lddh,
+                     one ? T * (f / 8) : f / 8, act};
+    const int64_t across = std::min<int64_t>((a.f8 + 255) / 256, 1 << 20);
     count_launch();
-    cudaError_t e = launch_dependent(
-        k_glu_grad, dim3((unsigned)across, (unsigned)std::min<int64_t>(T, std::max(1, 65535 / across))), dim3(256), 0,
-        s, a);
+    cudaError_t e = launch_dependent(k_glu_grad, dim3((unsigned)across, (unsigned)std::min<int64_t>(a.T, 65535)),
+                                     dim3(256), 0, s, a);
     if (e == cudaSuccess)
         e = cudaGetLastError();
     if (e == cudaSuccess && dX) {

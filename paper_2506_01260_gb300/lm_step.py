@@ -6,13 +6,17 @@ take the same way back.  The library's calls do everything but the matrix produc
 torch's.  Weights are random and the text is a synthetic chain of tokens, so the model only shows
 how the calls fit together:
 
-    python -m paper_2506_01260_gb300.lm_step
+    python -m paper_2506_01260_gb300.lm_step [gated]
+
+`gated`: stage 1 has a gated feed-forward block of its own, with norms before and after it.  (Behind
+a boundary: a norm's weights take a block's output out of S, which the streams that cross one stay in.)
 
 The embedding is T_fixed[ids] + T_S[ids] with T_S's rows in S = Col(U), and the block writes to the
 residual stream through a weight whose columns lie in S, so the stream minus T_fixed[ids] stays in
 S (Sec. 4.3) and the boundary loses nothing but roundings.
 """
 import math
+import sys
 
 import torch
 
@@ -47,8 +51,13 @@ class TwoStage:
         # gradients in fixed buffers, listed once for the norm and the clipping
         names = {"T_S": (vocab, d), "W_up": (d_ff, d), "W_down": (d, d_ff), "W_head": (vocab, d),
                  "w0": (d,), "w1": (d,)}
+        names.update(self._more(d, d_ff, normal))
         self.grads = {n: torch.zeros(s, device=device) for n, s in names.items()}
         self.list = sn.GradList(self.grads.values())
+
+    def _more(self, d, d_ff, normal):
+        """Makes stage 1's further parameters; their shapes."""
+        return {}
 
     # ---- forward -----------------------------------------------------------------------------
 
@@ -66,6 +75,15 @@ class TwoStage:
         C = sn.sn_compress_fwd(self.basis, x, ids, self.T_fixed, n)
         return sn.sn_decompress_fwd(self.basis, C, ids, self.T_fixed, n)
 
+    def _stage1(self, x1):
+        """What the head reads, and what the gradient needs."""
+        y1, _ = sn.sn_rmsnorm_fwd(x1, self.w1, EPS)
+        return y1, (x1,)
+
+    def _stage1_back(self, dy1, x1):
+        """The gradient of x1; the parameters' in self.grads."""
+        return sn.sn_rmsnorm_bwd(dy1, x1, self.w1, EPS, dw=self.grads["w1"])[0]
+
     # ---- one step -------------------------------------------------------------------------------
 
     def backward(self, ids, target):
@@ -75,7 +93,7 @@ class TwoStage:
         g = self.grads
         y0, h0, up, x0 = self._stage0(ids)
         x1 = self._boundary(x0, ids)
-        y1, _ = sn.sn_rmsnorm_fwd(x1, self.w1, EPS)
+        y1, kept = self._stage1(x1)
         logits = y1 @ self.W_head.T
         logp, lse, _, _, _ = sn.sn_logprob_fwd(logits, target, entropy=False, basis=self.basis)
         n = ((target >= 0) & (target < self.vocab)).sum().clamp(min=1).float()
@@ -83,7 +101,7 @@ class TwoStage:
         dlogp = (-1.0 / n).expand(ids.shape[0]).contiguous()
         dlogits = sn.sn_logprob_bwd(logits, lse, target, dlogp, out=logits)
         g["W_head"].copy_(dlogits.T @ y1)
-        dx1, _ = sn.sn_rmsnorm_bwd(dlogits @ self.W_head, x1, self.w1, EPS, dw=g["w1"])
+        dx1 = self._stage1_back(dlogits @ self.W_head, *kept)
         # the gradient crosses the boundary the same way
         dx0 = sn.sn_decompress_bwd(self.basis, sn.sn_compress_bwd(self.basis, dx1))
         g["W_down"].copy_(dx0.T @ up)
@@ -105,8 +123,10 @@ class TwoStage:
         dT = g["T_S"].to(BF16)
         in_S = sn.sn_decompress_bwd(b, sn.sn_compress_bwd(b, dT))
         self.T_S.add_(in_S, alpha=-lr)
-        for p, n in ((self.W_up, "W_up"), (self.W_head, "W_head"), (self.w0, "w0"), (self.w1, "w1")):
-            p.add_(g[n].to(p.dtype), alpha=-lr)
+        for n in g:
+            if n not in ("T_S", "W_down"):
+                p = getattr(self, n)
+                p.add_(g[n].to(p.dtype), alpha=-lr)
         return loss, norm
 
     def score(self, ids, top=5):
@@ -114,11 +134,50 @@ class TwoStage:
         the entropy and the `top` alternatives.  Stage 1's activations pass through 8 bits (e4m3, a
         scale a row), to show what that does to the scores; the products themselves are bf16."""
         _, _, _, x0 = self._stage0(ids)
-        codes, scale, _ = sn.sn_rmsnorm_fwd_quant(self._boundary(x0, ids), self.w1, EPS, "e4m3")
-        y1 = sn.sn_quant_restore(codes, scale, "e4m3")
+        y1 = self._scored(self._boundary(x0, ids))
         target = torch.cat([ids[1:], ids.new_full((1,), -1)])
         logp, _, H, alt, alt_logp = sn.sn_logprob_fwd(y1 @ self.W_head.T, target, top=top)
         return logp, H, alt, alt_logp
+
+
+    def _scored(self, x1):
+        codes, scale, _ = sn.sn_rmsnorm_fwd_quant(x1, self.w1, EPS, "e4m3")
+        return sn.sn_quant_restore(codes, scale, "e4m3")
+
+
+class GatedTwoStage(TwoStage):
+    """Stage 1 with a gated block between two norms: h = x1 + scale gate norm(down(act(gate y1) up y1)),
+    y1 = norm(x1), and the head reads norm(h)."""
+
+    act, scale = "silu", 0.5
+
+    def _more(self, d, d_ff, normal):
+        self.V_gate, self.V_up = (normal(d_ff, d, std=1 / math.sqrt(d)).to(BF16) for _ in range(2))
+        self.V_down = normal(d, d_ff, std=1 / math.sqrt(d_ff)).to(BF16)
+        self.w_post, self.w_pre = (torch.ones_like(self.w1) for _ in range(2))
+        self.gate = torch.ones(1, d, device=self.w1.device, dtype=BF16)
+        return {"V_gate": (d_ff, d), "V_up": (d_ff, d), "V_down": (d, d_ff), "w_post": (d,),
+                "w_pre": (d,), "gate": (1, d)}
+
+    def _stage1(self, x1, keep=True):
+        y1, _ = sn.sn_rmsnorm_fwd(x1, self.w1, EPS)
+        H, G, U = sn.sn_glu_fwd(y1, self.V_gate, self.V_up, self.act, keep=keep, basis=self.basis)
+        y = H @ self.V_down.T
+        z, h = sn.sn_blocknorm_fwd(y, x1, self.w_post, self.w_pre, EPS, scale=self.scale, gate=self.gate)
+        return z, (x1, y1, H, G, U, y, h)
+
+    def _stage1_back(self, dz, x1, y1, H, G, U, y, h):
+        g = self.grads
+        dy, dx1, _, _, _ = sn.sn_blocknorm_bwd(dz, h, y, self.w_post, self.w_pre, EPS, scale=self.scale,
+                                               gate=self.gate, dw_post=g["w_post"], dw_pre=g["w_pre"],
+                                               dgate=g["gate"])
+        g["V_down"].copy_(dy.T @ H)
+        dy1 = sn.sn_glu_bwd(dy @ self.V_down, y1, self.V_gate, self.V_up, G, U, self.act, dG=G, dU=U,
+                            dW_gate=g["V_gate"], dW_up=g["V_up"], basis=self.basis)[0]
+        return sn.sn_rmsnorm_bwd(dy1, x1, self.w1, EPS, dH=dx1, dw=g["w1"])[0]
+
+    def _scored(self, x1):
+        return self._stage1(x1, keep=False)[0]
 
 
 def chain(T, vocab, seed=0, device="cuda"):
@@ -129,8 +188,8 @@ def chain(T, vocab, seed=0, device="cuda"):
     return ids[:-1].int().to(device), ids[1:].int().to(device)
 
 
-def main(steps=60, T=2048):
-    model = TwoStage()
+def main(steps=60, T=2048, gated=False):
+    model = GatedTwoStage() if gated else TwoStage()
     for i in range(steps):
         loss, norm = model.step(*chain(T, model.vocab, seed=i))
         if i % 10 == 0 or i == steps - 1:
@@ -144,4 +203,4 @@ def main(steps=60, T=2048):
 
 
 if __name__ == "__main__":
-    main()
+    main(gated="gated" in sys.argv[1:])
