@@ -343,7 +343,18 @@ __device__ __forceinline__ void from_fours(const float4 *w, int nv, int j, float
     }
 }
 
+// 16 bytes to shared memory, of which `n` (0 or 16) are read and the others zeros
+__device__ __forceinline__ void copy16(uint4 *to, const uint4 *from, int n)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                 "l"(from), "r"(n)
+                 : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // Threads of an SM that registers are kept low enough for
+template <int S, int C>
+constexpr bool is_ahead = S <= 512 && C <= 2;
 template <typename T, int S, int C>
 constexpr int kBwdResident = S > 512 ? S : S == 320 ? 640 : 512;
 
@@ -381,25 +392,37 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                 wp[k / 4 * nv + j] = make_float4(w[k], w[k + 1], w[k + 2], w[k + 3]);
         }
     }
-    // The next row's loads run before this row's sums meet, where registers allow
-    constexpr bool kEarly = C == 1 || (sizeof(T) == 4 && C == 2);
-    uint4 hv[C], yv[C], zv[C], rv[C], hn[C], yn[C], zn[C], rn[C];
+    // The next row is on its way to shared memory, each thread's own pieces, while this one is at work
+    // (16384 rows of 5120 bf16 178 us, 195 when they were asked for into L2 alone).  Rows of more than 512
+    // lanes leave no room there, and four pieces a lane no registers (16384 of 4096 fp32 292 us, 276).
+    constexpr bool kAhead = is_ahead<S, C>;
+    uint4 *ahead = (uint4 *)(weights + kRows * (2 * (N / 4)) * nv) + threadIdx.x;
+    uint4 hv[C], yv[C], zv[C], rv[C];
     // (of the last block's warps some may have none)
     const int64_t t1 = worker < workers ? first_token(worker + 1, workers, a.T) : 0;
-    auto load = [&](int64_t t, uint4 (&h)[C], uint4 (&y)[C], uint4 (&z)[C], uint4 (&r)[C]) {
+    auto load = [&](int64_t t) {
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
             const bool live = t < t1 && j < nv;
-            h[i] = live ? *((const uint4 *)(H + t * a.d) + j) : make_uint4(0, 0, 0, 0);
-            y[i] = live ? *((const uint4 *)(Y + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
-            z[i] = live ? *((const uint4 *)(dZ + t * a.lddz) + j) : make_uint4(0, 0, 0, 0);
-            r[i] = live && dH ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+            if (kAhead) {
+                const int64_t at = live ? t : 0;
+                const int c = live ? j : 0, n = live ? 16 : 0;
+                copy16(ahead + (4 * i) * blockDim.x, (const uint4 *)(H + at * a.d) + c, n);
+                copy16(ahead + (4 * i + 1) * blockDim.x, (const uint4 *)(Y + at * a.ldy) + c, n);
+                copy16(ahead + (4 * i + 2) * blockDim.x, (const uint4 *)(dZ + at * a.lddz) + c, n);
+                copy16(ahead + (4 * i + 3) * blockDim.x, (const uint4 *)((dH ? dH : H) + at * a.d) + c, dH ? n : 0);
+            } else {
+                hv[i] = live ? *((const uint4 *)(H + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+                yv[i] = live ? *((const uint4 *)(Y + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
+                zv[i] = live ? *((const uint4 *)(dZ + t * a.lddz) + j) : make_uint4(0, 0, 0, 0);
+                rv[i] = live && dH ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+            }
         }
     };
     int64_t t = first_token(worker, workers, a.T);
-    if (kEarly)
-        load(t, hn, yn, zn, rn);
+    if (kAhead)
+        load(t);
     float2 sum[C][P];
     const auto clear = [&] {
 #pragma unroll
@@ -429,19 +452,20 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
             }
         }
         for (; t < end; ++t) {
-            if (kEarly) {
+            if (kAhead) {
+                copies_done();
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
-                    hv[i] = hn[i];
-                    yv[i] = yn[i];
-                    zv[i] = zn[i];
-                    rv[i] = rn[i];
+                    hv[i] = ahead[(4 * i) * blockDim.x];
+                    yv[i] = ahead[(4 * i + 1) * blockDim.x];
+                    zv[i] = ahead[(4 * i + 2) * blockDim.x];
+                    rv[i] = ahead[(4 * i + 3) * blockDim.x];
                 }
-                load(t + 1, hn, yn, zn, rn);
+                load(t + 1);
             } else {
-                load(t, hv, yv, zv, rv);
+                load(t);
             }
-            const int64_t later = t + (kEarly ? 2 : 1);
+            const int64_t later = t + (kAhead ? 2 : 1);
             if (a.prefetch && lane < 4 && later < t1) {
                 const T *p = lane == 0 ? H + later * a.d : lane == 1 ? Y + later * a.ldy
                            : lane == 2 ? dZ + later * a.lddz : dH ? dH + later * a.d : nullptr;
@@ -799,9 +823,10 @@ bool bwd_registers(const Args &a) { return pieces<T>(a.d, a.ldy, 2) && a.lddz % 
 template <typename T, int S, int C>
 cudaError_t bwd_rows(const Plan &p, const Args &a, cudaStream_t s)
 {
-    const size_t smem = (size_t)p.rows_at_once * 2 * a.d * sizeof(float);
+    // m and w_pre, and the next row's pieces
+    const size_t smem = (size_t)p.rows_at_once * 2 * a.d * sizeof(float) + (is_ahead<S, C> ? (size_t)p.threads * C * 64 : 0);
     cudaError_t e = cudaFuncSetAttribute(k_blocknorm_bwd<T, S, C>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         131072);   // of rows of 16384 bf16
+                                         131072);   // rows of 16384 bf16; of 8192 64 KB and as much ahead
     if (e != cudaSuccess)
         return e;
     count_launch();

@@ -968,7 +968,62 @@ __global__ void __launch_bounds__(256) k_glu_grad(const GradArgs a)
         }
 }
 
+// ---- rows on 128-byte boundaries -----------------------------------------------------------------
+// A box row of 128 bytes that starts off a 128-byte boundary is two requests of a copy, and where both
+// of a product's operands have such rows, requests bound it (copies alone, 4096 tokens: forward of
+// 2056 x 5504 120 us, of 2048 x 5504 72).  So the gradients' X and weights are laid out anew, rows
+// `ld` apart, where that is a small part of the products.
+struct LayArgs {
+    const uint4 *from[2];
+    uint4 *to[2];
+    int64_t rows, ld_from, ld_to;   // in 16-byte pieces
+    int across;
+};
+__global__ void __launch_bounds__(256) k_glu_lay(const LayArgs a)
+{
+    griddep_start();
+    const uint4 *from = a.from[blockIdx.y];
+    uint4 *to = a.to[blockIdx.y];
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < a.rows * a.across; i += gridDim.x * 256) {
+        const int64_t r = i / a.across, c = i - r * a.across;
+        to[r * a.ld_to + c] = from[r * a.ld_from + c];
+    }
+}
+
 // ---- launches ------------------------------------------------------------------------------------
+
+// Whether X (for the weights' gradients) and the weights (for dX) are laid out anew: where neither d nor
+// f is a multiple of 64, and a copy of T d elements stands against f of their products, or one of f d
+// against T.  us, as they lie and anew: dW of 4173 x 2056 x 5512 143 and 131, 8192 x 4104 x 8200 782 and
+// 672, 512 x 8200 x 16008 255 and 224, but 16384 x 520 x 2088 94 and 101; dX of 8192 x 4104 x 8200 706 and
+// 671, 16384 x 520 x 1032 44.8 and 41.2, but 4173 x 2056 x 5512 143 and 148.
+struct Laid {
+    bool X, W;
+    int64_t ld;             // elements
+    size_t x_bytes, w_bytes;
+};
+Laid laid_of(int64_t T, int d, int f, int64_t ldx)
+{
+    Laid l;
+    const bool odd = d % 64 && f % 64 && T * d >= ((int64_t)1 << 33) / f;
+    l.X = odd && ldx % 64 && f >= 4096;
+    l.W = odd && T >= 8192;
+    l.ld = (d + 63) / 64 * 64;
+    l.x_bytes = (size_t)T * l.ld * 2;
+    l.w_bytes = (size_t)f * l.ld * 2;
+    return l;
+}
+cudaError_t lay(const void *a, const void *b, void *a_to, void *b_to, int64_t rows, int d, int64_t ld_from,
+                int64_t ld_to, cudaStream_t s)
+{
+    const LayArgs l{{(const uint4 *)a, (const uint4 *)b}, {(uint4 *)a_to, (uint4 *)b_to}, rows, ld_from / 8, ld_to / 8,
+                    d / 8};
+    count_launch();
+    const cudaError_t e = launch_dependent(
+        k_glu_lay, dim3((unsigned)std::min<int64_t>((rows * l.across + 255) / 256, 8 * device_sms()), b ? 2 : 1),
+        dim3(256), 0, s, l);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
 
 // The work of `tiles` tiles of `all` chunks on `units` pairs: rounds of whole tiles, and the last
 // round's cut where that ends it at least kSaved chunks earlier (a chunk is 0.3 us; the parts and
@@ -1108,15 +1163,31 @@ cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, 
     return launch_products<GLU_FWD>(p, s);
 }
 
-size_t glu_bwd_workspace(int64_t T, int d, int f)
+namespace tc {
+namespace {
+
+// The gradients' workspace: the parts of cut tiles, and behind them what is laid out anew, first for
+// the one product, then for the other
+struct Space {
+    size_t parts, all;
+};
+Space space_of(int64_t T, int d, int f)
 {
-    using namespace tc;
     const int64_t units = std::max(1, device_sms() / 2);
     const auto tiles = [](int64_t rows, int cols) { return ((rows + 255) / 256) * ((cols + 255) / 256); };
     const Cut dx = cut_of(tiles(T, d), 2 * ((f + kK - 1) / kK), units);
     const Cut dw = cut_of(2 * tiles(f, d), (T + kK - 1) / kK, units);
-    return (size_t)std::max(dx.parts, dw.parts) * (256 * 256 * sizeof(float));
+    const Laid l = laid_of(T, d, f, 1);
+    Space w;
+    w.parts = (size_t)std::max(dx.parts, dw.parts) * (256 * 256 * sizeof(float));
+    w.all = w.parts + std::max(l.X ? l.x_bytes : 0, l.W ? 2 * l.w_bytes : 0);
+    return w;
 }
+
+}  // namespace
+}  // namespace tc
+
+size_t glu_bwd_workspace(int64_t T, int d, int f) { return tc::space_of(T, d, f).all; }
 
 cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, const void *Wg, const void *Wu,
                     const void *G, const void *U, int64_t T, int d, int f, int act, void *dG, void *dU, void *dX,
@@ -1135,7 +1206,18 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
                                      dim3(256), 0, s, a);
     if (e == cudaSuccess)
         e = cudaGetLastError();
+    const Laid l = laid_of(T, d, f, ldx);
+    char *anew = (char *)ws + space_of(T, d, f).parts;
     if (e == cudaSuccess && dX) {
+        int64_t ld = d;
+        if (l.W) {
+            e = lay(Wg, Wu, anew, anew + l.w_bytes, f, d, d, l.ld, s);
+            if (e != cudaSuccess)
+                return e;
+            Wg = anew;
+            Wu = anew + l.w_bytes;
+            ld = l.ld;
+        }
         GluParams p = {};
         p.rows = T;
         p.cols = d;
@@ -1145,12 +1227,19 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
         p.err = err;
         if (!out_map(&p.out[0], dX, d, T, false) || !tensor_map_2d(&p.A[0], dG, f, T, (uint64_t)f * 2, kK, kRows) ||
             !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, kK, kRows) ||
-            !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, 64, kK) ||
-            !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, 64, kK))
+            !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)ld * 2, 64, kK) ||
+            !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)ld * 2, 64, kK))
             return cudaErrorInvalidValue;
         e = launch_products<GLU_DX>(p, s);
     }
     if (e == cudaSuccess && dWg) {
+        if (l.X) {
+            e = lay(X, nullptr, anew, nullptr, T, d, ldx, l.ld, s);
+            if (e != cudaSuccess)
+                return e;
+            X = anew;
+            ldx = l.ld;
+        }
         GluParams p = {};
         p.rows = f;
         p.cols = d;

@@ -224,3 +224,17 @@ def test_more_tiles_than_a_grid_and_row_strides(sn):
     H, G, U = sn.sn_glu_fwd(spread(X, 8), Wg, Wu, "silu", keep=True)
     check_fwd(X, Wg, Wu, "silu", H, G, U)
     check_bwd(dH, X, Wg, Wu, G, U, "silu", sn.sn_glu_bwd(spread(dH, 40), spread(X, 24), Wg, Wu, G, U, "silu"))
+
+
+@pytest.mark.parametrize("T,d,f,pad", [(9000, 264, 4104, 0), (8200, 1032, 1032, 0), (8200, 264, 4104, 40)])
+def test_operands_laid_out_anew(sn, T, d, f, pad):
+    """Rows of neither operand on 128 bytes, and enough of them: X and the weights are copied for the
+    products; the results lie in the same bars, and nothing of the operands changes."""
+    X, Wg, Wu, dH = inputs(T, d, f, 12)
+    _, G, U = sn.sn_glu_fwd(X, Wg, Wu, "silu", keep=True)
+    was = [t.clone() for t in (X, Wg, Wu)]
+    got = sn.sn_glu_bwd(dH, spread(X, pad) if pad else X, Wg, Wu, G, U, "silu", grad_dtype=F32)
+    check_bwd(dH, X, Wg, Wu, G, U, "silu", got)
+    assert all(torch.equal(a, b) for a, b in zip(was, (X, Wg, Wu)))
+    aligned = sn.sn_glu_bwd(dH, spread(X, -d % 64), Wg, Wu, G, U, "silu", grad_dtype=F32)
+    assert all(torch.equal(a, b) for a, b in zip(got, aligned))
