@@ -8,6 +8,17 @@
 // Products read bf16 and accumulate in fp32 (TMEM); every output is rounded once.  dG and dU are
 // outputs and the operands of the products behind them, so they are rounded to bf16 in between, as
 // the stored G and U are: the tensor cores read 16 bits.
+//
+// The products of many tokens are bound by the tensor cores: a pair of CTAs multiplies 256 x 256 tiles
+// of 64 deep chunks, which a ring of TMA loads feeds, a chunk in 555 cycles where its four products
+// take 547, and eight warps drain one accumulator while the other fills.  (Two CTAs each for itself would
+// read B twice: 1.5 times the shared memory's traffic.)  Those of a few tokens are bound by the weights'
+// bytes, dG and dU by theirs.
+//
+// Measured, 8192 x 4096 x 14336 (T, d, f): forward 962 us (2.00 PFLOP/s), with G and U 999, dG and dU
+// 170 (6.9 TB/s), dX 995, the weights' gradients 985; at these rates the chip's power sets the clock
+// (1.63 to 1.75 GHz, tensor cores at work 94 to 95% of the cycles), and runs differ by 5%.  1 token of
+// 4096 x 14336 36.7 us (6.4 TB/s), 75 tokens 41, 1 of 8192 x 28672 137 (6.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 
