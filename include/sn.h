@@ -435,7 +435,8 @@ sn_status sn_logprob_bwd(sn_dtype dtype, const void *logits, int64_t T, int64_t 
  * S).  act (sn_act): silu g / (1 + e^-g); gelu g Phi(g), Phi the normal distribution
  * function; gelu_tanh, its approximation g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2;
  * relu.  bf16 only (SN_ERR_UNSUPPORTED for SN_F32); products accumulate in fp32, and every
- * output is rounded once.  d and f are multiples of 8 (SN_ERR_ALIGNMENT), at most 2^20.
+ * output is rounded once.  An infinity or a NaN gives what the formulas give, in its row of X or
+ * column of a product alone.  d and f are multiples of 8 (SN_ERR_ALIGNMENT), at most 2^20.
  * `errors` is a basis, whose error word records a wait that expired, or NULL. */
 typedef enum { SN_ACT_SILU = 0, SN_ACT_GELU = 1, SN_ACT_GELU_TANH = 2, SN_ACT_RELU = 3 } sn_act;
 

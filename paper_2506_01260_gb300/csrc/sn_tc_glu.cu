@@ -47,7 +47,7 @@ __device__ __forceinline__ float activate(float g, float &slope)
     if (ACT == SN_ACT_RELU) {
         if (SLOPE)
             slope = g > 0.f ? 1.f : 0.f;
-        return fmaxf(g, 0.f);
+        return max_nan(g, 0.f);
     }
     if (ACT == SN_ACT_SILU) {
         const float p = sigmoid(g);

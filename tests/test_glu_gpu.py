@@ -203,6 +203,31 @@ def test_extreme_projections(sn):
         assert ((dG[far].double() - on[far].double()).abs() <= 1e-10).all()
 
 
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("act", ACTS)
+def test_nans_and_infinities_stay_in_their_rows(sn, act, T):
+    """A NaN in a token's row, an infinity in a weight's: that row and that feature, nothing else."""
+    X, Wg, Wu, dH = inputs(T, 72, 136, 21)
+    H, G, U = sn.sn_glu_fwd(X, Wg, Wu, act, keep=True)
+    x, wu = X.clone(), Wu.clone()
+    x[7, 3] = float("nan")
+    wu[130, 0] = float("inf")
+    h, g, u = sn.sn_glu_fwd(x, Wg, wu, act, keep=True)
+    assert bool(torch.isnan(h[7]).all()) and bool(torch.isnan(g[7]).all()) and bool(torch.isnan(u[7]).all())
+    rows = [t for t in range(T) if t != 7]
+    cols = [j for j in range(136) if j != 130]
+    assert torch.equal(h[rows][:, cols], H[rows][:, cols]) and torch.equal(g[rows], G[rows])
+    assert not bool(torch.isfinite(u[rows, 130]).any())
+    dh = dH.clone()
+    dh[11, 5] = float("nan")
+    was = sn.sn_glu_bwd(dH, X, Wg, Wu, G, U, act)
+    got = sn.sn_glu_bwd(dh, X, Wg, Wu, G, U, act)
+    assert bool(torch.isnan(got[0][11]).all()) and bool(torch.isnan(got[1][5]).all()) and bool(torch.isnan(got[2][5]).all())
+    for i, bad in ((0, 11), (1, 5), (2, 5)):
+        keep = [r for r in range(got[i].shape[0]) if r != bad]
+        assert torch.equal(got[i][keep], was[i][keep])
+
+
 def test_no_tokens(sn):
     X, Wg, Wu, dH = inputs(1, 64, 32, 1)
     H, G, U = sn.sn_glu_fwd(X[:0], Wg, Wu, keep=True)
