@@ -50,7 +50,6 @@ struct Args {
     // itself where it is one for all tokens
     float *part_pre, *part_post;
     float *part_gate;           // gated: [workers + gates, d], S of worker w and gate i at w + i
-    bool prefetch;
 };
 
 // half of a factor's exponent: taken on either side of a product, nothing in between leaves fp32
@@ -347,20 +346,19 @@ __device__ __forceinline__ void from_fours(const float4 *w, int nv, int j, float
     }
 }
 
-// 16 bytes to shared memory, of which `n` (0 or 16) are read and the others zeros
-__device__ __forceinline__ void copy16(uint4 *to, const uint4 *from, int n)
+// 16 bytes to shared memory
+__device__ __forceinline__ void copy16(uint4 *to, const uint4 *from)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                 "l"(from), "r"(n)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from)
                  : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Threads of an SM that registers are kept low enough for
 template <int S, int C>
-constexpr bool is_ahead = S <= 512 && C <= 2;
+constexpr bool is_ahead = S <= 512 && C <= 3;
 template <typename T, int S, int C>
-constexpr int kBwdResident = S > 512 ? S : S == 320 ? 640 : 512;
+constexpr int kBwdResident = S > 512 ? S : 512;
 
 // A worker (a warp or a block) walks its run of tokens, a row at a time, and keeps dw_pre and the
 // present gate's S of its columns in registers; m and w_pre lie in shared memory, each thread's own
@@ -397,36 +395,45 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
         }
     }
     // The next row is on its way to shared memory, each thread's own pieces, while this one is at work
-    // (16384 rows of 5120 bf16 178 us, 195 when they were asked for into L2 alone).  Rows of more than 512
-    // lanes leave no room there, and four pieces a lane no registers (16384 of 4096 fp32 292 us, 276).
+    // (16384 rows of 4096 bf16 126 us, 134 when it was asked for into L2 instead, 137 with the row after
+    // it asked for as well).  Rows of more than 512 lanes leave no room there, and with four pieces a lane
+    // it costs (16384 of 8192 fp32 540 us, 480).
     constexpr bool kAhead = is_ahead<S, C>;
     uint4 *ahead = (uint4 *)(weights + kRows * (2 * (N / 4)) * nv) + threadIdx.x;
     uint4 hv[C], yv[C], zv[C], rv[C];
     // (of the last block's warps some may have none)
     const int64_t t1 = worker < workers ? first_token(worker + 1, workers, a.T) : 0;
     auto load = [&](int64_t t) {
+        const T *h = H + t * a.d, *y = Y + t * a.ldy, *z = dZ + t * a.lddz, *r = dH + t * a.d;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
-            const bool live = t < t1 && j < nv;
+            const bool in = j < nv;
             if (kAhead) {
-                const int64_t at = live ? t : 0;
-                const int c = live ? j : 0, n = live ? 16 : 0;
-                copy16(ahead + (4 * i) * blockDim.x, (const uint4 *)(H + at * a.d) + c, n);
-                copy16(ahead + (4 * i + 1) * blockDim.x, (const uint4 *)(Y + at * a.ldy) + c, n);
-                copy16(ahead + (4 * i + 2) * blockDim.x, (const uint4 *)(dZ + at * a.lddz) + c, n);
-                copy16(ahead + (4 * i + 3) * blockDim.x, (const uint4 *)((dH ? dH : H) + at * a.d) + c, dH ? n : 0);
+                if (in) {
+                    copy16(ahead + (4 * i) * blockDim.x, (const uint4 *)h + j);
+                    copy16(ahead + (4 * i + 1) * blockDim.x, (const uint4 *)y + j);
+                    copy16(ahead + (4 * i + 2) * blockDim.x, (const uint4 *)z + j);
+                    if (dH)
+                        copy16(ahead + (4 * i + 3) * blockDim.x, (const uint4 *)r + j);
+                }
             } else {
-                hv[i] = live ? *((const uint4 *)(H + t * a.d) + j) : make_uint4(0, 0, 0, 0);
-                yv[i] = live ? *((const uint4 *)(Y + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
-                zv[i] = live ? *((const uint4 *)(dZ + t * a.lddz) + j) : make_uint4(0, 0, 0, 0);
-                rv[i] = live && dH ? *((const uint4 *)(dH + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+                hv[i] = in ? *((const uint4 *)h + j) : make_uint4(0, 0, 0, 0);
+                yv[i] = in ? *((const uint4 *)y + j) : make_uint4(0, 0, 0, 0);
+                zv[i] = in ? *((const uint4 *)z + j) : make_uint4(0, 0, 0, 0);
+                rv[i] = in && dH ? *((const uint4 *)r + j) : make_uint4(0, 0, 0, 0);
             }
         }
     };
     int64_t t = first_token(worker, workers, a.T);
-    if (kAhead)
-        load(t);
+    if (kAhead) {
+        if (!dH)                               // nothing is ever copied there
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                ahead[(4 * i + 3) * blockDim.x] = make_uint4(0, 0, 0, 0);
+        if (t < t1)
+            load(t);
+    }
     float2 sum[C][P];
     const auto clear = [&] {
 #pragma unroll
@@ -465,16 +472,10 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
                     zv[i] = ahead[(4 * i + 2) * blockDim.x];
                     rv[i] = ahead[(4 * i + 3) * blockDim.x];
                 }
-                load(t + 1);
+                if (t + 1 < t1)
+                    load(t + 1);
             } else {
                 load(t);
-            }
-            const int64_t later = t + (kAhead ? 2 : 1);
-            if (a.prefetch && lane < 4 && later < t1) {
-                const T *p = lane == 0 ? H + later * a.d : lane == 1 ? Y + later * a.ldy
-                           : lane == 2 ? dZ + later * a.lddz : dH ? dH + later * a.d : nullptr;
-                if (p)
-                    prefetch_l2(p, (uint32_t)(a.d * sizeof(T)));
             }
             Row row;
             float m[6];
@@ -788,8 +789,11 @@ cudaError_t fwd(const Args &a, cudaStream_t s)
                     : fwd_rows<T, 1024, false, kPieces>(a, g, s);
 }
 
-// Pieces a lane of wide fp32 rows holds
-constexpr int kFew = 4;
+// Pieces a lane of the gradient holds of rows of nv.  With two of bf16, two blocks of up to 256 threads
+// are on an SM (one of 512 with one piece: 16384 rows of 4096 173 us when two took 137); three of fp32
+// keep more on the way (16384 of 4096 238 us, 275 with four; 4173 of 2056 37.3, 41.6).
+template <typename T>
+int pieces_of(int nv) { return nv <= 32 ? 1 : sizeof(T) == 2 || nv <= 512 ? 2 : nv <= 512 * 3 ? 3 : 4; }
 
 // The gradient's grid
 struct Plan {
@@ -809,11 +813,10 @@ Plan plan_of(int64_t T_, int d, bool registers, int64_t gates)
         p.rows_at_once = 1;
         per_sm = 2;
     } else {
-        const int g = nv <= 64 ? 32 : lanes_of(nv, nv <= 512 ? 2 : sizeof(T) == 4 ? kFew : 2);
+        const int g = lanes_of(nv, pieces_of<T>(nv));
         p.threads = g == 32 ? 256 : g;
         p.rows_at_once = g == 32 ? 8 : 1;
-        // (bf16 rows of a little more than 256 lanes: two blocks of up to 320)
-        per_sm = std::max(1, std::min(8, (sizeof(T) == 2 && g > 256 && g <= 320 ? 640 : 512) / p.threads));
+        per_sm = std::max(1, std::min(8, 512 / p.threads));
     }
     p.workers = std::min<int64_t>(T_, (int64_t)device_sms() * per_sm * p.rows_at_once);
     p.part = (size_t)p.workers * d;
@@ -830,7 +833,7 @@ cudaError_t bwd_rows(const Plan &p, const Args &a, cudaStream_t s)
     // m and w_pre, and the next row's pieces
     const size_t smem = (size_t)p.rows_at_once * 2 * a.d * sizeof(float) + (is_ahead<S, C> ? (size_t)p.threads * C * 64 : 0);
     cudaError_t e = cudaFuncSetAttribute(k_blocknorm_bwd<T, S, C>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         131072);   // rows of 16384 bf16; of 8192 64 KB and as much ahead
+                                         147456);   // rows of 6144 fp32: 48 KB, and 96 on the way
     if (e != cudaSuccess)
         return e;
     count_launch();
@@ -858,11 +861,9 @@ cudaError_t bwd(Args a, int64_t gates, float *dw_post, float *dw_pre, float *ws,
     else if (nv <= 512)
         e = bwd_rows<T, 256, 2>(p, a, s);
     else if constexpr (sizeof(T) == 4)
-        e = p.threads <= 256 ? bwd_rows<T, 256, kFew>(p, a, s) : bwd_rows<T, 512, kFew>(p, a, s);
+        e = pieces_of<T>(nv) == 3 ? bwd_rows<T, 512, 3>(p, a, s) : bwd_rows<T, 512, 4>(p, a, s);
     else
-        e = p.threads <= 320   ? bwd_rows<T, 320, 2>(p, a, s)
-            : p.threads <= 512 ? bwd_rows<T, 512, 2>(p, a, s)
-                               : bwd_rows<T, 1024, 2>(p, a, s);
+        e = p.threads <= 512 ? bwd_rows<T, 512, 2>(p, a, s) : bwd_rows<T, 1024, 2>(p, a, s);
     if (e != cudaSuccess)
         return e;
     const int64_t looked = gates > 1 ? std::min(gates, p.workers - 1) : 0;
@@ -948,7 +949,6 @@ cudaError_t blocknorm_bwd(sn_dtype dt, const void *dZ, int64_t lddz, const void 
     a.Z = dY;
     a.dgate = dgate;
     a.add = accumulate;
-    a.prefetch = (size_t)d * (dt == SN_BF16 ? 2 : 4) >= 4096;
     return dt == SN_BF16 ? bwd<__nv_bfloat16>(a, gates, dw_post, dw_pre, ws, s)
                          : bwd<float>(a, gates, dw_post, dw_pre, ws, s);
 }
