@@ -16,8 +16,8 @@
 // so a row's six sums meet once.
 //
 // Measured: forward of 16384 bf16 rows of 4096 80 us (6.7 TB/s), of 65536 of 8192 with 16 gates 660 (6.5);
-// gradient 133 us (6.05 TB/s; 58% of the issue slots, two blocks' barriers a row) and 1010 (6.4), of 4173
-// fp32 rows of 2056 41.6 (5.0), where the 9 rows a block walks and the sum of the parts cost latency.
+// gradient 126 us (6.4 TB/s, 5 us of it the sum of the parts) and 960 (6.7), of 4173 fp32 rows of 2056 37
+// (5.6), where the 14 rows a block walks and the sum of the parts cost latency.
 #include <algorithm>
 #include <atomic>
 

@@ -288,6 +288,7 @@ struct GluParams {
     // Work: whole tiles, then the tiles that would leave most pairs idle, cut into runs of `run`
     // chunks, a pair each (0: none is cut)
     int64_t whole, cut, run;
+    int64_t span;           // chunks of a cut tile as the runs count them: at least its own
     float *parts;           // of cut tiles, fp32: pair u's of tile j at u + j
     int act;
     bool add;               // to what the output holds
@@ -340,10 +341,10 @@ __device__ __forceinline__ bool work_at(const GluParams &p, int64_t n, Work &w)
     if (MODE == GLU_FWD || p.run == 0)
         return false;
     // (p.whole is a multiple of units where tiles are cut)
-    const int64_t lo = u * p.run, hi = min(lo + p.run, p.cut * all);
-    const int64_t j = lo / all + (n - p.whole / units);
-    w.k0 = max(lo, j * all) - j * all;
-    w.k1 = min(hi, (j + 1) * all) - j * all;
+    const int64_t lo = u * p.run, hi = min(lo + p.run, p.cut * p.span);
+    const int64_t j = lo / p.span + (n - p.whole / units);
+    w.k0 = max(lo, j * p.span) - j * p.span;
+    w.k1 = min(hi - j * p.span, all);
     if (w.k0 >= w.k1)
         return false;
     if (w.k1 - w.k0 < all)
@@ -689,7 +690,7 @@ __global__ void __launch_bounds__(256) k_glu_join(const __grid_constant__ GluPar
 {
     griddep_start();
     const int64_t all = p.chunks * (MODE == GLU_DX ? 2 : 1), j = blockIdx.y;
-    const int64_t u0 = j * all / p.run, u1 = ((j + 1) * all - 1) / p.run;
+    const int64_t u0 = j * p.span / p.run, u1 = (j * p.span + all - 1) / p.run;
     if (u0 == u1)                      // one pair had it whole
         return;
     const Tile t = tile_at<MODE, 2>(p, p.whole + j);
@@ -1037,19 +1038,28 @@ cudaError_t lay(const void *a, const void *b, void *a_to, void *b_to, int64_t ro
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-// The work of `tiles` tiles of `all` chunks on `units` pairs: rounds of whole tiles, and the last
-// round's cut where that ends it at least kSaved chunks earlier (a chunk is 0.3 us; the parts and
-// their sum take about 10).  A run is at least kRun chunks.
+// The work of `tiles` tiles (`down` of them down the rows) of `all` chunks on `units` pairs: rounds of
+// whole tiles, and the last round's cut where that ends it at least kSaved chunks earlier (a chunk is
+// 0.3 us; the parts and their sum take about 10).  A run is at least kRun chunks.  Runs of one length,
+// end to end, keep every pair at work; where tiles lie below one another, runs that divide each tile
+// alike, if they are hardly longer, let them read their common columns at the same time: dX of 512 x
+// 4096 x 14336 105 us with runs of 189, the weights read twice from DRAM, and 82 with runs of 224.
 constexpr int64_t kSaved = 32, kRun = 8;
 struct Cut {
-    int64_t whole, cut, run, parts;       // parts: places of 256 x 256
+    int64_t whole, cut, run, span, parts;       // parts: places of 256 x 256
 };
-Cut cut_of(int64_t tiles, int64_t all, int64_t units)
+Cut cut_of(int64_t tiles, int64_t down, int64_t all, int64_t units)
 {
-    const int64_t left = tiles % units, run = std::max(kRun, (left * all + units - 1) / units);
+    const int64_t left = tiles % units;
+    int64_t run = left ? std::max(kRun, (left * all + units - 1) / units) : 0, span = all;
     if (left == 0 || all - run < kSaved)
-        return Cut{tiles, 0, 0, 0};
-    return Cut{tiles - left, left, run, (left * all + run - 1) / run + left};
+        return Cut{tiles, 0, 0, all, 0};
+    const int64_t each = units / left, alike = (all + each - 1) / each;
+    if (down > 1 && each > 1 && alike >= kRun && 4 * alike <= 5 * run) {
+        run = alike;
+        span = each * run;
+    }
+    return Cut{tiles - left, left, run, span, (left * span + run - 1) / run + left};
 }
 
 template <int MODE, int CG>
@@ -1060,11 +1070,12 @@ cudaError_t launch_tiles(GluParams p, int sms, cudaStream_t s)
     constexpr int width = MODE == GLU_FWD ? kCols / 2 : kCols;
     p.nt = (p.cols + width - 1) / width;
     const int64_t tiles = p.mt * p.nt * (MODE == GLU_DW ? 2 : 1);
-    const Cut c = MODE != GLU_FWD && CG == 2 ? cut_of(tiles, p.chunks * (MODE == GLU_DX ? 2 : 1), units)
-                                             : Cut{tiles, 0, 0, 0};
+    const Cut c = MODE != GLU_FWD && CG == 2 ? cut_of(tiles, p.mt, p.chunks * (MODE == GLU_DX ? 2 : 1), units)
+                                             : Cut{tiles, 0, 0, 1, 0};
     p.whole = c.whole;
     p.cut = c.cut;
     p.run = c.run;
+    p.span = c.span;
     const int grid = (int)(c.cut ? units : std::min<int64_t>(tiles, units)) * CG;
     cudaError_t e = cudaFuncSetAttribute(k_glu<MODE, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Stage<CG>::kSmem);
     if (e != cudaSuccess)
@@ -1186,9 +1197,9 @@ struct Space {
 Space space_of(int64_t T, int d, int f)
 {
     const int64_t units = std::max(1, device_sms() / 2);
-    const auto tiles = [](int64_t rows, int cols) { return ((rows + 255) / 256) * ((cols + 255) / 256); };
-    const Cut dx = cut_of(tiles(T, d), 2 * ((f + kK - 1) / kK), units);
-    const Cut dw = cut_of(2 * tiles(f, d), (T + kK - 1) / kK, units);
+    const auto tiles = [](int64_t n) { return (n + 255) / 256; };
+    const Cut dx = cut_of(tiles(T) * tiles(d), tiles(T), 2 * ((f + kK - 1) / kK), units);
+    const Cut dw = cut_of(2 * tiles(f) * tiles(d), tiles(f), (T + kK - 1) / kK, units);
     const Laid l = laid_of(T, d, f, 1);
     Space w;
     w.parts = (size_t)std::max(dx.parts, dw.parts) * (256 * 256 * sizeof(float));
