@@ -220,9 +220,10 @@ int current_device()
 }  // namespace
 
 bool tensor_map_2d(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t row_bytes,
-                   uint32_t box_inner, uint32_t box_outer)
+                   uint32_t box_inner, uint32_t box_outer, bool two_lines)
 {
-    return map2d(m, ptr, inner, outer, row_bytes, box_inner, box_outer, true, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
+    return map2d(m, ptr, inner, outer, row_bytes, box_inner, box_outer, true,
+                 two_lines ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 }  // namespace tc

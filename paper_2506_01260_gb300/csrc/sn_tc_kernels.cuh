@@ -247,9 +247,10 @@ __host__ __device__ inline int64_t tile_row0(int tile, int reorder, int batches,
 // ---- host side -----------------------------------------------------------------------
 // A 2-D bf16 tensor of `outer` rows x `inner` elements, `row_bytes` apart, in 128-byte swizzled boxes.
 // L2 fetches 128 bytes at a time for it: where rows start off their 256 bytes, dX of 4173 x 2056 x 5512
-// takes 143 us, 158 with 256 (rows on them: the same).
+// takes 143 us, 158 with 256 (rows on them: the same).  two_lines: 256, for what comes from DRAM once
+// (weights for 1 and 75 tokens of 4096 x 14336: 37.5 and 40.6 us, 38.3 and 43.4 with 128).
 bool tensor_map_2d(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t row_bytes,
-                   uint32_t box_inner, uint32_t box_outer);
+                   uint32_t box_inner, uint32_t box_outer, bool two_lines = false);
 cudaError_t launch_contract(int mode, const ContractParams &p, int grid, cudaStream_t s);
 cudaError_t launch_expand(int amode, const ExpandParams &p, int grid, cudaStream_t s);
 cudaError_t launch_reconstruct(const ExpandParams &p, int grid, cudaStream_t s);
