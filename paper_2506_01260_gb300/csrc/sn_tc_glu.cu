@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
     // A warp issues copies and one issues products: all its lanes walk the loop and one is elected
     // at each issue, so that what the instructions read is the warp's alike and lies in uniform
     // registers.  (With one lane in the loop, a chunk's four products took that lane 630 cycles to
-    // issue, and the tensor cores 512 to do.)
+    // issue, and the tensor cores 547 to do.)
     if (warp == 0) {
         // ---------------------------------------------------------------- TMA producer
         Ring ring;
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
                     commit<CG>(accf_b + 8 * b);
                 __syncwarp();
             }
-            if (!ok && lane == 0) {    // products already issued end before TMEM is freed
+            if (!ok && elected()) {    // products already issued end before TMEM is freed
                 commit<CG>(drain_b);
                 drain_wait(drain_b, 0);
             }
@@ -864,7 +864,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
                 mma_commit(accf_b);
             __syncwarp();
         }
-        if (!ok && lane == 0) {
+        if (!ok && elected()) {        // (by the lane that issued them)
             mma_commit(drain_b);
             drain_wait(drain_b, 0);
         }
