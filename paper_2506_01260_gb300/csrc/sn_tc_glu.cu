@@ -18,7 +18,7 @@
 // Measured, 8192 x 4096 x 14336 (T, d, f): forward 962 us (2.00 PFLOP/s), with G and U 999, dG and dU
 // 170 (6.9 TB/s), dX 995, the weights' gradients 985; at these rates the chip's power sets the clock
 // (1.63 to 1.75 GHz, tensor cores at work 94 to 95% of the cycles), and runs differ by 5%.  1 token of
-// 4096 x 14336 36.7 us (6.4 TB/s), 75 tokens 41, 1 of 8192 x 28672 137 (6.9 TB/s).
+// 4096 x 14336 37.5 us (6.3 TB/s), 75 tokens 40.7, 1 of 8192 x 28672 139 (6.8 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -558,8 +558,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
     } else {
         // ---------------------------------------------------------------- epilogue
         // A warp has 32 rows (its TMEM lane quarter) and half of the columns, and sends 128 bytes
-        // of its rows at a time through its staging rows: stored by the threads, a row each, the
-        // outputs took 5 to 10% of the products' time.
+        // of its rows at a time through its staging rows, whole lines of the output.
         const int q = warp & 3, half = (warp - 2) >> 2;
         const uint32_t out = base + St::kOut + (warp - 2) * kOutBytes;
         Work w;
