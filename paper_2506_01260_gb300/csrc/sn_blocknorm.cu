@@ -15,7 +15,7 @@
 //   sum e y = (sum m y g - mean(g n2) sum m y n2) / rms(h) + sum m y dh,
 // so a row's six sums meet once.
 //
-// Measured: forward of 16384 bf16 rows of 4096 80 us (6.7 TB/s), of 65536 of 8192 with 16 gates 660 (6.5);
+// Measured: forward of 16384 bf16 rows of 4096 80 us (6.7 TB/s), of 65536 of 8192 with 16 gates 644 (6.7);
 // gradient 126 us (6.4 TB/s, 5 us of it the sum of the parts) and 960 (6.7), of 4173 fp32 rows of 2056 37
 // (5.6), where the 14 rows a block walks and the sum of the parts cost latency.
 #include <algorithm>
@@ -71,7 +71,7 @@ __device__ __forceinline__ int64_t gate_of(const Args &a, int64_t t)
 template <int S, int C>
 constexpr int kResident = S > 512 ? S : S == 512 ? 1024 : C == 1 ? 1536 : C == 2 ? 1024 : 768;
 
-template <typename T, int S, bool EXACT, int C>
+template <typename T, int S, bool EXACT, int C, bool GATED>
 __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<S, C> / Shape<S>::kThreads)
     k_blocknorm(const Args a)
 {
@@ -86,13 +86,16 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<S, C> / Shape<S>
     for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
         const int64_t t = t0 + (S == 32 ? threadIdx.x / 32 : 0);
         const bool live = S != 32 || t < a.T;
-        uint4 yv[C], rv[C];
+        uint4 yv[C], rv[C], gv[GATED ? C : 1];
+        const T *g = GATED ? gate + gate_of(a, live ? t : 0) * a.d : nullptr;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
             const bool in = live && j < nv;
             yv[i] = in ? *((const uint4 *)(Y + t * a.ldy) + j) : make_uint4(0, 0, 0, 0);
             rv[i] = in ? *((const uint4 *)(R + t * a.d) + j) : make_uint4(0, 0, 0, 0);
+            if (GATED)       // (asked for behind the sums, 32768 rows of 2048 with 128 gates took 96 us, 79 now)
+                gv[GATED ? i : 0] = in ? __ldg((const uint4 *)g + j) : make_uint4(0, 0, 0, 0);
         }
         float2 h[C][P], sq;
         float s[1], eps = a.eps, f = 1.f;
@@ -130,7 +133,6 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<S, C> / Shape<S>
         for (int i = 0; i < C; ++i)
             unpack_pairs(yv[i], h[i]);
         const float r1 = root() * a.scale;
-        const T *g = gate && live ? gate + gate_of(a, t) * a.d : nullptr;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int j = lane + G * i;
@@ -142,9 +144,9 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kResident<S, C> / Shape<S>
 #pragma unroll
                 for (int k = 0; k < P; ++k)
                     h[i][k] = mul2(h[i][k], mul2(both(r1), make_float2(w[2 * k], w[2 * k + 1])));
-                if (g) {
+                if (GATED) {
                     float2 m[P];
-                    unpack_pairs(__ldg((const uint4 *)g + j), m);
+                    unpack_pairs(gv[GATED ? i : 0], m);
 #pragma unroll
                     for (int k = 0; k < P; ++k)
                         h[i][k] = mul2(h[i][k], m[k]);
@@ -764,8 +766,10 @@ cudaError_t fwd_rows(const Args &a, int lanes, cudaStream_t s)
 {
     constexpr int kRows = Shape<S>::kRows;
     const int64_t blocks = (a.T + kRows - 1) / kRows;
-    return launch(k_blocknorm<T, S, EXACT, C>, std::min<int64_t>(blocks, (int64_t)1 << 30), S == 32 ? 256 : lanes, a,
-                  s);
+    const int64_t grid = std::min<int64_t>(blocks, (int64_t)1 << 30);
+    const int threads = S == 32 ? 256 : lanes;
+    return a.gate ? launch(k_blocknorm<T, S, EXACT, C, true>, grid, threads, a, s)
+                  : launch(k_blocknorm<T, S, EXACT, C, false>, grid, threads, a, s);
 }
 
 template <typename T>
@@ -837,8 +841,9 @@ cudaError_t bwd_rows(const Plan &p, const Args &a, cudaStream_t s)
     if (e != cudaSuccess)
         return e;
     count_launch();
-    e = launch_dependent(k_blocknorm_bwd<T, S, C>, dim3((unsigned)((p.workers + p.rows_at_once - 1) / p.rows_at_once)), dim3(p.threads), smem,
-                         s, a);
+    e = launch_dependent(k_blocknorm_bwd<T, S, C>,
+                         dim3((unsigned)((p.workers + p.rows_at_once - 1) / p.rows_at_once)), dim3(p.threads), smem, s,
+                         a);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

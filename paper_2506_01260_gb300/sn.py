@@ -111,7 +111,8 @@ EXPORTS = ["sn_basis_create", "sn_basis_destroy", "sn_basis_shape", "sn_compress
            "sn_embed_fwd", "sn_embed_bwd_workspace", "sn_embed_bwd", "sn_rmsnorm_fwd",
            "sn_rmsnorm_fwd_quant", "sn_rmsnorm_bwd_workspace", "sn_rmsnorm_bwd",
            "sn_blocknorm_fwd", "sn_blocknorm_bwd_workspace", "sn_blocknorm_bwd", "sn_logprob_fwd",
-           "sn_logprob_bwd", "sn_glu_fwd", "sn_glu_bwd_workspace", "sn_glu_bwd", "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
+           "sn_logprob_bwd", "sn_glu_fwd", "sn_glu_bwd_workspace", "sn_glu_bwd",
+           "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
            "sn_wire_bytes", "sn_wire_send",
            "sn_wire_recv", "sn_check_errors", "sn_selftest_wait_timeout",
            "sn_selftest_barrier_timeout", "sn_launch_count",
