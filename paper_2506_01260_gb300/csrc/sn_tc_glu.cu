@@ -1099,9 +1099,8 @@ bool out_map(CUtensorMap *m, const void *out, int cols, int64_t rows, bool f32)
 // Pairs of CTAs where the stream's context has the whole GPU; with a part of it a pair might find
 // no place.
 template <int MODE>
-cudaError_t launch_products(const GluParams &p, cudaStream_t s)
+cudaError_t launch_products(const GluParams &p, int all, int sms, cudaStream_t s)
 {
-    const int all = device_sms(), sms = stream_sms(s);
     return sms < all ? launch_tiles<MODE, 1>(p, sms, s) : launch_tiles<MODE, 2>(p, sms, s);
 }
 
@@ -1183,7 +1182,7 @@ cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, 
         !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)d * 2, kK, 128) ||
         !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)d * 2, kK, 128))
         return cudaErrorInvalidValue;
-    return launch_products<GLU_FWD>(p, s);
+    return launch_products<GLU_FWD>(p, device_sms(), sms, s);
 }
 
 namespace tc {
@@ -1223,14 +1222,15 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
     const bool one = lddh == f;
     const GradArgs a{(const b16 *)dH, (const b16 *)G, (const b16 *)U, (b16 *)dG, (b16 *)dU, one ? 1 : T, lddh,
                      one ? T * (f / 8) : f / 8, act};
-    const int64_t across = std::min<int64_t>((a.f8 + 255) / 256, 8 * device_sms());
+    const int all = device_sms(), sms = dX || dWg ? stream_sms(s) : all;
+    const int64_t across = std::min<int64_t>((a.f8 + 255) / 256, 8 * all);
     count_launch();
     cudaError_t e = launch_dependent(k_glu_grad, dim3((unsigned)across, (unsigned)std::min<int64_t>(a.T, 65535)),
                                      dim3(256), 0, s, a);
     if (e == cudaSuccess)
         e = cudaGetLastError();
     const Laid l = laid_of(T, d, f, ldx);
-    char *anew = (char *)ws + space_of(T, d, f).parts;
+    char *anew = l.X || l.W ? (char *)ws + space_of(T, d, f).parts : nullptr;
     if (e == cudaSuccess && dX) {
         int64_t ld = d;
         if (l.W) {
@@ -1253,7 +1253,7 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
             !tensor_map_2d(&p.B[0], Wg, d, f, (uint64_t)ld * 2, 64, kK) ||
             !tensor_map_2d(&p.B[1], Wu, d, f, (uint64_t)ld * 2, 64, kK))
             return cudaErrorInvalidValue;
-        e = launch_products<GLU_DX>(p, s);
+        e = launch_products<GLU_DX>(p, all, sms, s);
     }
     if (e == cudaSuccess && dWg) {
         if (l.X) {
@@ -1278,7 +1278,7 @@ cudaError_t glu_bwd(const void *dH, int64_t lddh, const void *X, int64_t ldx, co
             !tensor_map_2d(&p.A[1], dU, f, T, (uint64_t)f * 2, 64, kK) ||
             !tensor_map_2d(&p.B[0], X, d, T, (uint64_t)ldx * 2, 64, kK))
             return cudaErrorInvalidValue;
-        e = launch_products<GLU_DW>(p, s);
+        e = launch_products<GLU_DW>(p, all, sms, s);
     }
     return e;
 }

@@ -919,8 +919,9 @@ def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None,
     else:
         dW_gate = dW_up = None
     if workspace is None:
-        nbytes = max(16, sn_glu_bwd_workspace(T, d, f))
-        workspace = empty(nbytes, dtype=torch.uint8, device=dev)
+        nbytes = sn_glu_bwd_workspace(T, d, f)
+        if nbytes:
+            workspace = empty(nbytes, dtype=torch.uint8, device=dev)
     else:
         _need(workspace, "workspace")
         nbytes = workspace.numel() * workspace.element_size()
@@ -928,7 +929,7 @@ def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None,
                            W_gate.data_ptr(), W_up.data_ptr(), G.data_ptr(), U.data_ptr(), T, d, f,
                            ACTIVATIONS[act], dG.data_ptr(), dU.data_ptr(), _ptr(dX),
                            _dtype(dW_gate) if need_dW else SN_BF16, _ptr(dW_gate), _ptr(dW_up),
-                           bool(accumulate), workspace.data_ptr(), nbytes, _stream_of(dH, stream)),
+                           bool(accumulate), _ptr(workspace), nbytes, _stream_of(dH, stream)),
            "sn_glu_bwd")
     return dX, dW_gate, dW_up, dG, dU
 

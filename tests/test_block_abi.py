@@ -117,7 +117,7 @@ def test_memory_is_the_given_streams(stand_in, no_sizes, name):  # noqa: F811
         "blocknorm_fwd": lambda s: sn.sn_blocknorm_fwd(X, X, w, w, 1e-5, gate=gate, stream=s),
         "blocknorm_bwd": lambda s: sn.sn_blocknorm_bwd(X, X, X, w, w, 1e-5, gate=gate, dH=X, stream=s),
     }[name]
-    many = {"glu_fwd": 1, "glu_fwd_keep": 3, "glu_bwd": 6, "blocknorm_fwd": 2, "blocknorm_bwd": 6}[name]
+    many = {"glu_fwd": 1, "glu_fwd_keep": 3, "glu_bwd": 5, "blocknorm_fwd": 2, "blocknorm_bwd": 6}[name]
     for given in (GIVEN, types.SimpleNamespace(cuda_stream=GIVEN)):
         del streams[:], made[:]
         call(given)
