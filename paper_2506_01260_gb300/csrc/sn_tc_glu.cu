@@ -1096,12 +1096,26 @@ bool out_map(CUtensorMap *m, const void *out, int cols, int64_t rows, bool f32)
     return tensor_map_2d(m, out, (uint64_t)cols * (f32 ? 2 : 1), rows, (uint64_t)cols * (f32 ? 4 : 2), 64, 32);
 }
 
+// Whether the forward is expected earlier from CTAs each for itself, in cycles: a chunk takes them 650 and
+// a pair 547, a pair's start and end 3300 more, and tiles of half the rows may fill the rounds better (us,
+// pairs and single CTAs: 1024 tokens of 512 x 2048 9.2 and 7.9, 300 of 1024 x 4096 11.8 and 10.8, 640 of
+// 4096 x 14336 109 and 102; 300 of 2048 x 8192 26.0 and 30.6, 2048 of 4096 x 14336 267 and 310).
+bool alone(const GluParams &p, int sms)
+{
+    const int64_t nt = (p.cols + kCols / 2 - 1) / (kCols / 2);
+    const auto rounds = [&](int rows, int units) {
+        return ((p.rows + rows - 1) / rows * nt + units - 1) / units;
+    };
+    return rounds(kRows, sms) * p.chunks * 650 < rounds(2 * kRows, std::max(1, sms / 2)) * p.chunks * 547 + 3300;
+}
+
 // Pairs of CTAs where the stream's context has the whole GPU; with a part of it a pair might find
 // no place.
 template <int MODE>
 cudaError_t launch_products(const GluParams &p, int all, int sms, cudaStream_t s)
 {
-    return sms < all ? launch_tiles<MODE, 1>(p, sms, s) : launch_tiles<MODE, 2>(p, sms, s);
+    return sms < all || (MODE == GLU_FWD && alone(p, sms)) ? launch_tiles<MODE, 1>(p, sms, s)
+                                                           : launch_tiles<MODE, 2>(p, sms, s);
 }
 
 // Rows of each weight that a CTA takes at a time, in as few rounds as 128 rows allow
