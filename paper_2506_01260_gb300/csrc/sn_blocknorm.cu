@@ -49,7 +49,11 @@ struct Args {
     // [parts, d], a part a block, of dw_pre and (gated: a part a worker) of dw_post, which is S
     // itself where it is one for all tokens
     float *part_pre, *part_post;
-    float *part_gate;           // gated: [workers + gates, d], S of worker w and gate i at w + i
+    // gated: S of a worker and a gate that it shares with others.  A worker shares two gates at most, the
+    // one that its first token lies inside of, at 2 w, and the one that its last does, at 2 w + 1; with
+    // fewer gates than workers (few_gates) worker w's of gate i at w + i are fewer rows.
+    float *part_gate;
+    bool few_gates;
 };
 
 // half of a factor's exponent: taken on either side of a product, nothing in between leaves fp32
@@ -222,6 +226,12 @@ __global__ void __launch_bounds__(kAnyThreads) k_blocknorm_any(const Args a)
 // Of T tokens, worker w of W takes those from w T / W on; token t is worker ((t + 1) W - 1) / T's.
 __device__ __forceinline__ int64_t first_token(int64_t w, int64_t W, int64_t T) { return w * T / W; }
 __device__ __forceinline__ int64_t worker_of(int64_t t, int64_t W, int64_t T) { return ((t + 1) * W - 1) / T; }
+
+// The row of part_gate for worker w's tokens of gate i from t on
+__device__ __forceinline__ int64_t shared_at(const Args &a, int64_t w, int64_t i, int64_t t)
+{
+    return a.few_gates ? w + i : 2 * w + (t == i * a.per_gate);
+}
 
 // The six sums of a row, over its elements or pairs of them
 template <typename F>
@@ -560,7 +570,7 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
             load_weight(a.post, j * N, w);
             Vec<T>::unpack(__ldg((const uint4 *)((const T *)a.gate + i_gate * a.d) + j), g);
             float *post = a.part_post + worker * a.d + j * N;
-            float *to = whole ? a.dgate + i_gate * a.d + j * N : a.part_gate + (worker + i_gate) * a.d + j * N;
+            float *to = (whole ? a.dgate + i_gate * a.d : a.part_gate + shared_at(a, worker, i_gate, t0) * a.d) + j * N;
 #pragma unroll
             for (int k = 0; k < N; k += 4) {
                 float4 q = make_float4(sum[i][k / 2].x, sum[i][k / 2].y, sum[i][k / 2 + 1].x, sum[i][k / 2 + 1].y);
@@ -630,7 +640,7 @@ __global__ void __launch_bounds__(kAnyThreads) k_blocknorm_bwd_any(const Args a)
     for (int64_t t = first_token(blockIdx.x, gridDim.x, a.T); t < t1;) {
         const int64_t i = a.gated ? gate_of(a, t) : 0, end = a.gated ? min(t1, (i + 1) * a.per_gate) : t1;
         const bool whole = end - t == a.per_gate;
-        float *to = !a.gated ? nullptr : whole ? a.dgate + i * a.d : a.part_gate + (blockIdx.x + i) * a.d;
+        float *to = !a.gated ? nullptr : whole ? a.dgate + i * a.d : a.part_gate + shared_at(a, blockIdx.x, i, t) * a.d;
         if (to && !(whole && a.add))
             for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
                 to[j] = 0.f;
@@ -677,7 +687,7 @@ struct JoinArgs {
     int d;
     int64_t T, workers, gates, per_gate, looked;
     int runs;
-    bool add;
+    bool few_gates, add;
 };
 // dw_pre and dw_post (blockIdx.y): 32 columns and 32 runs of parts a block.  Where S is one for all
 // tokens, it makes dw_post and dgate.
@@ -727,11 +737,13 @@ __global__ void __launch_bounds__(256) k_blocknorm_dgate(const JoinArgs a)
             const int64_t w1 = worker_of((i + 1) * a.per_gate - 1, a.workers, a.T);
             if (w0 < w1 && (a.looked == a.gates || w0 == y)) {       // not one worker's, nor another warp's
                 to = a.dgate + i * a.d + j;
-                const float *part = a.gate + (w0 + i) * a.d + j;
+                // (see shared_at: worker w0 has the gate's first token, the others' first tokens lie inside)
+                const float *part = a.gate + (a.few_gates ? w0 + i : 2 * w0) * a.d + j;
+                const int64_t step = a.few_gates ? a.d : 2 * (int64_t)a.d, front = a.few_gates ? 0 : a.d;
                 const int parts = (int)(w1 - w0 + 1), per = (parts + a.runs - 1) / a.runs;
 #pragma unroll 8
                 for (int p = run * per, end = min(parts, p + per); p < end; ++p)
-                    s += __ldg(part + (int64_t)p * a.d);
+                    s += __ldg(part + (p == 0 ? front : p * step));
             }
         }
         if (a.runs > 1) {
@@ -824,7 +836,10 @@ Plan plan_of(int64_t T_, int d, bool registers, int64_t gates)
     }
     p.workers = std::min<int64_t>(T_, (int64_t)device_sms() * per_sm * p.rows_at_once);
     p.part = (size_t)p.workers * d;
-    p.gate_parts = gates > 1 ? (size_t)(p.workers + gates) * d : 0;
+    // (none where every gate is one worker's)
+    const int64_t per = p.workers > 0 && T_ % p.workers == 0 ? T_ / p.workers : 1;
+    const bool shared = gates > 1 && gates < T_ && per % (T_ / gates) != 0;
+    p.gate_parts = shared ? (size_t)(p.workers + std::min(p.workers, gates)) * d : 0;
     return p;
 }
 
@@ -857,6 +872,7 @@ cudaError_t bwd(Args a, int64_t gates, float *dw_post, float *dw_pre, float *ws,
     a.part_pre = ws;
     a.part_post = ws + p.part;
     a.part_gate = ws + 2 * p.part;
+    a.few_gates = gates < p.workers;
     const int nv = a.d / Vec<T>::N;
     cudaError_t e;
     if (!registers)
@@ -875,7 +891,7 @@ cudaError_t bwd(Args a, int64_t gates, float *dw_post, float *dw_pre, float *ws,
     const int blocks = (int)((p.workers + p.rows_at_once - 1) / p.rows_at_once);
     const JoinArgs j{a.part_pre, a.part_post, a.part_gate, blocks, gates > 1 ? (int)p.workers : blocks, dw_pre, dw_post,
                      a.dgate, a.post, gates == 1 ? a.gate : nullptr, sizeof(T) == 2, a.scale, a.d, a.T, p.workers,
-                     gates, a.per_gate, looked, p.workers >= 8 * gates ? 8 : 1, a.add};
+                     gates, a.per_gate, looked, p.workers >= 8 * gates ? 8 : 1, a.few_gates, a.add};
     const unsigned across = (unsigned)((a.d - 1) / 32 + 1);
     count_launch();
     e = launch_dependent(k_blocknorm_dw, dim3(across, 2), dim3(32, 32), 0, s, j);
