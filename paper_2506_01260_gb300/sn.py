@@ -559,6 +559,23 @@ def _given_or(t, name, shape, dtype, empty, device):
     return t
 
 
+def _kept_by_device(size):
+    """A workspace's size goes by its arguments and the current device's SMs: asked for once for each
+    device.  (Without torch's CUDA state the current device is not known here.)"""
+    @functools.lru_cache(maxsize=256)
+    def kept(device, *args, **named):
+        return size(*args, **named)
+
+    @functools.wraps(size)
+    def of_device(*args, **named):
+        if not torch.cuda.is_initialized():
+            return size(*args, **named)
+        return kept(torch.cuda.current_device(), *args, **named)
+
+    of_device.cache_clear = kept.cache_clear
+    return of_device
+
+
 def _stream_of(t, stream):
     """As _stream; by default the current stream of t's device."""
     return _raw_stream(t.get_device()) if stream is None else _stream(stream)
@@ -588,7 +605,7 @@ def sn_embed_fwd(table, ids, scale=1.0, out=None, out_dtype=None, basis=None, st
     return out
 
 
-@functools.lru_cache(maxsize=256)
+@_kept_by_device
 def sn_embed_bwd_workspace(T, vocab, d):
     n = _SZ()
     _check(_lib.sn_embed_bwd_workspace(T, vocab, d, ctypes.byref(n)), "sn_embed_bwd_workspace")
@@ -674,7 +691,7 @@ def sn_rmsnorm_fwd_quant(X, w, eps, fmt, R=None, H=None, group=0, codes=None, sc
     return codes, scale, X if H is None else H
 
 
-@functools.lru_cache(maxsize=256)
+@_kept_by_device
 def sn_rmsnorm_bwd_workspace(T, d):
     n = _SZ()
     _check(_lib.sn_rmsnorm_bwd_workspace(T, d, ctypes.byref(n)), "sn_rmsnorm_bwd_workspace")
@@ -750,7 +767,7 @@ def sn_blocknorm_fwd(Y, R, w_post, w_pre, eps, scale=1.0, gate=None, H=None, out
     return out, H
 
 
-@functools.lru_cache(maxsize=256)
+@_kept_by_device
 def sn_blocknorm_bwd_workspace(T, d, gates):
     n = _SZ()
     _check(_lib.sn_blocknorm_bwd_workspace(T, d, gates, ctypes.byref(n)),
@@ -879,7 +896,7 @@ def sn_glu_fwd(X, W_gate, W_up, act="silu", keep=False, out=None, G=None, U=None
     return out, G, U
 
 
-@functools.lru_cache(maxsize=256)
+@_kept_by_device
 def sn_glu_bwd_workspace(T, d, f):
     n = _SZ()
     _check(_lib.sn_glu_bwd_workspace(T, d, f, ctypes.byref(n)), "sn_glu_bwd_workspace")
