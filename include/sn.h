@@ -40,7 +40,10 @@
  *     (other streams, other host threads), nor backward calls each other; a
  *     forward and a backward call may.
  *   - Every wait inside a kernel is bounded; a wait that expires records
- *     SN_ERR_TIMEOUT in the error word and the kernel returns.
+ *     SN_ERR_TIMEOUT in the error word and the kernel returns, its outputs
+ *     unfinished.  Calls that wait without a basis (the gated projections with
+ *     `errors` NULL) record it in a word of the device's own, which every
+ *     sn_check_errors reports.
  */
 #ifndef SN_H
 #define SN_H
@@ -437,7 +440,8 @@ sn_status sn_logprob_bwd(sn_dtype dtype, const void *logits, int64_t T, int64_t 
  * relu.  bf16 only (SN_ERR_UNSUPPORTED for SN_F32); products accumulate in fp32, and every
  * output is rounded once.  An infinity or a NaN gives what the formulas give, in its row of X or
  * column of a product alone.  d and f are multiples of 8 (SN_ERR_ALIGNMENT), at most 2^20.
- * `errors` is a basis, whose error word records a wait that expired, or NULL. */
+ * `errors` is a basis, whose error word records a wait that expired, or NULL: the device's own
+ * word does. */
 typedef enum { SN_ACT_SILU = 0, SN_ACT_GELU = 1, SN_ACT_GELU_TANH = 2, SN_ACT_RELU = 3 } sn_act;
 
 /* X: [T, d] with row stride ldx (elements, a multiple of 8); W_gate, W_up: [f, d]; H:
@@ -509,8 +513,10 @@ sn_status sn_wire_bytes(sn_basis_t basis, sn_dtype dtype, int64_t T, size_t *byt
 sn_status sn_wire_send(const void *src_device, void *dst_host, size_t bytes, sn_stream_t stream);
 sn_status sn_wire_recv(const void *src_host, void *dst_device, size_t bytes, sn_stream_t stream);
 
-/* Synchronise `stream`, then return and clear the basis' asynchronous error
- * (SN_ERR_BAD_ID or SN_ERR_TIMEOUT; SN_OK if none was recorded). */
+/* Synchronise `stream`, then return and clear the asynchronous errors of the basis
+ * (SN_ERR_BAD_ID, SN_ERR_TIMEOUT or SN_ERR_NUMERIC; SN_OK if none was recorded) and of
+ * the calls on the current device that wait without one (SN_ERR_TIMEOUT).  basis may be
+ * NULL: those calls' alone. */
 sn_status sn_check_errors(sn_basis_t basis, sn_stream_t stream);
 
 /* Failure-detection self-test of the bounded-wait rule: every in-kernel wait
@@ -530,6 +536,10 @@ sn_status sn_selftest_wait_timeout(sn_basis_t basis, sn_stream_t stream);
  * another: one CTA waits for arrivals that nobody makes, gives up at the limit with
  * SN_ERR_TIMEOUT, and a second wait ends at once on the flag that the first one left. */
 sn_status sn_selftest_barrier_timeout(sn_basis_t basis, sn_stream_t stream);
+
+/* The same for a call that waits without a basis: the next sn_check_errors on the device,
+ * of any basis or none, returns SN_ERR_TIMEOUT. */
+sn_status sn_selftest_unclaimed_timeout(sn_stream_t stream);
 
 /* Number of kernels this library has launched in this process. */
 uint64_t sn_launch_count(void);

@@ -1185,16 +1185,17 @@ sn_status sn_wire_recv(const void *src_host, void *dst_device, size_t bytes, sn_
 
 sn_status sn_check_errors(sn_basis_t b, sn_stream_t stream)
 {
-    if (!b)
-        return SN_ERR_INVALID_ARG;
-    unsigned int word = 0;
+    unsigned int word = 0, unclaimed = 0;
     cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
-    if (e == cudaSuccess)
+    if (e == cudaSuccess && b)
         e = cudaMemcpy(&word, b->err, sizeof word, cudaMemcpyDeviceToHost);
     if (e == cudaSuccess && word)
         e = cudaMemset(b->err, 0, sizeof word);
+    if (e == cudaSuccess)
+        e = sn::take_unclaimed(&unclaimed);
     if (e != cudaSuccess)
         return SN_ERR_CUDA;
+    word |= unclaimed;
     if (word & SN_EBIT_TIMEOUT)
         return SN_ERR_TIMEOUT;
     if (word & SN_EBIT_BAD_ID)

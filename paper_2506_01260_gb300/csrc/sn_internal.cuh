@@ -224,7 +224,10 @@ cudaError_t logprob_fwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld
 cudaError_t logprob_bwd(sn_dtype dt, const void *x, int64_t T, int V, int64_t ld, const int32_t *target,
                         const float *lse, const float *dlogp, const float *entropy, const float *dentropy,
                         float scale, void *dx, int64_t ldd, cudaStream_t s);
-// Gated projections of a feed-forward block; their gradients (err: null or a basis' error word)
+// Gated projections of a feed-forward block; their gradients (err: a basis' error word, or null: a wait
+// that expires is recorded in the current device's own, which take_unclaimed reads and clears)
+cudaError_t take_unclaimed(unsigned int *word);
+cudaError_t unclaimed_timeout(cudaStream_t s);   // records such a wait
 cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, int64_t T, int d, int f, int act,
                     void *G, void *U, void *H, unsigned int *err, cudaStream_t s);
 size_t glu_bwd_workspace(int64_t T, int d, int f);

@@ -13,6 +13,9 @@
 // sn_selftest_barrier_timeout: one CTA waits in the grid barrier of the cooperative kernels
 // for twice the arrivals that its grid makes, and gives up at the limit; its next wait
 // ends at once on the flag that the first one left.
+//
+// sn_selftest_unclaimed_timeout: one warp waits as the gated projections' do, for a phase that
+// nothing completes and without a basis, so that the device's own word records it.
 #include "sn_tc.cuh"
 
 namespace {
@@ -72,6 +75,11 @@ sn_status selftest(sn_basis_t b, void (*kernel)(unsigned int *), cudaStream_t st
 extern "C" sn_status sn_selftest_wait_timeout(sn_basis_t b, sn_stream_t stream)
 {
     return selftest(b, k_wait_timeout, (cudaStream_t)stream);
+}
+
+extern "C" sn_status sn_selftest_unclaimed_timeout(sn_stream_t stream)
+{
+    return sn::unclaimed_timeout((cudaStream_t)stream) == cudaSuccess ? SN_OK : SN_ERR_CUDA;
 }
 
 extern "C" sn_status sn_selftest_barrier_timeout(sn_basis_t b, sn_stream_t stream)

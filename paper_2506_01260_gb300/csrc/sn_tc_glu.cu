@@ -191,8 +191,11 @@ __device__ __forceinline__ bool mbar_test_cluster(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// A bounded wait of a whole warp, as warp_wait's; `err` may be null.  The votes tell the compiler
-// that the warp stays together.  CLUSTER: for what the other CTA's threads have done.
+// Where a wait that expires is recorded in calls without an error word of their own, one a device
+__device__ unsigned int g_unclaimed;
+
+// A bounded wait of a whole warp, as warp_wait's; `err` may be null (g_unclaimed).  The votes tell the
+// compiler that the warp stays together.  CLUSTER: for what the other CTA's threads have done.
 template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *abort, unsigned int *err)
 {
@@ -209,8 +212,8 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
             return false;
         if (__any_sync(0xffffffffu, global_ns() - t0 > kWaitLimitNs)) {
             *abort = 1;
-            if (err && threadIdx.x % 32 == 0)
-                atomicOr(err, SN_EBIT_TIMEOUT);
+            if (threadIdx.x % 32 == 0)
+                atomicOr(err ? err : &g_unclaimed, SN_EBIT_TIMEOUT);
             return false;
         }
     }
@@ -1002,6 +1005,20 @@ __global__ void __launch_bounds__(256) k_glu_lay(const LayArgs a)
     }
 }
 
+// A wait for a phase that nothing completes, without an error word
+__global__ void __launch_bounds__(32) k_unclaimed_timeout()
+{
+    __shared__ __align__(8) uint64_t bar;
+    __shared__ int abort_flag;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&bar), 1);
+        abort_flag = 0;
+        mbar_fence_init();
+    }
+    __syncthreads();
+    wait(smem_u32(&bar), 0, &abort_flag, nullptr);
+}
+
 // ---- launches ------------------------------------------------------------------------------------
 
 // Whether X (for the weights' gradients) and the weights (for dX) are laid out anew: where neither d nor
@@ -1165,6 +1182,19 @@ cudaError_t launch_few(FewParams p, const __nv_bfloat16 *X, int64_t ldx, const _
 
 }  // namespace
 }  // namespace tc
+
+cudaError_t take_unclaimed(unsigned int *word)
+{
+    const unsigned int none = 0;
+    const cudaError_t e = cudaMemcpyFromSymbol(word, tc::g_unclaimed, sizeof none);
+    return e == cudaSuccess && *word ? cudaMemcpyToSymbol(tc::g_unclaimed, &none, sizeof none) : e;
+}
+cudaError_t unclaimed_timeout(cudaStream_t s)
+{
+    count_launch();
+    tc::k_unclaimed_timeout<<<1, 32, 0, s>>>();
+    return cudaGetLastError();
+}
 
 cudaError_t glu_fwd(const void *X, int64_t ldx, const void *Wg, const void *Wu, int64_t T, int d, int f, int act,
                     void *G, void *U, void *H, unsigned int *err, cudaStream_t s)

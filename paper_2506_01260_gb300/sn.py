@@ -96,6 +96,7 @@ _sig("sn_wire_send", [_P, _P, _SZ, _P])
 _sig("sn_wire_recv", [_P, _P, _SZ, _P])
 _sig("sn_check_errors", [_P, _P])
 _sig("sn_selftest_wait_timeout", [_P, _P])
+_sig("sn_selftest_unclaimed_timeout", [_P])
 _sig("sn_selftest_barrier_timeout", [_P, _P])
 _sig("sn_launch_count", [], ctypes.c_uint64)
 _sig("sn_status_string", [_ST], ctypes.c_char_p)
@@ -115,7 +116,7 @@ EXPORTS = ["sn_basis_create", "sn_basis_destroy", "sn_basis_shape", "sn_compress
            "sn_grads_create", "sn_grads_destroy", "sn_grads_sumsq", "sn_grads_clip",
            "sn_wire_bytes", "sn_wire_send",
            "sn_wire_recv", "sn_check_errors", "sn_selftest_wait_timeout",
-           "sn_selftest_barrier_timeout", "sn_launch_count",
+           "sn_selftest_barrier_timeout", "sn_selftest_unclaimed_timeout", "sn_launch_count",
            "sn_status_string"]
 
 
@@ -877,7 +878,8 @@ def sn_glu_fwd(X, W_gate, W_up, act="silu", keep=False, out=None, G=None, U=None
                stream=None):
     """H = act(X W_gate^T) * (X W_up^T) for X [T, d] and weights [f, d]; returns (H, G, U): the two
     products, bf16 as the gradient reads them, with keep=True (or where given), else None.  X may
-    be a row-strided view; act "silu", "gelu", "gelu_tanh" or "relu"."""
+    be a row-strided view; act "silu", "gelu", "gelu_tanh" or "relu".  A wait that expired in the
+    kernel is reported by sn_check_errors (of the basis, or without one by the next of any)."""
     ldx = _rows(X, "X")
     T, d = X.shape
     _need(W_gate, "W_gate", X.dtype)
@@ -1173,9 +1175,10 @@ def sn_wire_recv(src_host, dst_device, stream=None):
     return dst_device
 
 
-def sn_check_errors(basis, stream=None):
-    """Synchronise the stream; raise SNError if a bad id or a timeout was recorded."""
-    _check(_lib.sn_check_errors(basis.handle, _stream(stream)), "sn_check_errors")
+def sn_check_errors(basis=None, stream=None):
+    """Synchronise the stream; raise SNError if a bad id or a timeout was recorded for the basis, or
+    a timeout for a call that was given none (without a basis: those calls' alone)."""
+    _check(_lib.sn_check_errors(_error_basis(basis), _stream(stream)), "sn_check_errors")
 
 
 def sn_selftest_wait_timeout(basis, stream=None):
@@ -1191,6 +1194,12 @@ def sn_selftest_barrier_timeout(basis, stream=None):
     nobody makes and gives up at the limit."""
     _check(_lib.sn_selftest_barrier_timeout(basis.handle, _stream(stream)),
            "sn_selftest_barrier_timeout")
+
+
+def sn_selftest_unclaimed_timeout(stream=None):
+    """The same for a call that waits without a basis: the next sn_check_errors, of any basis or
+    none, reports it."""
+    _check(_lib.sn_selftest_unclaimed_timeout(_stream(stream)), "sn_selftest_unclaimed_timeout")
 
 
 def sn_launch_count():
