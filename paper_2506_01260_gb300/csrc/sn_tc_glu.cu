@@ -191,33 +191,6 @@ __device__ __forceinline__ bool mbar_test_cluster(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// Where a wait that expires is recorded in calls without an error word of their own, one a device
-__device__ unsigned int g_unclaimed;
-
-// A bounded wait of a whole warp, as warp_wait's; `err` may be null (g_unclaimed).  The votes tell the
-// compiler that the warp stays together.  CLUSTER: for what the other CTA's threads have done.
-template <bool CLUSTER = false>
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *abort, unsigned int *err)
-{
-    const auto test = [&] {
-        return __all_sync(0xffffffffu, CLUSTER ? mbar_test_cluster(bar, parity) : mbar_test(bar, parity));
-    };
-    if (test())
-        return true;
-    const uint64_t t0 = global_ns();
-    while (true) {
-        if (test())
-            return true;
-        if (__any_sync(0xffffffffu, *abort))
-            return false;
-        if (__any_sync(0xffffffffu, global_ns() - t0 > kWaitLimitNs)) {
-            *abort = 1;
-            if (threadIdx.x % 32 == 0)
-                atomicOr(err ? err : &g_unclaimed, SN_EBIT_TIMEOUT);
-            return false;
-        }
-    }
-}
 // Whether a phase has completed, without waiting at all
 __device__ __forceinline__ uint32_t peek(uint32_t bar, uint32_t parity)
 {
@@ -229,6 +202,41 @@ __device__ __forceinline__ uint32_t peek(uint32_t bar, uint32_t parity)
         : "r"(bar), "r"(parity)
         : "memory");
     return ok;
+}
+// Where a wait that expires is recorded in calls without an error word of their own, one a device
+__device__ unsigned int g_unclaimed;
+
+// A bounded wait of a whole warp, as warp_wait's; `err` may be null (g_unclaimed).  The votes tell the
+// compiler that the warp stays together.  CLUSTER: for what the other CTA's threads have done.
+// `moving`: a barrier whose phases go on while what the wait is for is at work, and the limit starts
+// again at each: a tile of dW may take longer than it (one CTA's of 640 million tokens 3.3 s).
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *abort, unsigned int *err,
+                                     uint32_t moving = 0)
+{
+    const auto test = [&] {
+        return __all_sync(0xffffffffu, CLUSTER ? mbar_test_cluster(bar, parity) : mbar_test(bar, parity));
+    };
+    if (test())
+        return true;
+    uint64_t t0 = global_ns();
+    bool phase = false;
+    while (true) {
+        if (test())
+            return true;
+        if (__any_sync(0xffffffffu, *abort))
+            return false;
+        if (moving && __any_sync(0xffffffffu, peek(moving, 0)) != phase) {
+            phase = !phase;
+            t0 = global_ns();
+        }
+        if (__any_sync(0xffffffffu, global_ns() - t0 > kWaitLimitNs)) {
+            *abort = 1;
+            if (threadIdx.x % 32 == 0)
+                atomicOr(err ? err : &g_unclaimed, SN_EBIT_TIMEOUT);
+            return false;
+        }
+    }
 }
 // Whether `is` holds in all 256 threads of the eight epilogue warps; a barrier for them
 __device__ __forceinline__ bool all_of_eight(bool is)
@@ -568,7 +576,7 @@ __global__ void __launch_bounds__(kGluThreads, 1) k_glu(const __grid_constant__ 
         for (uint32_t it = 0; work_at<MODE, CG>(p, it, w); ++it) {
             const Tile &t = w.t;
             const uint32_t b = it & 1, nb = it >> 1;
-            if (!wait(accf_b + 8 * b, nb & 1, abort_flag, p.err))
+            if (!wait(accf_b + 8 * b, nb & 1, abort_flag, p.err, empty_b))
                 break;
             tc_fence_after();
             const uint32_t taddr = tmem + b * kCols + ((uint32_t)(32 * q) << 16);
