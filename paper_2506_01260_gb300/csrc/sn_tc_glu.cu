@@ -34,13 +34,21 @@ enum { GLU_FWD = 0, GLU_DX = 1, GLU_DW = 2 };
 
 // ---- the activations ---------------------------------------------------------------------
 
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+// From the exponential that is at most 1, so that the quotient's denominator is from 1 to 2 (from e^-x,
+// a share below 2^-126 came out 0: __fdividef's, beyond 2^126)
+__device__ __forceinline__ float sigmoid(float x)
+{
+    const float t = __expf(-fabsf(x));
+    return __fdividef(x < 0.f ? t : 1.f, 1.f + t);
+}
 
 // gelu's tanh form is g sigmoid(2 x), x = sqrt(2 / pi) (g + 0.044715 g^3)
 constexpr float kTanhA = 1.5957691216057308f, kTanhB = 0.044715f;
 
-// act(g); with SLOPE also act'(g).  The shares p of g are taken as sigmoids and as erfc, whose
-// relative error does not grow where they vanish.
+// act(g); with SLOPE also act'(g).  The shares p of g are taken as sigmoids and as erfc, so that nothing
+// cancels where they vanish.  Their relative error grows there with the exponential's argument x, by
+// 2^-23 |x| for its own and as much for each two roundings of x: below 2^-14 wherever bf16 still shows the
+// result, where an output's is 2^-8.
 template <int ACT, bool SLOPE>
 __device__ __forceinline__ float activate(float g, float &slope)
 {
@@ -959,7 +967,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
 
 // ---- dG and dU ---------------------------------------------------------------------------------
 // Bound by DRAM: three bf16 arrays read, two written.  8 blocks an SM walk them (8192 x 14336, silu
-// 170 us, 6.9 TB/s; a block for every 256 pieces 185).  gelu's erfc takes longer than the memory: 255.
+// 170 us, 6.9 TB/s; a block for every 256 pieces 185).  relu 177,
+// gelu_tanh 182; gelu's erfc takes longer than the memory: 251.
 struct GradArgs {
     const __nv_bfloat16 *dH, *G, *U;
     __nv_bfloat16 *dG, *dU;
