@@ -911,15 +911,20 @@ def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None,
     """(dX, dW_gate, dW_up, dG, dU) from dH and the forward's G and U.  dG may be G and dU may be U.
     need_dX=False or need_dW=False leave those products out (None); the weights' gradients are in
     `grad_dtype` (by default the weights' type) and added to with accumulate=True.  dH and X may be
-    row-strided views."""
+    row-strided views; what no asked product reads may be None (X with need_dW=False, the weights with
+    need_dX=False)."""
     ldh = _rows(dH, "dH")
     T, f = dH.shape
-    ldx = _rows(X, "X", dH.dtype)
-    d = X.shape[1]
-    if X.shape[0] != T:
+    if (need_dW and X is None) or (need_dX and (W_gate is None or W_up is None)):
+        raise ValueError("dX needs W_gate and W_up, the weights' gradients need X")
+    ldx = 0 if X is None else _rows(X, "X", dH.dtype)
+    # (without any of them nothing has a width)
+    d = next((t.shape[-1] for t in (X, W_gate, W_up) if t is not None), 8)
+    if X is not None and X.shape[0] != T:
         raise ValueError("X must have dH's rows")
     for t, name in ((W_gate, "W_gate"), (W_up, "W_up")):
-        _given(t, name, (f, d), dH.dtype)
+        if t is not None:
+            _given(t, name, (f, d), dH.dtype)
     for t, name in ((G, "G"), (U, "U")):
         _given(t, name, (T, f), dH.dtype)
     dev = dH.device
@@ -932,7 +937,7 @@ def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None,
             raise ValueError("accumulate=True needs dW_gate and dW_up")
         if dW_gate is not None and grad_dtype is None:
             grad_dtype = dW_gate.dtype
-        grad_dtype = grad_dtype or W_gate.dtype
+        grad_dtype = grad_dtype or dH.dtype
         dW_gate = _given_or(dW_gate, "dW_gate", (f, d), grad_dtype, empty, dev)
         dW_up = _given_or(dW_up, "dW_up", (f, d), grad_dtype, empty, dev)
     else:
@@ -944,8 +949,8 @@ def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None,
     else:
         _need(workspace, "workspace")
         nbytes = workspace.numel() * workspace.element_size()
-    _check(_lib.sn_glu_bwd(_error_basis(basis), _dtype(dH), dH.data_ptr(), ldh, X.data_ptr(), ldx,
-                           W_gate.data_ptr(), W_up.data_ptr(), G.data_ptr(), U.data_ptr(), T, d, f,
+    _check(_lib.sn_glu_bwd(_error_basis(basis), _dtype(dH), dH.data_ptr(), ldh, _ptr(X), ldx,
+                           _ptr(W_gate), _ptr(W_up), G.data_ptr(), U.data_ptr(), T, d, f,
                            ACTIVATIONS[act], dG.data_ptr(), dU.data_ptr(), _ptr(dX),
                            _dtype(dW_gate) if need_dW else SN_BF16, _ptr(dW_gate), _ptr(dW_up),
                            bool(accumulate), _ptr(workspace), nbytes, _stream_of(dH, stream)),
