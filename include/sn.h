@@ -462,7 +462,7 @@ sn_status sn_glu_bwd_workspace(int64_t T, int32_t d, int32_t f, size_t *bytes);
  * [T, d], or NULL (not computed; W_gate and W_up may then be NULL).  dW_gate, dW_up: [f, d]
  * in grad_dtype, added to with accumulate != 0, or both NULL (X may then be NULL).  No other
  * overlaps.  Sums are taken in a fixed order: the same inputs give the same bits.
- * workspace: 16-byte aligned, at least sn_glu_bwd_workspace bytes. */
+ * workspace: 16-byte aligned, at least sn_glu_bwd_workspace bytes (none without a product). */
 sn_status sn_glu_bwd(sn_basis_t errors, sn_dtype dtype, const void *dH, int64_t lddh, const void *X,
                      int64_t ldx, const void *W_gate, const void *W_up, const void *G, const void *U,
                      int64_t T, int32_t d, int32_t f, int32_t act, void *dG, void *dU, void *dX,

@@ -1045,7 +1045,7 @@ sn_status sn_glu_bwd(sn_basis_t errors, sn_dtype dt, const void *dH, int64_t ldd
     st = check_glu(dt, T, d, f, act, {lddh, dw ? ldx : 0});
     if (st != SN_OK || (T == 0 && (!dw || accumulate)))
         return st;
-    const size_t need = sn::glu_bwd_workspace(T, d, f), es = esize(gdt);
+    const size_t need = dx || dw ? sn::glu_bwd_workspace(T, d, f) : 0, es = esize(gdt);
     if (T > 0 && (!dH || !G || !U || !dG || !dU || (dx && (!Wg || !Wu)) || (dw && !X) ||
                   (need > 0 && (!ws || ws_bytes < need))))
         return SN_ERR_INVALID_ARG;

@@ -943,7 +943,7 @@ def sn_glu_bwd(dH, X, W_gate, W_up, G, U, act="silu", dG=None, dU=None, dX=None,
     else:
         dW_gate = dW_up = None
     if workspace is None:
-        nbytes = sn_glu_bwd_workspace(T, d, f)
+        nbytes = sn_glu_bwd_workspace(T, d, f) if need_dX or need_dW else 0
         if nbytes:
             workspace = empty(nbytes, dtype=torch.uint8, device=dev)
     else:

@@ -52,3 +52,18 @@ def test_same_bits_as_with_every_operand(sn, T, d, f):
                 sn.sn_glu_bwd(dH, None, None, None, G, U, need_dX=False, need_dW=False)):
         assert all(a is None or torch.equal(a, b) for a, b in zip(got, whole))
         assert got[3] is not None and got[4] is not None
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,f", [(40, 264, 136), (2000, 520, 2088), (1000, 8, 16), (3000, 1024, 520)])
+def test_without_products_any_workspace_will_do(sn, T, d, f):
+    """One of the size for this width, a small one, and none: dG and dU alone have no use for it."""
+    from test_glu_gpu import inputs
+    X, Wg, Wu, dH = inputs(T, d, f, 3)
+    _, G, U = sn.sn_glu_fwd(X, Wg, Wu, "silu", keep=True)
+    whole = sn.sn_glu_bwd(dH, X, Wg, Wu, G, U)
+    for operands in ((X, Wg, Wu), (None, None, None)):
+        for n in (sn.sn_glu_bwd_workspace(T, d, f), 16, None):
+            ws = None if n is None else torch.empty(max(16, n), dtype=torch.uint8, device="cuda")
+            got = sn.sn_glu_bwd(dH, *operands, G, U, need_dX=False, need_dW=False, workspace=ws)
+            assert torch.equal(got[3], whole[3]) and torch.equal(got[4], whole[4])
