@@ -49,9 +49,9 @@ struct Args {
     // [parts, d], a part a block, of dw_pre and (gated: a part a worker) of dw_post, which is S
     // itself where it is one for all tokens
     float *part_pre, *part_post;
-    // gated: S of a worker and a gate that it shares with others.  A worker shares two gates at most, the
-    // one that its first token lies inside of, at 2 w, and the one that its last does, at 2 w + 1; with
-    // fewer gates than workers (few_gates) worker w's of gate i at w + i are fewer rows.
+    // gated: S of a worker and a gate that it shares with others.  A worker shares two gates at most, its
+    // first, at 2 w, and its last, at 2 w + 1; with fewer gates than workers (few_gates) worker w's of gate
+    // i at w + i are fewer rows.
     float *part_gate;
     bool few_gates;
 };
@@ -227,10 +227,10 @@ __global__ void __launch_bounds__(kAnyThreads) k_blocknorm_any(const Args a)
 __device__ __forceinline__ int64_t first_token(int64_t w, int64_t W, int64_t T) { return w * T / W; }
 __device__ __forceinline__ int64_t worker_of(int64_t t, int64_t W, int64_t T) { return ((t + 1) * W - 1) / T; }
 
-// The row of part_gate for worker w's tokens of gate i from t on
-__device__ __forceinline__ int64_t shared_at(const Args &a, int64_t w, int64_t i, int64_t t)
+// The row of part_gate for worker w's tokens of gate i, its first gate or not
+__device__ __forceinline__ int64_t shared_at(const Args &a, int64_t w, int64_t i, bool first)
 {
-    return a.few_gates ? w + i : 2 * w + (t == i * a.per_gate);
+    return a.few_gates ? w + i : 2 * w + !first;
 }
 
 // The six sums of a row, over its elements or pairs of them
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Sh
             load_weight(a.post, j * N, w);
             Vec<T>::unpack(__ldg((const uint4 *)((const T *)a.gate + i_gate * a.d) + j), g);
             float *post = a.part_post + worker * a.d + j * N;
-            float *to = (whole ? a.dgate + i_gate * a.d : a.part_gate + shared_at(a, worker, i_gate, t0) * a.d) + j * N;
+            float *to = (whole ? a.dgate + i_gate * a.d : a.part_gate + shared_at(a, worker, i_gate, first) * a.d) + j * N;
 #pragma unroll
             for (int k = 0; k < N; k += 4) {
                 float4 q = make_float4(sum[i][k / 2].x, sum[i][k / 2].y, sum[i][k / 2 + 1].x, sum[i][k / 2 + 1].y);
@@ -637,10 +637,11 @@ __global__ void __launch_bounds__(kAnyThreads) k_blocknorm_bwd_any(const Args a)
     for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
         pre[j] = post[j] = 0.f;
     const int64_t t1 = first_token(blockIdx.x + 1, gridDim.x, a.T);
-    for (int64_t t = first_token(blockIdx.x, gridDim.x, a.T); t < t1;) {
+    int64_t t = first_token(blockIdx.x, gridDim.x, a.T);
+    for (bool first = true; t < t1; first = false) {
         const int64_t i = a.gated ? gate_of(a, t) : 0, end = a.gated ? min(t1, (i + 1) * a.per_gate) : t1;
         const bool whole = end - t == a.per_gate;
-        float *to = !a.gated ? nullptr : whole ? a.dgate + i * a.d : a.part_gate + shared_at(a, blockIdx.x, i, t) * a.d;
+        float *to = !a.gated ? nullptr : whole ? a.dgate + i * a.d : a.part_gate + shared_at(a, blockIdx.x, i, first) * a.d;
         if (to && !(whole && a.add))
             for (int j = threadIdx.x; j < a.d; j += kAnyThreads)
                 to[j] = 0.f;
@@ -732,18 +733,27 @@ __global__ void __launch_bounds__(256) k_blocknorm_dgate(const JoinArgs a)
         const int64_t y = y0 + threadIdx.y / a.runs;
         float s = 0.f, *to = nullptr;
         if (y < a.looked && j < a.d) {
-            const int64_t i = a.looked == a.gates ? y : first_token(y + 1, a.workers, a.T) / a.per_gate;
-            const int64_t w0 = worker_of(i * a.per_gate, a.workers, a.T);
-            const int64_t w1 = worker_of((i + 1) * a.per_gate - 1, a.workers, a.T);
-            if (w0 < w1 && (a.looked == a.gates || w0 == y)) {       // not one worker's, nor another warp's
+            int64_t i = y, at;                  // the gate's first part (see shared_at)
+            int parts;
+            if (a.few_gates) {
+                const int64_t w0 = worker_of(i * a.per_gate, a.workers, a.T);
+                parts = (int)(worker_of((i + 1) * a.per_gate - 1, a.workers, a.T) - w0) + 1;
+                at = w0 + i;
+            } else {
+                // a worker has a gate's tokens at least, so that two share one at most: the last of
+                // worker y's and the first of the next one's, unless that one's tokens start with it
+                const int64_t t = first_token(y + 1, a.workers, a.T);
+                i = (uint32_t)t / (uint32_t)a.per_gate;
+                parts = t > i * a.per_gate ? 2 : 1;
+                at = 2 * y + 1;
+            }
+            if (parts > 1) {                    // (else one worker has written it)
                 to = a.dgate + i * a.d + j;
-                // (see shared_at: worker w0 has the gate's first token, the others' first tokens lie inside)
-                const float *part = a.gate + (a.few_gates ? w0 + i : 2 * w0) * a.d + j;
-                const int64_t step = a.few_gates ? a.d : 2 * (int64_t)a.d, front = a.few_gates ? 0 : a.d;
-                const int parts = (int)(w1 - w0 + 1), per = (parts + a.runs - 1) / a.runs;
+                const float *part = a.gate + at * a.d + j;
+                const int per = (parts + a.runs - 1) / a.runs;
 #pragma unroll 8
                 for (int p = run * per, end = min(parts, p + per); p < end; ++p)
-                    s += __ldg(part + (p == 0 ? front : p * step));
+                    s += __ldg(part + (int64_t)p * a.d);
             }
         }
         if (a.runs > 1) {
