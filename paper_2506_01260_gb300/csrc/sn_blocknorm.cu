@@ -17,7 +17,10 @@
 //
 // Measured: forward of 16384 bf16 rows of 4096 80 us (6.7 TB/s), of 65536 of 8192 with 16 gates 644 (6.7);
 // gradient 126 us (6.4 TB/s, 5 us of it the sum of the parts) and 960 (6.7), of 4173 fp32 rows of 2056 37
-// (5.6), where the 14 rows a block walks and the sum of the parts cost latency.
+// (5.6), where the 14 rows a block walks and the sum of the parts cost latency.  fp32 forward of 16384 rows
+// of 4096 160 us (6.7).  A gate for every few tokens costs what happens between two of its rows: gradient of
+// 16384 bf16 rows of 4096, each call behind a flush of L2, 133 us without a gate, 147 with one for 128
+// tokens, 163 for 16, 200 for 3 and 307 for each.
 #include <algorithm>
 #include <atomic>
 
@@ -366,17 +369,18 @@ __device__ __forceinline__ void copy16(uint4 *to, const uint4 *from)
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// Threads of an SM that registers are kept low enough for
+// Whether a row is copied ahead (see k_blocknorm_bwd)
 template <int S, int C>
 constexpr bool is_ahead = S <= 512 && C <= 3;
-template <typename T, int S, int C>
+// Threads of an SM that registers are kept low enough for
+template <int S>
 constexpr int kBwdResident = S > 512 ? S : 512;
 
 // A worker (a warp or a block) walks its run of tokens, a row at a time, and keeps dw_pre and the
 // present gate's S of its columns in registers; m and w_pre lie in shared memory, each thread's own
 // columns.
 template <typename T, int S, int C>
-__global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<T, S, C> / Shape<S>::kThreads)
+__global__ void __launch_bounds__(Shape<S>::kThreads, kBwdResident<S> / Shape<S>::kThreads)
     k_blocknorm_bwd(const Args a)
 {
     griddep_start();

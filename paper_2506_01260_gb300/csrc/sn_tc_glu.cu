@@ -15,10 +15,13 @@
 // read B twice: 1.5 times the shared memory's traffic.)  Those of a few tokens are bound by the weights'
 // bytes, dG and dU by theirs.
 //
-// Measured, 8192 x 4096 x 14336 (T, d, f): forward 962 us (2.00 PFLOP/s), with G and U 999, dG and dU
-// 170 (6.9 TB/s), dX 995, the weights' gradients 985; at these rates the chip's power sets the clock
-// (1.63 to 1.75 GHz, tensor cores at work 94 to 95% of the cycles), and runs differ by 5%.  1 token of
-// 4096 x 14336 37.5 us (6.3 TB/s), 75 tokens 40.7, 1 of 8192 x 28672 139 (6.8 TB/s).
+// Measured, 8192 x 4096 x 14336 (T, d, f), in bursts of 20 calls: forward 949 us (2.03 PFLOP/s), with G and U
+// 981, dG and dU 171 (6.9 TB/s), beyond those dX 1041 and the weights' gradients 973; a product of the same
+// size of the vendor's library, in turn with them, 937, 1013 and 956.  The chip's power sets the clock where
+// the tensor cores are at work 93 to 95% of the cycles, in a step lower (1.46 GHz at 1.4 kW): the forward for
+// seconds 1117 us, the library's product 1107, and forward and gradients in turn 3650 us (1.58 PFLOP/s), 15%
+// more than the bursts' sum.  1 token of 4096 x 14336 37.5 us (6.3 TB/s), 75 tokens 40.5, 1 of 8192 x 28672
+// 139 (6.8 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -967,8 +970,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) k_glu_few(const __grid_constan
 
 // ---- dG and dU ---------------------------------------------------------------------------------
 // Bound by DRAM: three bf16 arrays read, two written.  8 blocks an SM walk them (8192 x 14336, silu
-// 170 us, 6.9 TB/s; a block for every 256 pieces 185).  relu 177,
-// gelu_tanh 182; gelu's erfc takes longer than the memory: 251.
+// 171 us, 6.9 TB/s, relu 177, gelu_tanh 182; a block for every 256 pieces 185).  gelu's erfc takes longer
+// than the memory: 251.
 struct GradArgs {
     const __nv_bfloat16 *dH, *G, *U;
     __nv_bfloat16 *dG, *dU;
@@ -1040,9 +1043,13 @@ __global__ void __launch_bounds__(32) k_unclaimed_timeout()
 
 // Whether X (for the weights' gradients) and the weights (for dX) are laid out anew: where neither d nor
 // f is a multiple of 64, and a copy of T d elements stands against f of their products, or one of f d
-// against T.  us, as they lie and anew: dW of 4173 x 2056 x 5512 143 and 131, 8192 x 4104 x 8200 782 and
-// 672, 512 x 8200 x 16008 255 and 224, but 16384 x 520 x 2088 94 and 101; dX of 8192 x 4104 x 8200 706 and
-// 671, 16384 x 520 x 1032 44.8 and 41.2, but 4173 x 2056 x 5512 143 and 148.
+// against T.  us, as they lie and anew.
+//   dW by f: 2088 (8192 x 520) 49.9 and 52.9, (16384 x 1032) 122 and 123; 3000 (2000 x 2056) 43.7 and 43.8,
+//   (8192) 147 and 138; 4088 (4173 x 2056) 108 and 97, 4104 111 and 102, 5512 142 and 128; 8200 (8192 x 4104)
+//   743 and 661.  (From about 3000 on it pays already, by 5 to 10%.)
+//   dX by T: 2000 (2056 x 5512) 67.9 and 80.7; 4173 144 and 148; 6000 196 and 191; 8192 259 and 253; 16384
+//   509 and 463; 8192 of 520 x 2088 44.0 and 44.6, of 4104 x 8200 702 and 662.
+// Below 2^33 products neither makes much (8192 x 520 x 1032, 0.5 of that: dX 30.9 and 29.6, dW 31.4 and 35.4).
 struct Laid {
     bool X, W;
     int64_t ld;             // elements

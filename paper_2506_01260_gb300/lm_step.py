@@ -131,16 +131,16 @@ class TwoStage:
 
     def score(self, ids, top=5):
         """For every position: the log probability of the token that follows (none for the last),
-        the entropy and the `top` alternatives.  Stage 1's activations pass through 8 bits (e4m3, a
-        scale a row), to show what that does to the scores; the products themselves are bf16."""
+        the entropy and the `top` alternatives."""
         _, _, _, x0 = self._stage0(ids)
         y1 = self._scored(self._boundary(x0, ids))
         target = torch.cat([ids[1:], ids.new_full((1,), -1)])
         logp, _, H, alt, alt_logp = sn.sn_logprob_fwd(y1 @ self.W_head.T, target, top=top)
         return logp, H, alt, alt_logp
 
-
     def _scored(self, x1):
+        """What the head reads for scores.  It passes through 8 bits (e4m3, a scale a row), to show what
+        that does to them; the products themselves are bf16."""
         codes, scale, _ = sn.sn_rmsnorm_fwd_quant(x1, self.w1, EPS, "e4m3")
         return sn.sn_quant_restore(codes, scale, "e4m3")
 
@@ -177,6 +177,7 @@ class GatedTwoStage(TwoStage):
         return sn.sn_rmsnorm_bwd(dy1, x1, self.w1, EPS, dH=dx1, dw=g["w1"])[0]
 
     def _scored(self, x1):
+        """In 16 bits, as for training; nothing is kept for a gradient."""
         return self._stage1(x1, keep=False)[0]
 
 
